@@ -7,7 +7,9 @@
  * transformer layer, and weight gradients have to be repacked between the
  * TP = t' and TP = t layouts around the data-parallel sync.  This library is
  * one GPU's part of that: the shard plan, the shard's MLP and attention
- * projection GEMMs (forward and backward), and the gradient reshard.
+ * projection GEMMs (forward and backward), the gradient reshard, and what a
+ * layer has between its GEMMs: the attention core, the norms with gate and
+ * residual, and for serving a paged key / value cache and attention over it.
  *
  * Conventions shared by every call
  *   - "device" pointers are HIP device memory owned by the caller; "host"
@@ -334,6 +336,123 @@ int ntp_attn_core_shard_bwd(ntp_handle_t* h, const ntp_attn_core_shape_t* shape,
                             void* stream);
 
 /* ---------------------------------------------------------------------------
+ * Norms of a block, with its gate and residual (what stands between the all-reduced partial sums of one
+ * layer shard call and the input of the next; every rank holds whole rows of H elements here):
+ *   r  = Z, or Norm(Z) .* post_gamma + post_beta        the norm behind the block
+ *   X' = residual_scale X + branch_scale (g .* r)       gate and residual
+ *   Y  = Norm(X') .* pre_gamma + pre_beta               the norm before the next block (on the unrounded X')
+ * with, per row t of H elements, Norm(t) = (t - mean) rstd,
+ *   NTP_NORM_RMS    mean = 0,              rstd = 1 / sqrt(sum t^2 / H + eps)
+ *   NTP_NORM_LAYER  mean = sum t / H,      rstd = 1 / sqrt(sum (t - mean)^2 / H + eps).
+ * Parts are left out by NULL: post_gamma (no norm behind the block), pre_gamma (no norm before the next one; Y
+ * must then be NULL too), the betas, and Z (no block yet: X' = X, Xout is not written and must be NULL,
+ * residual_scale and branch_scale do not count).  gate: NTP_GATE_NONE (g = 1), NTP_GATE_CHANNEL (gate = H elements, the same for every
+ * token) or NTP_GATE_TOKEN (gate = [M x H] with leading dimension ldgate).
+ * Z, Y, the gate and the norm vectors are bf16; X and X' (and their gradients) are bf16, or fp32 where residual_fp32 != 0.  Sums are
+ * fp32, each output is rounded once.  16-byte aligned base pointers; leading dimensions and H multiples of 8
+ * (fp32 matrices: of 4); H <= 32768 (UNSUPPORTED beyond); eps > 0.
+ * Matrices without rows (M = 0) may be NULL.  No buffer may alias another, with two exceptions: Xout may be X, and dX may be dXout (same pointer and leading dimension). */
+#define NTP_NORM_RMS 0
+#define NTP_NORM_LAYER 1
+#define NTP_GATE_NONE 0
+#define NTP_GATE_CHANNEL 1
+#define NTP_GATE_TOKEN 2
+typedef struct ntp_block_norm_shape {
+  int64_t M, H;
+  int32_t norm, gate;    /* NTP_NORM_*, NTP_GATE_* */
+  int32_t residual_fp32; /* 0: X, Xout and their gradients are bf16; else fp32 */
+  float eps, residual_scale, branch_scale;
+} ntp_block_norm_shape_t;
+typedef struct ntp_block_norm_weights { /* DEVICE, bf16 */
+  const void *post_gamma, *post_beta, *gate, *pre_gamma, *pre_beta;
+  int64_t ldgate; /* NTP_GATE_TOKEN only */
+} ntp_block_norm_weights_t;
+typedef struct ntp_block_norm_grads { /* DEVICE; any of them may be NULL: that gradient is not wanted */
+  float *post_gamma, *post_beta;      /* fp32 [H] */
+  void* gate;                         /* NTP_GATE_CHANNEL: fp32 [H]; NTP_GATE_TOKEN: bf16 [M x H] with leading dimension ldgate */
+  float *pre_gamma, *pre_beta;        /* fp32 [H] */
+  int64_t ldgate;                     /* NTP_GATE_TOKEN only */
+} ntp_block_norm_grads_t;
+
+/* Forward.  Stats (DEVICE, fp32 [4 x M], may be NULL): the rows' mean and rstd of the norm behind the block (rows 0, 1) and of the one
+ * before the next (rows 2, 3), which the backward call reads; rows of a norm that is left out are not
+ * written, the mean of an RMS norm is written as 0.  Xout may be NULL if only Y is wanted. */
+int ntp_block_norm_fwd(ntp_handle_t* h, const ntp_block_norm_shape_t* shape, const ntp_block_norm_weights_t* weights, const void* X,
+                       int64_t ldx, const void* Z, int64_t ldz, void* Xout, int64_t ldxo, void* Y, int64_t ldy, float* Stats, void* stream);
+/* Backward.  dXout: gradient that arrives at X' along the residual stream (NULL: none); dY: gradient at Y (NULL
+ * exactly where pre_gamma is); Xout, Z and Stats as the forward call wrote and read them (Xout: X where there was no Z; not read,
+ * and may be NULL, without pre_gamma; Z is read where post_gamma or a gate is set, and may be NULL otherwise).
+ *   G  = dXout + gradient of the norm before the next block
+ *   dX = residual_scale G,   dZ = gradient of branch_scale (g .* r) under G
+ * (dZ NULL: the forward call had no Z; post_gamma must be NULL and gate NTP_GATE_NONE, and dX = G) and the gradients of the gate and
+ * the norm vectors, sums over the tokens: fp32, in an order that M, H, the handle and its workspace fix
+ * (deterministic); accumulate != 0 adds into the fp32 ones (gradient accumulation over micro-batches).  The sums over tokens are
+ * taken by as many workgroups as the handle's workspace has room for their partial
+ * sums (ntp_workspace_bytes, NTP_CALL_BLOCK_NORM; one workgroup without a workspace: slow). */
+int ntp_block_norm_bwd(ntp_handle_t* h, const ntp_block_norm_shape_t* shape, const ntp_block_norm_weights_t* weights, const void* dXout,
+                       int64_t lddxo, const void* dY, int64_t lddy, const void* Xout, int64_t ldxo, const void* Z, int64_t ldz,
+                       const float* Stats, void* dX, int64_t lddx, void* dZ, int64_t lddz, const ntp_block_norm_grads_t* grads,
+                       int32_t accumulate, void* stream);
+
+/* ---------------------------------------------------------------------------
+ * Paged cache of the keys and values of a rank's local KV heads (serving).  K and V are DEVICE arrays of n_pages
+ * pages; a page holds page_size tokens of all kv_cnt local heads, head by head:
+ *   element (page, g, t, c) at  page * page_stride + (g * page_size + t) * head_dim + c     (bf16)
+ * so that one head's tokens of a page are one contiguous piece.  page_size: a power of two, 16 .. 65536 (UNSUPPORTED
+ * otherwise); page_stride >= kv_cnt * page_size * head_dim and a multiple of 8 (larger strides let K and V share one array); K and V 16-byte
+ * aligned.  A slot names one token's place: page * page_size + t.
+ *
+ * ntp_kv_append_shard: the tokens of QKV [M x (q_cnt + 2 kv_cnt) head_dim] (ntp_attn_proj_shard_fwd's output, columns [Q heads | K
+ * heads | V heads]) are rotated to their positions and their keys and values appended.  The first rotary_dim elements of every
+ * query and key head (a multiple of 16, <= head_dim; 0: no rotation) are rotated in pairs (x1, x2) number i = 0 .. rotary_dim / 2 - 1 by
+ * the angle a = position * inv_freq[i]:  (x1 cos a - x2 sin a, x2 cos a + x1 sin a), the pairs being elements i and i + rotary_dim / 2,
+ * or 2 i and 2 i + 1 (interleaved != 0).  Angles are formed and reduced in fp64, results rounded once.
+ *   positions  DEVICE int32 [M]     inv_freq  DEVICE fp64 [rotary_dim / 2]     (either may be NULL with rotary_dim 0)
+ *   slots      DEVICE int64 [M]: where row m's rotated keys and its values go in the cache; a row whose slot lies
+ *              outside [0, n_pages * page_size) (-1 for the padding of a batch) is not stored.  Stored rows need different slots:
+ *              where two name the same one, that slot holds pieces of either.  slots and cache may both be NULL: nothing is appended
+ *   Qout       [M x q_cnt head_dim] rotated queries, NULL: not wanted
+ *   Kout       [M x kv_cnt head_dim] rotated keys beside the cache, NULL: not wanted
+ * A prompt's rows go on to ntp_attn_core_shard_fwd, which reads packed QKV: Qout and Kout may be the query and key columns of QKV itself
+ * (QKV with ldqkv, and QKV + q_cnt * head_dim with ldqkv); no other aliasing.  head_dim 64 or 128 (UNSUPPORTED otherwise). */
+typedef struct ntp_kv_cache {
+  void *K, *V;
+  int64_t n_pages, page_stride;
+  int32_t page_size;
+} ntp_kv_cache_t;
+typedef struct ntp_kv_append_shape {
+  int64_t M;
+  int32_t q_cnt, kv_cnt, head_dim;
+  int32_t rotary_dim, interleaved;
+} ntp_kv_append_shape_t;
+int ntp_kv_append_shard(ntp_handle_t* h, const ntp_kv_append_shape_t* shape, const ntp_kv_cache_t* cache, const void* QKV, int64_t ldqkv,
+                        const int32_t* positions, const int64_t* slots, const double* inv_freq, void* Qout, int64_t ldq, void* Kout,
+                        int64_t ldk, void* stream);
+
+/* Attention of one new token per sequence over the paged cache (Eq. 5 with one query row): for sequence s and local query head j,
+ *   C[s, j] = softmax(q_j K_g^T / sqrt(head_dim)) V_g      over the first lengths[s] tokens of the sequence,
+ * the new token's key and value, appended before, included.  KV head g of query head j as in ntp_attn_core_shard_fwd.
+ *   Q            [n_seq x q_cnt head_dim] bf16: ntp_kv_append_shard's Qout (or the query columns of QKV)
+ *   block_table  DEVICE int32 [n_seq x ldt]: entry t of row s is the page that holds tokens t * page_size ..; rows need
+ *                ceil(max_len / page_size) <= ldt entries, of which those past a sequence's end are not used.  Tokens of an entry outside
+ *                [0, n_pages) are left out of the softmax
+ *   lengths      DEVICE int32 [n_seq]; 0 or less: no tokens.  max_len (host) bounds them, longer sequences are cut to it: it sizes the
+ *                launch, and a captured graph serves every length up to it
+ *   C            [n_seq x q_cnt head_dim] bf16; a sequence with no tokens gets zeros
+ *   LSE          DEVICE fp32 [q_cnt x n_seq], may be NULL: natural logarithm of the sum of exp(score); -inf for no tokens
+ * What lies in the cache behind a sequence's last token is not used (it may be NaN).  Few long sequences are cut along their length
+ * where the handle's workspace has room for the pieces' fp32 partial results (ntp_workspace_bytes, NTP_CALL_ATTN_DECODE_SHARD). */
+typedef struct ntp_attn_decode_shape {
+  int32_t n_seq, max_len;
+  int32_t q_cnt, kv_cnt;
+  int32_t q_off, kv_off, group;
+  int32_t head_dim;
+} ntp_attn_decode_shape_t;
+int ntp_attn_decode_shard(ntp_handle_t* h, const ntp_attn_decode_shape_t* shape, const ntp_kv_cache_t* cache, const void* Q, int64_t ldq,
+                          const int32_t* block_table, int64_t ldt, const int32_t* lengths, void* C, int64_t ldc, float* LSE,
+                          void* stream);
+
+/* ---------------------------------------------------------------------------
  * Weight gradients written straight into the destination layout of the
  * reshard (Sec. 3.1 "Shard-mapping algorithm"; Appendix, the pre-sync hook):
  * the gradient GEMMs of a backward call store each output row where the
@@ -511,10 +630,14 @@ int ntp_kernel_timing_read(ntp_handle_t* h, ntp_kernel_time_t* out, int64_t max_
  *   NTP_CALL_MLP_SHARD        const ntp_mlp_shape_t*        ntp_mlp_shard_fwd, _bwd, _bwd_resharded
  *   NTP_CALL_ATTN_PROJ_SHARD  const ntp_attn_shape_t*       ntp_attn_proj_shard_fwd, _bwd, _bwd_resharded
  *   NTP_CALL_ATTN_CORE_SHARD  const ntp_attn_core_shape_t*  ntp_attn_core_shard_fwd, _bwd
+ *   NTP_CALL_BLOCK_NORM       const ntp_block_norm_shape_t* ntp_block_norm_bwd (with every gradient wanted)
+ *   NTP_CALL_ATTN_DECODE_SHARD const ntp_attn_decode_shape_t* ntp_attn_decode_shard
  * Errors: NTP_ERR_INVALID_ARG (NULL, unknown call, a shape the call itself would refuse). */
 #define NTP_CALL_MLP_SHARD 0
 #define NTP_CALL_ATTN_PROJ_SHARD 1
 #define NTP_CALL_ATTN_CORE_SHARD 2
+#define NTP_CALL_BLOCK_NORM 3
+#define NTP_CALL_ATTN_DECODE_SHARD 4
 int ntp_workspace_bytes(const ntp_handle_t* h, int32_t call, const void* shape, int64_t* bytes);
 int ntp_set_workspace(ntp_handle_t* h, void* workspace, int64_t bytes);
 

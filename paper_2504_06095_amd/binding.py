@@ -45,11 +45,18 @@ NTP_PROBE_MFMA_AND_SOFTMAX = 7
 NTP_CALL_MLP_SHARD = 0
 NTP_CALL_ATTN_PROJ_SHARD = 1
 NTP_CALL_ATTN_CORE_SHARD = 2
+NTP_CALL_BLOCK_NORM = 3
+NTP_CALL_ATTN_DECODE_SHARD = 4
 # NTP_OPT_GEMM_TILE values by name
 GEMM_TILES = {"auto": 0, "generic": 1, "256x256": 2, "256x224": 3, "224x256": 4, "256x192": 5, "192x256": 6,
               "256x128": 7, "128x256": 8, "128x128": 9, "128x128w8": 10}
 NTP_GELU_ERF = 0
 NTP_GELU_TANH = 1
+NTP_NORM_RMS = 0
+NTP_NORM_LAYER = 1
+NTP_GATE_NONE = 0
+NTP_GATE_CHANNEL = 1
+NTP_GATE_TOKEN = 2
 NTP_KIND_PLAIN = 0
 NTP_KIND_QKV_GQA = 1
 
@@ -62,6 +69,7 @@ EXPORTS = (
     "ntp_mlp_shard_bwd_resharded", "ntp_attn_proj_shard_bwd_resharded", "ntp_attn_core_shard_fwd", "ntp_attn_core_shard_bwd",
     "ntp_set_workspace", "ntp_gemm_choice", "ntp_attn_core_choice", "ntp_create", "ntp_destroy", "ntp_device_info",
     "ntp_set_option", "ntp_workspace_bytes", "ntp_attn_proj_shard_fwd_static", "ntp_replica_sum", "ntp_probe_rates", "ntp_attn_core_bwd_rows",
+    "ntp_block_norm_fwd", "ntp_block_norm_bwd", "ntp_kv_append_shard", "ntp_attn_decode_shard",
 )
 
 
@@ -106,6 +114,31 @@ class AttnCoreShape(C.Structure):
     _fields_ = [("n_seq", C.c_int32), ("seq_len", C.c_int32), ("q_cnt", C.c_int32), ("kv_cnt", C.c_int32),
                 ("q_off", C.c_int32), ("kv_off", C.c_int32), ("group", C.c_int32), ("head_dim", C.c_int32),
                 ("causal", C.c_int32)]
+
+
+class BlockNormShape(C.Structure):
+    _fields_ = [("M", C.c_int64), ("H", C.c_int64), ("norm", C.c_int32), ("gate", C.c_int32), ("residual_fp32", C.c_int32),
+                ("eps", C.c_float), ("residual_scale", C.c_float), ("branch_scale", C.c_float)]
+
+
+class BlockNormWeights(C.Structure):
+    _fields_ = [(n, C.c_void_p) for n in ("post_gamma", "post_beta", "gate", "pre_gamma", "pre_beta")] + [("ldgate", C.c_int64)]
+
+
+class BlockNormGrads(C.Structure):
+    _fields_ = BlockNormWeights._fields_
+
+
+class KvCache(C.Structure):
+    _fields_ = [("K", C.c_void_p), ("V", C.c_void_p), ("n_pages", C.c_int64), ("page_stride", C.c_int64), ("page_size", C.c_int32)]
+
+
+class KvAppendShape(C.Structure):
+    _fields_ = [("M", C.c_int64)] + [(n, C.c_int32) for n in ("q_cnt", "kv_cnt", "head_dim", "rotary_dim", "interleaved")]
+
+
+class AttnDecodeShape(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("n_seq", "max_len", "q_cnt", "kv_cnt", "q_off", "kv_off", "group", "head_dim")]
 
 
 class RowSegment(C.Structure):
@@ -179,6 +212,11 @@ def lib() -> C.CDLL:
                                                         + [segp, C.c_int32, segp, C.c_int32] + [C.c_int32, vp])
         L.ntp_attn_core_shard_fwd.argtypes = [vp, C.POINTER(AttnCoreShape), vp, i64, vp, i64, vp, vp]
         L.ntp_attn_core_shard_bwd.argtypes = [vp, C.POINTER(AttnCoreShape), vp, i64, vp, i64, vp, i64, vp, vp, vp, i64, vp]
+        normp, weightp, cachep = C.POINTER(BlockNormShape), C.POINTER(BlockNormWeights), C.POINTER(KvCache)
+        L.ntp_block_norm_fwd.argtypes = [vp, normp, weightp] + [vp, i64] * 4 + [vp, vp]
+        L.ntp_block_norm_bwd.argtypes = [vp, normp, weightp] + [vp, i64] * 4 + [vp] + [vp, i64] * 2 + [C.POINTER(BlockNormGrads), C.c_int32, vp]
+        L.ntp_kv_append_shard.argtypes = [vp, C.POINTER(KvAppendShape), cachep, vp, i64, vp, vp, vp, vp, i64, vp, i64, vp]
+        L.ntp_attn_decode_shard.argtypes = [vp, C.POINTER(AttnDecodeShape), cachep, vp, i64, vp, i64, vp, vp, i64, vp, vp]
         L.ntp_kernel_timing_enable.argtypes = [vp, C.c_int32]
         L.ntp_kernel_timing_read.argtypes = [vp, C.POINTER(KernelTime), i64, C.POINTER(i64)]
         L.ntp_calibration_copy.argtypes = [vp, vp, vp, i64, vp]
@@ -419,6 +457,122 @@ def ntp_attn_core_shard_bwd(shape: AttnCoreShape, QKV, C_, dC, LSE, Delta, dQKV,
             raise TypeError("LSE / Delta: contiguous fp32 device tensors expected")
     _check(lib().ntp_attn_core_shard_bwd(_h(handle), C.byref(shape), q, ldq, c, ldc, g, ldg, LSE.data_ptr(), Delta.data_ptr(), d, ldd,
                                          _stream()), "ntp_attn_core_shard_bwd")
+
+
+def _vec(t, dtype, n=None):
+    """Device pointer of a contiguous device tensor (of n elements), or None."""
+    if t is None:
+        return None
+    if t.dtype is not dtype:
+        raise TypeError(f"expected {dtype}, got {t.dtype}")
+    if not t.is_cuda or not t.is_contiguous():
+        raise ValueError("expected a contiguous device tensor")
+    if n is not None and t.numel() != n:
+        raise ValueError(f"expected {n} elements, got {t.numel()}")
+    return t.data_ptr()
+
+
+def _rows(t, dtype, m, n, name):
+    """_mat of a tensor that must have m rows of n elements."""
+    if t is not None and tuple(t.size()) != (m, n):
+        raise ValueError(f"{name}: expected {m} x {n}, got {tuple(t.size())}")
+    p, ld = _mat(t, dtype)
+    return p, max(ld, n) if t is not None and m <= 1 else ld  # (the stride of a single row does not count)
+
+
+def block_norm_shape(M, H, norm: int = NTP_NORM_RMS, gate: int = NTP_GATE_NONE, residual_fp32: bool = False, eps: float = 1e-5,
+                     residual_scale: float = 1.0, branch_scale: float = 1.0) -> BlockNormShape:
+    return BlockNormShape(M, H, norm, gate, int(bool(residual_fp32)), eps, residual_scale, branch_scale)
+
+
+def _norm_weights(shape, torch, post_gamma, post_beta, gate, pre_gamma, pre_beta):
+    bf, H = torch.bfloat16, shape.H
+    token = shape.gate == NTP_GATE_TOKEN
+    g, ldg = _rows(gate, bf, shape.M, H, "gate") if token else (_vec(gate, bf, H), 0)
+    return BlockNormWeights(_vec(post_gamma, bf, H), _vec(post_beta, bf, H), g, _vec(pre_gamma, bf, H), _vec(pre_beta, bf, H), ldg)
+
+
+def ntp_block_norm_fwd(shape: BlockNormShape, X, Z=None, Xout=None, Y=None, Stats=None, post_gamma=None, post_beta=None, gate=None, pre_gamma=None,
+                       pre_beta=None, handle=None) -> None:
+    """X, Z [M, H] -> Xout = a X + b gate * post_norm(Z) and Y = pre_norm(Xout), [M, H]; Stats fp32 [4, M] for the backward call (optional).
+    X and Xout are bf16, or fp32 with residual_fp32; everything else is bf16."""
+    torch = _torch or _bind_torch()
+    bf, rt, M, H = torch.bfloat16, torch.float32 if shape.residual_fp32 else torch.bfloat16, shape.M, shape.H
+    w = _norm_weights(shape, torch, post_gamma, post_beta, gate, pre_gamma, pre_beta)
+    args = [*_rows(X, rt, M, H, "X"), *_rows(Z, bf, M, H, "Z"), *_rows(Xout, rt, M, H, "Xout"), *_rows(Y, bf, M, H, "Y")]
+    _check(lib().ntp_block_norm_fwd(_h(handle), C.byref(shape), C.byref(w), *args, _vec(Stats, torch.float32, 4 * M), _stream()), "ntp_block_norm_fwd")
+
+
+def ntp_block_norm_bwd(shape: BlockNormShape, dXout, dY, Xout, Z, Stats, dX, dZ, post_gamma=None, post_beta=None, gate=None, pre_gamma=None,
+                       pre_beta=None, d_post_gamma=None, d_post_beta=None, d_gate=None, d_pre_gamma=None, d_pre_beta=None, accumulate: bool = False,
+                       handle=None) -> None:
+    """Gradient of ntp_block_norm_fwd: dX, dZ [M, H] and the fp32 [H] gradients that are given (d_gate: bf16 [M, H] for a gate per token)."""
+    torch = _torch or _bind_torch()
+    bf, f32, M, H = torch.bfloat16, torch.float32, shape.M, shape.H
+    rt = f32 if shape.residual_fp32 else bf
+    w = _norm_weights(shape, torch, post_gamma, post_beta, gate, pre_gamma, pre_beta)
+    g, ldg = _rows(d_gate, bf, M, H, "d_gate") if shape.gate == NTP_GATE_TOKEN else (_vec(d_gate, f32, H), 0)
+    grads = BlockNormGrads(_vec(d_post_gamma, f32, H), _vec(d_post_beta, f32, H), g, _vec(d_pre_gamma, f32, H), _vec(d_pre_beta, f32, H), ldg)
+    args = [*_rows(dXout, rt, M, H, "dXout"), *_rows(dY, bf, M, H, "dY"), *_rows(Xout, rt, M, H, "Xout"), *_rows(Z, bf, M, H, "Z"), _vec(Stats, f32, 4 * M),
+            *_rows(dX, rt, M, H, "dX"), *_rows(dZ, bf, M, H, "dZ")]
+    _check(lib().ntp_block_norm_bwd(_h(handle), C.byref(shape), C.byref(w), *args, C.byref(grads), int(bool(accumulate)), _stream()), "ntp_block_norm_bwd")
+
+
+def kv_cache(K, V) -> KvCache:
+    """The paged cache held in two bf16 device tensors [n_pages, kv_cnt, page_size, head_dim] (pages may lie apart; inside a page they are
+    contiguous).  The tensors must outlive it."""
+    torch = _torch or _bind_torch()
+    for t in (K, V):
+        if t.dtype is not torch.bfloat16:
+            raise TypeError(f"expected {torch.bfloat16}, got {t.dtype}")
+        if not t.is_cuda or t.dim() != 4 or (t.shape[0] > 0 and not t[0].is_contiguous()):
+            raise ValueError("expected a device tensor [n_pages, kv_cnt, page_size, head_dim], contiguous inside a page")
+    if K.shape != V.shape or (K.shape[0] > 1 and K.stride(0) != V.stride(0)):
+        raise ValueError("K and V must have the same shape and the same distance between pages")
+    n, g, p, d = K.shape
+    c = KvCache(K.data_ptr() if n else None, V.data_ptr() if n else None, n, K.stride(0) if n > 1 else g * p * d, p)
+    c.kv_cnt, c.head_dim, c.tensors = g, d, (K, V)
+    return c
+
+
+def _fits_cache(cache, shape):
+    if (cache.kv_cnt, cache.head_dim) != (shape.kv_cnt, shape.head_dim):
+        raise ValueError(f"the cache holds {cache.kv_cnt} heads of {cache.head_dim}, the shape says {shape.kv_cnt} of {shape.head_dim}")
+
+
+def kv_append_shape(M, plan: dict, rotary_dim: int | None = None, interleaved: bool = False) -> KvAppendShape:
+    """Shape of the append call from a rank's ntp_attn_shard_plan; rotary_dim: the whole head unless given, 0 for no rotation."""
+    return KvAppendShape(M, plan["q_cnt"], plan["kv_cnt"], plan["head_dim"], plan["head_dim"] if rotary_dim is None else rotary_dim, int(bool(interleaved)))
+
+
+def ntp_kv_append_shard(shape: KvAppendShape, cache: KvCache | None, QKV, positions, slots, inv_freq, Qout=None, Kout=None, handle=None) -> None:
+    """QKV [M, (q_cnt + 2 kv_cnt) d] bf16: queries and keys rotated to positions (int32 [M]) by inv_freq (fp64 [rotary_dim / 2]); keys and values
+    go to slots (int64 [M], -1: nowhere) of the cache, rotated queries to Qout and keys to Kout where given."""
+    torch = _torch or _bind_torch()
+    bf, M, d = torch.bfloat16, shape.M, shape.head_dim
+    if cache is not None:
+        _fits_cache(cache, shape)
+    args = [*_rows(QKV, bf, M, (shape.q_cnt + 2 * shape.kv_cnt) * d, "QKV"), _vec(positions, torch.int32, M), _vec(slots, torch.int64, M),
+            _vec(inv_freq, torch.float64, shape.rotary_dim // 2), *_rows(Qout, bf, M, shape.q_cnt * d, "Qout"), *_rows(Kout, bf, M, shape.kv_cnt * d, "Kout")]
+    _check(lib().ntp_kv_append_shard(_h(handle), C.byref(shape), C.byref(cache) if cache is not None else None, *args, _stream()), "ntp_kv_append_shard")
+
+
+def attn_decode_shape(n_seq, max_len, plan: dict, group: int) -> AttnDecodeShape:
+    """Shape of the attention call of one new token per sequence, from a rank's ntp_attn_shard_plan and the query heads per KV head."""
+    return AttnDecodeShape(n_seq, max_len, plan["q_cnt"], plan["kv_cnt"], plan["q_off"], plan["kv_off"], group, plan["head_dim"])
+
+
+def ntp_attn_decode_shard(shape: AttnDecodeShape, cache: KvCache, Q, block_table, lengths, C_, LSE=None, handle=None) -> None:
+    """Q [n_seq, q_cnt d] bf16 over the first lengths (int32 [n_seq]) tokens in the pages block_table (int32 [n_seq, >= pages of max_len]) names
+    -> C_ [n_seq, q_cnt d] bf16 and LSE [q_cnt, n_seq] fp32 (optional)."""
+    torch = _torch or _bind_torch()
+    bf, n, w = torch.bfloat16, shape.n_seq, shape.q_cnt * shape.head_dim
+    _fits_cache(cache, shape)
+    if block_table.size(0) != n or block_table.size(1) * cache.page_size < shape.max_len:
+        raise ValueError(f"block_table: expected {n} rows of at least {-(-shape.max_len // cache.page_size)} pages, got {tuple(block_table.size())}")
+    t, ldt = _rows(block_table, torch.int32, n, block_table.size(1), "block_table")
+    _check(lib().ntp_attn_decode_shard(_h(handle), C.byref(shape), C.byref(cache), *_rows(Q, bf, n, w, "Q"), t, ldt, _vec(lengths, torch.int32, n),
+                                       *_rows(C_, bf, n, w, "C_"), _vec(LSE, torch.float32, n * shape.q_cnt), _stream()), "ntp_attn_decode_shard")
 
 
 def ntp_reshard_row_segments(spec: TensorSpec, src_tp: int, src_rank: int, dst_tp: int, dst_shards):

@@ -284,6 +284,12 @@ extern "C" int ntp_workspace_bytes(const ntp_handle_t* h, int32_t call, const vo
   } else if (call == NTP_CALL_ATTN_CORE_SHARD) {
     const int st = ntp::attn_core_workspace_wish(h, static_cast<const ntp_attn_core_shape_t*>(shape), &need);
     if (st != NTP_OK) return st;
+  } else if (call == NTP_CALL_BLOCK_NORM) {
+    const int st = ntp::block_norm_workspace_wish(h, static_cast<const ntp_block_norm_shape_t*>(shape), &need);
+    if (st != NTP_OK) return st;
+  } else if (call == NTP_CALL_ATTN_DECODE_SHARD) {
+    const int st = ntp::attn_decode_workspace_wish(h, static_cast<const ntp_attn_decode_shape_t*>(shape), &need);
+    if (st != NTP_OK) return st;
   } else {
     return NTP_ERR_INVALID_ARG;
   }
