@@ -437,7 +437,7 @@ int ntp_kv_append_shard(ntp_handle_t* h, const ntp_kv_append_shape_t* shape, con
  *                ceil(max_len / page_size) <= ldt entries, of which those past a sequence's end are not used.  Tokens of an entry outside
  *                [0, n_pages) are left out of the softmax
  *   lengths      DEVICE int32 [n_seq]; 0 or less: no tokens.  max_len (host) bounds them, longer sequences are cut to it: it sizes the
- *                launch, and a captured graph serves every length up to it
+ *                launch, and a captured graph serves every length up to it.  At most 2^30 (UNSUPPORTED beyond)
  *   C            [n_seq x q_cnt head_dim] bf16; a sequence with no tokens gets zeros
  *   LSE          DEVICE fp32 [q_cnt x n_seq], may be NULL: natural logarithm of the sum of exp(score); -inf for no tokens
  * What lies in the cache behind a sequence's last token is not used (it may be NaN).  Few long sequences are cut along their length

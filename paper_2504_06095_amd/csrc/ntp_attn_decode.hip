@@ -1,96 +1,341 @@
 // Attention of one new token per sequence over the paged key / value cache (ntp_attn_decode_shard): for sequence s and query head j
 //   C[s, j] = sum_t p_t V[t] / sum_t p_t,   p_t = exp(q_j . K[t] / sqrt(d) - max),   t over the sequence's tokens.
-// One pass over the keys with a running maximum and sum.  Every key and value is used by the query heads of one KV head only, 4 d bytes for
-// 4 d operations a query head: HBM bounds it.
+// One pass over the keys with a running maximum and sum.  Every key and value is read once, 4 d bytes for 4 d operations a query head: HBM bounds it.
+//
+// A workgroup takes a piece of one sequence's tokens for (up to) 16 query heads of one KV head; its four wavefronts take its tiles of 8 KB of keys and 8 KB
+// of values in turn, each with a running maximum and sum of its own, and put their results together at the end.  Both products run on the
+// 16x16x32 bf16 matrix instruction with the query head on the lane axis (S^T = K Q^T, O^T += V^T P^T), the scores go from the one to the other in
+// registers.  With one query head 15 of 16 columns are idle: matrix work is far from the bound, 16 instructions a tile against 16 KB from HBM.
+// Keys go from memory straight to the fragments' registers; values, needed transposed, through a part of the LDS that is the wavefront's own, by DMA, so that
+// nothing but the end needs a barrier.  What hides the latency is the number of wavefronts: 16 KB in flight for each.
+//
+// A page holds a multiple of 16 tokens, so 16 tokens of one head are one contiguous block; each block is a buffer view of its own that ends with the
+// sequence: what lies behind the last token, or in a page that does not exist, reads as zeros and never reaches the products (it may be NaN).
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
 #include <cmath>
 #include <cstdint>
 
+#include "ntp_gemm_kernels.h"
+#include "ntp_gemm_ring.h"
 #include "ntp_internal.h"
 #include "ntp_kv_cache.h"
 
 namespace {
 
 using ntp::off16;
+using ntp_gemm::bf16x8;
+using ntp_gemm::f32x4;
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
-constexpr int kThreads = 256;
+constexpr int kThreads = 256, kWaves = 4, kBlock = 16;  // kBlock: tokens of a contiguous block
+constexpr int kTileBytes = 8192;                        // of keys, and of values, per tile
+template <int D>
+constexpr int kTile = kTileBytes / (2 * D);  // tokens per tile: 32 or 64
 
 struct DecodeArgs {
   const uint16_t *Q, *K, *V;
   const int32_t *table, *lengths;
   uint16_t* C;
   float* LSE;
+  float* parts;  // pieces > 1: [n_seq x q_cnt][pieces][D + 4]: unnormalised output, maximum (log2 units), sum
   int64_t ldq, ldc, ldt, page_stride, n_pages;
   int32_t n_seq, max_len, q_cnt, q_off, kv_off, group, page_size, page_log2;
-  float scale_log2;  // log2(e) / sqrt(d)
+  int32_t kv_first, kv_used, head_tiles;  // local KV heads that are read; 16-head tiles of a KV head's query heads
+  int32_t pieces, piece_len;              // a sequence is cut into pieces of piece_len tokens
+  float scale_log2;                       // log2(e) / sqrt(d)
 };
 
-__device__ __forceinline__ float bf_lo(uint32_t v) { return __builtin_bit_cast(float, v << 16); }
-__device__ __forceinline__ float bf_hi(uint32_t v) { return __builtin_bit_cast(float, v & 0xffff0000u); }
+__device__ __forceinline__ float fast_exp2(float x) { return __builtin_amdgcn_exp2f(x); }
 
-// One workgroup per (sequence, query head): D / 8 lanes share a key, 16 bytes each.
+// Maximum / sum over the four lanes l % 16 + {0, 16, 32, 48}, left in all four: the 16-lane rows, then the halves trade places in registers.
+template <typename F>
+__device__ __forceinline__ float over_rows(float v, F&& f) {
+  {
+    const uint32_t x = __builtin_bit_cast(uint32_t, v);
+    const auto r = __builtin_amdgcn_permlane16_swap(x, x, false, false);
+    const uint32_t r0 = r[0], r1 = r[1];
+    v = f(__builtin_bit_cast(float, r0), __builtin_bit_cast(float, r1));
+  }
+  const uint32_t x = __builtin_bit_cast(uint32_t, v);
+  const auto r = __builtin_amdgcn_permlane32_swap(x, x, false, false);
+  const uint32_t r0 = r[0], r1 = r[1];
+  return f(__builtin_bit_cast(float, r0), __builtin_bit_cast(float, r1));
+}
+
+// `bytes` bytes at p; what lies behind them reads as zeros.
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t view(const uint16_t* p, int bytes) {
+  return __builtin_amdgcn_make_buffer_rsrc(const_cast<uint16_t*>(p), 0, bytes, 0x00020000);
+}
+__device__ __forceinline__ bf16x8 load_16(__amdgpu_buffer_rsrc_t rs, uint32_t off) {
+  return __builtin_bit_cast(bf16x8, __builtin_amdgcn_raw_buffer_load_b128(rs, off, 0, 0));
+}
+__device__ __forceinline__ void dma_16(__amdgpu_buffer_rsrc_t rs, unsigned char* dst, uint32_t off) {
+  __builtin_amdgcn_raw_ptr_buffer_load_lds(rs, (ntp_gemm::lds_void*)dst, 16, off, 0, 0, 0);
+}
+__device__ __forceinline__ void dma_done() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
+
+template <int OFF>
+__device__ __forceinline__ u32x2 lds_tr_b64(uint32_t addr) {
+#if !defined(__HIP_DEVICE_COMPILE__)
+  return u32x2{};
+#else
+  u32x2 v;
+  asm volatile("ds_read_b64_tr_b16 %0, %1 offset:%2" : "=v"(v) : "v"(addr), "n"(OFF) : "memory");
+  return v;
+#endif
+}
+// The reads requested before have arrived: every later use of their registers depends on this wait.
+__device__ __forceinline__ void lds_reads_done(u32x2 (&r)[16]) {
+#if defined(__HIP_DEVICE_COMPILE__)
+  asm volatile("s_waitcnt lgkmcnt(0)"
+               : "+v"(r[0]), "+v"(r[1]), "+v"(r[2]), "+v"(r[3]), "+v"(r[4]), "+v"(r[5]), "+v"(r[6]), "+v"(r[7])
+               :
+               : "memory");
+  asm volatile("" : "+v"(r[8]), "+v"(r[9]), "+v"(r[10]), "+v"(r[11]), "+v"(r[12]), "+v"(r[13]), "+v"(r[14]), "+v"(r[15]) : : "memory");
+#endif
+}
+
+template <int... Is, typename F>
+__device__ __forceinline__ void unrolled(std::integer_sequence<int, Is...>, F&& f) {
+  (f(std::integral_constant<int, Is>{}), ...);
+}
+
+// Rows of D values in the LDS hold their 16-byte chunks permuted: chunk c of row r sits at slot c ^ swz(r), so that the rows that a transposing read
+// touches per cycle lie on distinct banks (as the attention core's tiles).
 template <int D>
-__global__ __launch_bounds__(kThreads) void attn_decode_kernel(const DecodeArgs a) {
-  constexpr int LPK = D / 8, KEYS = kThreads / LPK;  // lanes per key, keys at a time
-  __shared__ float part[KEYS][D + 2];
-  const int head = blockIdx.x % a.q_cnt, seq = blockIdx.x / a.q_cnt;
-  const int g = (a.q_off + head) / a.group - a.kv_off;
+__device__ __forceinline__ uint32_t swz(int r) {
+  return D == 128 ? uint32_t((r & 7) << 1) : uint32_t(((r >> 1) & 3) << 1);
+}
+
+template <int D>
+__global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(3))) void attn_decode_kernel(const DecodeArgs a) {
+  constexpr int KS = D / 32, DB = D / 16;           // K-steps of the score product, 16-column blocks of the output
+  constexpr int T = kTile<D>, NB = T / kBlock;      // tokens and blocks per tile
+  constexpr int BLOCK_BYTES = kBlock * D * 2, DMA = BLOCK_BYTES / 1024;  // DMA instructions per block
+  constexpr int ROW = D + 4;                        // floats of a wavefront's result row: outputs, maximum, sum
+  constexpr int LDS = kWaves * std::max(kTileBytes, 16 * ROW * 4);
+  __shared__ __attribute__((aligned(1024))) unsigned char lds[LDS];
+
+  const int units = a.kv_used * a.head_tiles * a.n_seq;
+  const int piece = int(blockIdx.x) / units, unit = int(blockIdx.x) % units;  // (the pieces that every sequence has go first)
+  const int seq = unit % a.n_seq, tile16 = unit / a.n_seq % a.head_tiles, g = a.kv_first + unit / a.n_seq / a.head_tiles;
   const int len = std::min(a.lengths[seq], a.max_len);
-  const int sub = threadIdx.x % LPK, slot = threadIdx.x / LPK;
-  const u32x4 qr = *reinterpret_cast<const u32x4*>(a.Q + int64_t(seq) * a.ldq + int64_t(head) * D + sub * 8);
-  float q[8], acc[8] = {}, m = -INFINITY, l = 0.f;
+  const int k_lo = piece * a.piece_len, k_hi = std::min(len, k_lo + a.piece_len);
+  if (piece > 0 && k_lo >= len) return;
+  // this KV head's local query heads, and the 16 (or fewer) of this workgroup
+  const int64_t first = int64_t(a.kv_off + g) * a.group - a.q_off;
+  const int j0 = int(std::max<int64_t>(first, 0)) + tile16 * 16, j1 = int(std::min<int64_t>(std::min<int64_t>(first + a.group, a.q_cnt), j0 + 16));
+  if (j0 >= j1) return;
+
+  const int lane = threadIdx.x & 63, lq = lane & 15, lh = lane >> 4;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  unsigned char* const sV = lds + wave * kTileBytes;
+  const uint32_t lV = uint32_t(reinterpret_cast<uintptr_t>(sV));
+
+  bf16x8 qf[KS] = {};  // operand B[k][j]: j = query head (lane % 16), k = 8 consecutive columns
+  if (j0 + lq < j1) {
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    q[2 * i] = bf_lo(qr[i]) * a.scale_log2;
-    q[2 * i + 1] = bf_hi(qr[i]) * a.scale_log2;
+    for (int ks = 0; ks < KS; ++ks) qf[ks] = *reinterpret_cast<const bf16x8*>(a.Q + int64_t(seq) * a.ldq + int64_t(j0 + lq) * D + ks * 32 + lh * 8);
   }
-  for (int key = slot; key < len; key += KEYS) {
-    const int page = a.table[int64_t(seq) * a.ldt + (key >> a.page_log2)];
-    if (page < 0 || page >= a.n_pages) continue;
-    const int64_t at = int64_t(page) * a.page_stride + (int64_t(g) * a.page_size + (key & (a.page_size - 1))) * D + sub * 8;
-    const u32x4 k = *reinterpret_cast<const u32x4*>(a.K + at), v = *reinterpret_cast<const u32x4*>(a.V + at);
-    float s = 0.f;
+
+  // lane offsets: key fragments (row lane % 16, columns lane / 16 * 8 on), DMA of a block's chunks, transposing reads
+  const uint32_t koff = uint32_t(lq * D + lh * 8) * 2;
+  uint32_t voff[DMA], col[DB];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) s = fmaf(q[2 * i], bf_lo(k[i]), fmaf(q[2 * i + 1], bf_hi(k[i]), s));
+  for (int i = 0; i < DMA; ++i) {
+    const int p = i * 64 + lane, row = p / (D / 8), slot = p % (D / 8);
+    voff[i] = uint32_t(row * D * 2) + ((uint32_t(slot) ^ swz<D>(row)) * 16u);
+  }
+  const int rv = lh * 4 + (lq >> 2);
 #pragma unroll
-    for (int x = 1; x < LPK; x *= 2) s += __shfl_xor(s, x);
-    const float m_new = fmaxf(m, s), m_use = m_new == -INFINITY ? 0.f : m_new;  // (no score above -inf so far: weights of 0)
-    const float alpha = exp2f(m - m_use), p = exp2f(s - m_use);
-    l = l * alpha + p;
-    m = m_new;
+  for (int db = 0; db < DB; ++db) col[db] = lV + uint32_t(rv * D * 2) + uint32_t(lq & 1) * 8u + ((uint32_t(db * 2 + ((lq & 3) >> 1)) ^ swz<D>(rv)) * 16u);
+
+  f32x4 acc[DB];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      acc[2 * i] = fmaf(acc[2 * i], alpha, p * bf_lo(v[i]));
-      acc[2 * i + 1] = fmaf(acc[2 * i + 1], alpha, p * bf_hi(v[i]));
+  for (int db = 0; db < DB; ++db) acc[db] = f32x4{0.f, 0.f, 0.f, 0.f};
+  float m_run = -INFINITY, l_run = 0.f;
+
+  // page numbers of the wavefront's next 64 blocks, one a lane: its tile number i is tile i * kWaves + wave of the piece
+  const int32_t* const row_of_table = a.table + int64_t(seq) * a.ldt;
+  auto pages_from = [&](int i) {
+    const int key = k_lo + ((i + lane / NB) * kWaves + wave) * T + (lane % NB) * kBlock;
+    return key < k_hi ? row_of_table[key >> a.page_log2] : -1;
+  };
+  const int n_tiles = std::max(0, (k_hi - k_lo + T - 1) / T);
+  int32_t pages = pages_from(0);
+  for (int i = 0; i * kWaves + wave < n_tiles; ++i) {
+    if (i > 0 && i % (64 / NB) == 0) pages = pages_from(i);
+    const int key0 = k_lo + (i * kWaves + wave) * T;
+    bf16x8 kf[NB][KS];
+    int valid[NB];
+#pragma unroll
+    for (int b = 0; b < NB; ++b) {
+      const int key = key0 + b * kBlock;
+      const int page = __builtin_amdgcn_readlane(pages, (i % (64 / NB)) * NB + b);
+      const bool there = page >= 0 && page < a.n_pages;
+      valid[b] = there ? std::min(std::max(k_hi - key, 0), kBlock) : 0;
+      const int64_t at = there ? int64_t(page) * a.page_stride + (int64_t(g) * a.page_size + (key & (a.page_size - 1))) * D : 0;
+      const __amdgpu_buffer_rsrc_t keys = view(a.K + at, valid[b] * D * 2), values = view(a.V + at, valid[b] * D * 2);
+#pragma unroll
+      for (int ks = 0; ks < KS; ++ks) kf[b][ks] = load_16(keys, koff + ks * 64);
+#pragma unroll
+      for (int j = 0; j < DMA; ++j) dma_16(values, sV + b * BLOCK_BYTES + j * 1024, voff[j]);
     }
-  }
+    // scores, transposed: st[b][r] = score of query head lane % 16 with token key0 + b * 16 + lane / 16 * 4 + r
+    f32x4 st[NB];
 #pragma unroll
-  for (int i = 0; i < 8; ++i) part[slot][sub * 8 + i] = acc[i];
-  if (sub == 0) {
-    part[slot][D] = m;
-    part[slot][D + 1] = l;
+    for (int b = 0; b < NB; ++b) {
+      st[b] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int ks = 0; ks < KS; ++ks) st[b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf[b][ks], qf[ks], st[b], 0, 0, 0);
+      if (valid[b] < kBlock) {
+#pragma unroll
+        for (int r = 0; r < 4; ++r)
+          if (lh * 4 + r >= valid[b]) st[b][r] = -INFINITY;
+      }
+    }
+    float mx = -INFINITY;
+#pragma unroll
+    for (int b = 0; b < NB; ++b)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) mx = fmaxf(mx, st[b][r]);
+    mx = over_rows(mx, [](float x, float y) { return fmaxf(x, y); }) * a.scale_log2;
+    const float m_new = fmaxf(m_run, mx), m_use = m_new == -INFINITY ? 0.f : m_new;  // (no score above -inf so far: weights of 0)
+    const float alpha = fast_exp2(m_run - m_use);
+    float ls = 0.f;
+    bf16x8 pf[NB / 2];  // weights as operand B of the second product, per 32 tokens (rounded to bf16 for it; their sum is not)
+#pragma unroll
+    for (int b = 0; b < NB; ++b)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        const float p = fast_exp2(fmaf(st[b][r], a.scale_log2, -m_use));
+        ls += p;
+        pf[b / 2][(b & 1) * 4 + r] = static_cast<__bf16>(p);
+      }
+    l_run = l_run * alpha + ls;  // of this lane's tokens; the four lane groups are added at the end
+    m_run = m_new;
+    if (__any(alpha != 1.0f)) {
+#pragma unroll
+      for (int db = 0; db < DB; ++db) acc[db] *= alpha;
+    }
+    dma_done();  // the values are in the LDS
+    u32x2 vf[16];  // [(db * NB / 2 + s2) * 2 + half]
+    unrolled(std::make_integer_sequence<int, 16>{}, [&](auto n) {
+      constexpr int db = decltype(n)::value / NB, q = decltype(n)::value % NB;
+      vf[decltype(n)::value] = lds_tr_b64<q * BLOCK_BYTES>(col[db]);
+    });
+    lds_reads_done(vf);
+#pragma unroll
+    for (int db = 0; db < DB; ++db)
+#pragma unroll
+      for (int s2 = 0; s2 < NB / 2; ++s2) {
+        const u32x2 lo = vf[db * NB + s2 * 2], hi = vf[db * NB + s2 * 2 + 1];
+        const u32x4 both = {lo[0], lo[1], hi[0], hi[1]};
+        acc[db] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, both), pf[s2], acc[db], 0, 0, 0);
+      }
+  }
+
+  // the wavefronts' results, one row per query head
+  l_run = over_rows(l_run, [](float x, float y) { return x + y; });
+  __syncthreads();
+  float* const mine = reinterpret_cast<float*>(lds) + (wave * 16 + lq) * ROW;
+#pragma unroll
+  for (int db = 0; db < DB; ++db) *reinterpret_cast<f32x4*>(mine + db * 16 + lh * 4) = acc[db];
+  if (lh == 0) {
+    mine[D] = m_run;
+    mine[D + 1] = l_run;
   }
   __syncthreads();
-  if (threadIdx.x >= D) return;
-  float top = -INFINITY, sum = 0.f, o = 0.f;
-  for (int i = 0; i < KEYS; ++i) top = fmaxf(top, part[i][D]);
-  if (top == -INFINITY) top = 0.f;
-  for (int i = 0; i < KEYS; ++i) {
-    const float w = exp2f(part[i][D] - top);
-    sum = fmaf(w, part[i][D + 1], sum);
-    o = fmaf(w, part[i][threadIdx.x], o);
+  const int row = threadIdx.x >> 4, c0 = (threadIdx.x & 15) * 4, head = j0 + row;
+  if (head >= j1) return;
+  const float* const res = reinterpret_cast<const float*>(lds) + row * ROW;
+  float top = -INFINITY, w[kWaves], sum = 0.f;
+#pragma unroll
+  for (int i = 0; i < kWaves; ++i) top = fmaxf(top, res[i * 16 * ROW + D]);
+  const float base = top == -INFINITY ? 0.f : top;
+#pragma unroll
+  for (int i = 0; i < kWaves; ++i) {
+    w[i] = fast_exp2(res[i * 16 * ROW + D] - base);
+    sum = fmaf(w[i], res[i * 16 * ROW + D + 1], sum);
   }
-  a.C[int64_t(seq) * a.ldc + int64_t(head) * D + threadIdx.x] = __builtin_bit_cast(uint16_t, static_cast<__bf16>(sum == 0.f ? 0.f : o / sum));
-  if (a.LSE && threadIdx.x == 0) a.LSE[int64_t(head) * a.n_seq + seq] = (top + log2f(sum)) * 0.6931471805599453f;
+  float* const part = a.parts + ((int64_t(seq) * a.q_cnt + head) * a.pieces + piece) * (D + 4);
+  const float inv = sum == 0.f ? 0.f : 1.0f / sum;
+#pragma unroll
+  for (int c = c0; c < D; c += 64) {
+    f32x4 o = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int i = 0; i < kWaves; ++i) o += w[i] * *reinterpret_cast<const f32x4*>(res + i * 16 * ROW + c);
+    if (a.pieces > 1) {
+      *reinterpret_cast<f32x4*>(part + c) = o;
+    } else {
+      ntp_gemm::u16x4 out;
+#pragma unroll
+      for (int r = 0; r < 4; ++r) out[r] = ntp_gemm::f32_to_bf16(o[r] * inv);
+      *reinterpret_cast<ntp_gemm::u16x4*>(a.C + int64_t(seq) * a.ldc + int64_t(head) * D + c) = out;
+    }
+  }
+  if (c0 == 0) {
+    if (a.pieces > 1) {
+      part[D] = top;
+      part[D + 1] = sum;
+    } else if (a.LSE) {
+      a.LSE[int64_t(head) * a.n_seq + seq] = (base + log2f(sum)) * 0.6931471805599453f;
+    }
+  }
+}
+
+// The pieces of one (sequence, query head) put together: D / 4 lanes hold the outputs, 1024 / D groups of them take the pieces in turn.
+template <int D>
+__global__ __launch_bounds__(kThreads) void attn_decode_join_kernel(const DecodeArgs a) {
+  constexpr int L = D / 4, G = kThreads / L;
+  __shared__ float lds[G][D + 4];
+  const int row = blockIdx.x, head = row % a.q_cnt, seq = row / a.q_cnt;
+  const int len = std::min(a.lengths[seq], a.max_len);
+  const int used = len > 0 ? (len + a.piece_len - 1) / a.piece_len : 0;
+  const int grp = threadIdx.x / L, c = threadIdx.x % L * 4;
+  const float* const parts = a.parts + int64_t(row) * a.pieces * (D + 4);
+  f32x4 o = {0.f, 0.f, 0.f, 0.f};
+  float m = -INFINITY, l = 0.f;
+  for (int i = grp; i < used; i += G) {
+    const float* p = parts + int64_t(i) * (D + 4);
+    const f32x4 v = *reinterpret_cast<const f32x4*>(p + c);
+    const float m_new = fmaxf(m, p[D]), base = m_new == -INFINITY ? 0.f : m_new;
+    const float w0 = fast_exp2(m - base), w1 = fast_exp2(p[D] - base);
+    o = o * w0 + v * w1;
+    l = l * w0 + p[D + 1] * w1;
+    m = m_new;
+  }
+  *reinterpret_cast<f32x4*>(&lds[grp][c]) = o;
+  if (c == 0) {
+    lds[grp][D] = m;
+    lds[grp][D + 1] = l;
+  }
+  __syncthreads();
+  if (grp > 0) return;
+  float top = -INFINITY, sum = 0.f;
+  for (int i = 0; i < G; ++i) top = fmaxf(top, lds[i][D]);
+  const float base = top == -INFINITY ? 0.f : top;
+  o = f32x4{0.f, 0.f, 0.f, 0.f};
+  for (int i = 0; i < G; ++i) {
+    const float w = fast_exp2(lds[i][D] - base);
+    sum = fmaf(w, lds[i][D + 1], sum);
+    o += w * *reinterpret_cast<const f32x4*>(&lds[i][c]);
+  }
+  const float inv = sum == 0.f ? 0.f : 1.0f / sum;
+  ntp_gemm::u16x4 out;
+#pragma unroll
+  for (int r = 0; r < 4; ++r) out[r] = ntp_gemm::f32_to_bf16(o[r] * inv);
+  *reinterpret_cast<ntp_gemm::u16x4*>(a.C + int64_t(seq) * a.ldc + int64_t(head) * D + c) = out;
+  if (a.LSE && c == 0) a.LSE[int64_t(head) * a.n_seq + seq] = (base + log2f(sum)) * 0.6931471805599453f;
 }
 
 int check_decode_shape(const ntp_attn_decode_shape_t* s) {
   if (!s || s->n_seq < 0 || s->max_len < 0 || s->q_cnt < 0 || s->kv_cnt < 0 || s->q_off < 0 || s->kv_off < 0 || s->group < 1) return NTP_ERR_INVALID_ARG;
   if (s->head_dim != 64 && s->head_dim != 128) return NTP_ERR_UNSUPPORTED;
-  if (int64_t(s->n_seq) * s->q_cnt > 0x7fffffffll || int64_t(s->q_off) + s->q_cnt > 0x7fffffffll) return NTP_ERR_UNSUPPORTED;
+  if (s->max_len > 1 << 30 || int64_t(s->n_seq) * s->q_cnt > 0x7fffffffll || int64_t(s->q_off) + s->q_cnt > 0x7fffffffll) return NTP_ERR_UNSUPPORTED;
   // the KV heads of the local query heads ascend: the first and the last must be local
   if (s->q_cnt > 0) {
     const int64_t first = int64_t(s->q_off) / s->group - s->kv_off, last = (int64_t(s->q_off) + s->q_cnt - 1) / s->group - s->kv_off;
@@ -99,11 +344,40 @@ int check_decode_shape(const ntp_attn_decode_shape_t* s) {
   return NTP_OK;
 }
 
+struct DecodeChoice {
+  int32_t kv_first, kv_used, head_tiles, pieces, piece_len;
+  int64_t units, ws_bytes;
+};
+
+// How a call is cut.  One workgroup per unit (sequence, KV head, 16 query heads) and piece; pieces are cut so that a launch has some workgroups for
+// every compute unit, but not below one tile for each wavefront.
+DecodeChoice choose_decode(const ntp_handle* h, int64_t ws_bytes, const ntp_attn_decode_shape_t* s) {
+  DecodeChoice c{};
+  c.pieces = 1;
+  c.piece_len = std::max(s->max_len, 1);
+  if (s->q_cnt == 0 || s->n_seq == 0) return c;
+  c.kv_first = s->q_off / s->group - s->kv_off;
+  c.kv_used = (s->q_off + s->q_cnt - 1) / s->group - s->kv_off - c.kv_first + 1;
+  c.head_tiles = (std::min(s->group, s->q_cnt) + 15) / 16;
+  c.units = int64_t(c.kv_used) * c.head_tiles * s->n_seq;
+  const int64_t step = kWaves * (kTileBytes / (2 * s->head_dim));
+  const int64_t want = std::max<int64_t>(1, 8 * int64_t(h->compute_units) / c.units);
+  const int64_t per = std::max<int64_t>((s->max_len + want - 1) / want, 2 * step);
+  const int64_t len = (per + step - 1) / step * step, pieces = (s->max_len + len - 1) / len;
+  const int64_t bytes = int64_t(s->n_seq) * s->q_cnt * pieces * (s->head_dim + 4) * 4;
+  if (pieces > 1 && bytes <= ws_bytes && pieces * c.units <= 0x7fffffffll) {
+    c.pieces = int32_t(pieces);
+    c.piece_len = int32_t(len);
+    c.ws_bytes = bytes;
+  }
+  return c;
+}
+
 }  // namespace
 
-int ntp::attn_decode_workspace_wish(const ntp_handle*, const ntp_attn_decode_shape_t* s, int64_t* bytes) {
+int ntp::attn_decode_workspace_wish(const ntp_handle* h, const ntp_attn_decode_shape_t* s, int64_t* bytes) {
   if (check_decode_shape(s) != NTP_OK) return NTP_ERR_INVALID_ARG;
-  *bytes = 0;
+  *bytes = choose_decode(h, INT64_MAX, s).ws_bytes;
   return NTP_OK;
 }
 
@@ -119,19 +393,28 @@ extern "C" int ntp_attn_decode_shard(ntp_handle_t* h, const ntp_attn_decode_shap
   auto off4 = [](const void* p) { return (reinterpret_cast<uintptr_t>(p) & 3) != 0; };
   if (off16(Q) || off16(C) || ldq % 8 || ldc % 8 || off4(block_table) || off4(lengths) || off4(LSE)) return NTP_ERR_ALIGNMENT;
   if (h->device < 0) return NTP_ERR_NO_DEVICE;
+  const DecodeChoice c = choose_decode(h, h->workspace ? h->workspace_bytes : 0, s);
+  if (c.units > 0x7fffffffll) return NTP_ERR_UNSUPPORTED;
   DecodeArgs a{};
   a.Q = static_cast<const uint16_t*>(Q), a.K = static_cast<const uint16_t*>(cache->K), a.V = static_cast<const uint16_t*>(cache->V);
-  a.table = block_table, a.lengths = lengths, a.C = static_cast<uint16_t*>(C), a.LSE = LSE;
+  a.table = block_table, a.lengths = lengths, a.C = static_cast<uint16_t*>(C), a.LSE = LSE, a.parts = static_cast<float*>(h->workspace);
   a.ldq = ldq, a.ldc = ldc, a.ldt = ldt, a.page_stride = cache->page_stride, a.n_pages = cache->n_pages;
   a.n_seq = s->n_seq, a.max_len = s->max_len, a.q_cnt = s->q_cnt, a.q_off = s->q_off, a.kv_off = s->kv_off, a.group = s->group;
   a.page_size = cache->page_size, a.page_log2 = ntp::log2_of(cache->page_size);
+  a.kv_first = c.kv_first, a.kv_used = c.kv_used, a.head_tiles = c.head_tiles, a.pieces = c.pieces, a.piece_len = c.piece_len;
   a.scale_log2 = float(1.4426950408889634 / std::sqrt(double(s->head_dim)));
   hipStream_t hs = static_cast<hipStream_t>(stream);
-  if (ntp::timing_on(h)) ntp::timing_begin(h, stream, "attn_decode", 4.0 * s->n_seq * double(s->max_len) * s->head_dim * s->q_cnt, 0.0);
-  const dim3 grid(uint32_t(int64_t(s->n_seq) * s->q_cnt));
+  if (ntp::timing_on(h))
+    ntp::timing_begin(h, stream, c.pieces > 1 ? "attn_decode_cut" : "attn_decode", 4.0 * s->n_seq * double(s->max_len) * s->head_dim * s->q_cnt, 0.0);
+  const dim3 grid(uint32_t(c.units * c.pieces)), joins(uint32_t(int64_t(s->n_seq) * s->q_cnt));
   if (s->head_dim == 128) hipLaunchKernelGGL(attn_decode_kernel<128>, grid, dim3(kThreads), 0, hs, a);
   else hipLaunchKernelGGL(attn_decode_kernel<64>, grid, dim3(kThreads), 0, hs, a);
-  const bool ok = hipGetLastError() == hipSuccess;
+  bool ok = hipGetLastError() == hipSuccess;
+  if (ok && c.pieces > 1) {
+    if (s->head_dim == 128) hipLaunchKernelGGL(attn_decode_join_kernel<128>, joins, dim3(kThreads), 0, hs, a);
+    else hipLaunchKernelGGL(attn_decode_join_kernel<64>, joins, dim3(kThreads), 0, hs, a);
+    ok = hipGetLastError() == hipSuccess;
+  }
   ntp::timing_end(h, stream);
   return ok ? NTP_OK : NTP_ERR_LAUNCH;
 }
