@@ -7,13 +7,16 @@
 //   dX = a G,   dr = b G g,   dg = b G r,   v = dr gp,   dZ = rstd_z (v - mean_H(v) - hat_z mean_H(v hat_z))
 //   dgn = sum dY hat_x,  dbn = sum dY,  dgp = sum dr hat_z,  dbp = sum dr,  and dg summed likewise for a gate per channel (sums over the rows).
 //
-// One workgroup takes a row at a time; a thread holds the row's 16-byte chunks tid, tid + threads, ... in registers, so that every matrix is read and
-// written once.  What bounds both directions is HBM: 8 to 18 bytes an element against some 20 operations.
+// A row belongs to T threads (a power of two from 64 to 1024), which hold its 16-byte chunks tid, tid + T, ... in registers (V a thread), so that
+// every matrix is read and written once; a workgroup takes several rows side by side where T is small.  What bounds both directions is HBM: 8 to 18 bytes an
+// element against some 20 to 40 operations.  The backward kernel is persistent, one workgroup per compute unit with a contiguous share of the rows, because the sums over
+// the rows stay in its registers until the end; the next row's loads are in flight while this one's sums go round.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
 #include <cmath>
 #include <cstdint>
+#include <type_traits>
 
 #include "ntp_internal.h"
 
@@ -23,8 +26,10 @@ typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
 constexpr int kMaxThreads = 1024, kMaxWaves = kMaxThreads / 64;
+constexpr int kFwdThreads = 256, kBwdThreads = 512;  // of a workgroup, where a row has no more of its own
+constexpr int kMaxV = 4;
 constexpr int kVectors = 5;  // gradients that are sums over the rows: gp, bp, gate, gn, bn
-constexpr int64_t kMaxH = 32768;
+constexpr int64_t kMaxH = int64_t(kMaxThreads) * kMaxV * 8;
 
 struct NormArgs {
   const void* X;  // X (forward) or X' (backward)
@@ -39,7 +44,7 @@ struct NormArgs {
   float* sums[kVectors];  // where the sums over the rows go (NULL: not wanted)
   float* parts;           // [groups][wanted sums][H] partial sums; NULL with one group, whose sums go to `sums`
   int64_t ldx, ldz, ldxo, ldy, lddxo, lddy, ldgate, lddgate, M;
-  int32_t H, layer, gate_kind, xf32, accumulate, n_sums;
+  int32_t H, layer, gate_kind, xf32, accumulate, n_sums, t_log2;  // (1 << t_log2: threads of a row)
   float eps, a, b, inv_h;
 };
 
@@ -48,36 +53,50 @@ __device__ __forceinline__ float bf_hi(uint32_t v) { return __builtin_bit_cast(f
 __device__ __forceinline__ uint32_t bf_pack(float lo, float hi) {  // round to nearest even
   return uint32_t(__builtin_bit_cast(uint16_t, static_cast<__bf16>(lo))) | uint32_t(__builtin_bit_cast(uint16_t, static_cast<__bf16>(hi))) << 16;
 }
-__device__ __forceinline__ void load8(const uint16_t* p, float (&v)[8]) {
-  const u32x4 r = *reinterpret_cast<const u32x4*>(p);
+__device__ __forceinline__ void unpack8(u32x4 r, float (&v)[8]) {
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
     v[2 * i] = bf_lo(r[i]);
     v[2 * i + 1] = bf_hi(r[i]);
   }
 }
+__device__ __forceinline__ u32x4 raw8(const uint16_t* p) { return *reinterpret_cast<const u32x4*>(p); }
+__device__ __forceinline__ void load8(const uint16_t* p, float (&v)[8]) { unpack8(raw8(p), v); }
 __device__ __forceinline__ void store8(uint16_t* p, const float (&v)[8]) {
   u32x4 r;
 #pragma unroll
   for (int i = 0; i < 4; ++i) r[i] = bf_pack(v[2 * i], v[2 * i + 1]);
   *reinterpret_cast<u32x4*>(p) = r;
 }
-// elements `at` .. `at` + 7 of a bf16 or fp32 matrix
-__device__ __forceinline__ void load8x(const void* p, int64_t at, int f32, float (&v)[8]) {
-  if (f32) {
-    const f32x4* q = reinterpret_cast<const f32x4*>(static_cast<const float*>(p) + at);
-    const f32x4 lo = q[0], hi = q[1];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      v[i] = lo[i];
-      v[4 + i] = hi[i];
-    }
-  } else {
-    load8(static_cast<const uint16_t*>(p) + at, v);
+// Eight elements of the residual stream, bf16 or fp32, as they lie in memory.
+template <bool F32>
+struct Raw {
+  u32x4 w[F32 ? 2 : 1];
+  __device__ __forceinline__ void load(const void* p, int64_t at) {
+    const u32x4* q = reinterpret_cast<const u32x4*>(static_cast<const char*>(p) + at * (F32 ? 4 : 2));
+    w[0] = q[0];
+    if constexpr (F32) w[1] = q[1];
   }
-}
-__device__ __forceinline__ void store8x(void* p, int64_t at, int f32, const float (&v)[8]) {
-  if (f32) {
+  __device__ __forceinline__ void zero() {
+    w[0] = u32x4{0, 0, 0, 0};
+    if constexpr (F32) w[1] = w[0];
+  }
+  __device__ __forceinline__ void get(float (&v)[8]) const {
+    if constexpr (F32) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const uint32_t lo = w[0][i], hi = w[1][i];
+        v[i] = __builtin_bit_cast(float, lo);
+        v[4 + i] = __builtin_bit_cast(float, hi);
+      }
+    } else {
+      unpack8(w[0], v);
+    }
+  }
+};
+template <bool F32>
+__device__ __forceinline__ void store8x(void* p, int64_t at, const float (&v)[8]) {
+  if constexpr (F32) {
     f32x4* q = reinterpret_cast<f32x4*>(static_cast<float*>(p) + at);
     q[0] = f32x4{v[0], v[1], v[2], v[3]};
     q[1] = f32x4{v[4], v[5], v[6], v[7]};
@@ -110,30 +129,31 @@ __device__ __forceinline__ float wave_sum(float v) {
   return __builtin_bit_cast(float, r0) + __builtin_bit_cast(float, r1);
 }
 
-// Sums of N values over the workgroup, in the order of the wavefronts.  `turn` alternates between two sets of slots: a set is written again only
-// after a barrier that every thread reaches behind its reads of it.
+// Sums of N values over the threads of a row, in the order of their wavefronts.  `turn` alternates between two sets of slots: a set is written
+// again only after a barrier that every thread reaches behind its reads of it.
 template <int N>
-__device__ __forceinline__ void block_sum(float (&v)[N], float (*slots)[kMaxWaves][2], int& turn) {
-  const int waves = blockDim.x >> 6;
+__device__ __forceinline__ void row_sum(int t_log2, float (&v)[N], float (*slots)[kMaxWaves][2], int& turn) {
 #pragma unroll
   for (int n = 0; n < N; ++n) v[n] = wave_sum(v[n]);
+  const int waves = 1 << (t_log2 - 6);
   if (waves == 1) return;
+  const int wave = threadIdx.x >> 6, first = wave & ~(waves - 1);
   if ((threadIdx.x & 63) == 0) {
 #pragma unroll
-    for (int n = 0; n < N; ++n) slots[turn][threadIdx.x >> 6][n] = v[n];
+    for (int n = 0; n < N; ++n) slots[turn][wave][n] = v[n];
   }
   __syncthreads();
 #pragma unroll
   for (int n = 0; n < N; ++n) v[n] = 0.f;
   for (int w = 0; w < waves; ++w)
 #pragma unroll
-    for (int n = 0; n < N; ++n) v[n] += slots[turn][w][n];
+    for (int n = 0; n < N; ++n) v[n] += slots[turn][first + w][n];
   turn ^= 1;
 }
 
 // Mean and rstd of a row held in registers (columns behind H hold zeros).
 template <int V>
-__device__ __forceinline__ void row_stats(const NormArgs& a, const float (&t)[V][8], float& mean, float& rstd, float (*slots)[kMaxWaves][2], int& turn) {
+__device__ __forceinline__ void row_stats(const NormArgs& a, int tid, const float (&t)[V][8], float& mean, float& rstd, float (*slots)[kMaxWaves][2], int& turn) {
   float s[1];
   mean = 0.f;
   if (a.layer) {
@@ -142,170 +162,227 @@ __device__ __forceinline__ void row_stats(const NormArgs& a, const float (&t)[V]
     for (int v = 0; v < V; ++v)
 #pragma unroll
       for (int i = 0; i < 8; ++i) s[0] += t[v][i];
-    block_sum<1>(s, slots, turn);
+    row_sum<1>(a.t_log2, s, slots, turn);
     mean = s[0] * a.inv_h;
   }
   s[0] = 0.f;
 #pragma unroll
   for (int v = 0; v < V; ++v)
-    if (int(threadIdx.x + v * blockDim.x) * 8 < a.H) {
+    if ((tid + (v << a.t_log2)) * 8 < a.H) {
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
         const float d = t[v][i] - mean;
         s[0] = fmaf(d, d, s[0]);
       }
     }
-  block_sum<1>(s, slots, turn);
+  row_sum<1>(a.t_log2, s, slots, turn);
   rstd = 1.0f / sqrtf(fmaf(s[0], a.inv_h, a.eps));
 }
 
-template <int V>
+template <int V, bool XF32>
 __global__ __launch_bounds__(kMaxThreads) void block_norm_fwd_kernel(const NormArgs a) {
   __shared__ float slots[2][kMaxWaves][2];
   int turn = 0;
-  for (int64_t row = blockIdx.x; row < a.M; row += gridDim.x) {
-    float x[V][8], z[V][8];
+  const int tid = threadIdx.x & ((1 << a.t_log2) - 1);
+  const int64_t row = (int64_t(blockIdx.x) * blockDim.x + threadIdx.x) >> a.t_log2;
+  const bool on = row < a.M;
+  float x[V][8], z[V][8];
+#pragma unroll
+  for (int v = 0; v < V; ++v) {
+    const int c = (tid + (v << a.t_log2)) * 8;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) x[v][i] = z[v][i] = 0.f;
+    if (on && c < a.H) {
+      Raw<XF32> r;
+      r.load(a.X, row * a.ldx + c);
+      r.get(x[v]);
+      if (a.Z) load8(a.Z + row * a.ldz + c, z[v]);
+    }
+  }
+  if (a.Z) {
+    if (a.pg) {
+      float mean, rstd;
+      row_stats<V>(a, tid, z, mean, rstd, slots, turn);
+      if (a.Stats && on && tid == 0) {
+        a.Stats[row] = mean;
+        a.Stats[a.M + row] = rstd;
+      }
+#pragma unroll
+      for (int v = 0; v < V; ++v) {
+        const int c = (tid + (v << a.t_log2)) * 8;
+        if (c < a.H) {
+          float g[8], b[8] = {};
+          load8(a.pg + c, g);
+          if (a.pb) load8(a.pb + c, b);
+#pragma unroll
+          for (int i = 0; i < 8; ++i) z[v][i] = fmaf((z[v][i] - mean) * rstd, g[i], b[i]);
+        }
+      }
+    }
 #pragma unroll
     for (int v = 0; v < V; ++v) {
-      const int c = int(threadIdx.x + v * blockDim.x) * 8;
-#pragma unroll
-      for (int i = 0; i < 8; ++i) x[v][i] = z[v][i] = 0.f;
-      if (c < a.H) {
-        load8x(a.X, row * a.ldx + c, a.xf32, x[v]);
-        if (a.Z) load8(a.Z + row * a.ldz + c, z[v]);
-      }
-    }
-    if (a.Z) {
-      if (a.pg) {
-        float mean, rstd;
-        row_stats<V>(a, z, mean, rstd, slots, turn);
-        if (a.Stats && threadIdx.x == 0) {
-          a.Stats[row] = mean;
-          a.Stats[a.M + row] = rstd;
-        }
-#pragma unroll
-        for (int v = 0; v < V; ++v) {
-          const int c = int(threadIdx.x + v * blockDim.x) * 8;
-          if (c < a.H) {
-            float g[8], b[8] = {};
-            load8(a.pg + c, g);
-            if (a.pb) load8(a.pb + c, b);
-#pragma unroll
-            for (int i = 0; i < 8; ++i) z[v][i] = fmaf((z[v][i] - mean) * rstd, g[i], b[i]);
-          }
-        }
-      }
-#pragma unroll
-      for (int v = 0; v < V; ++v) {
-        const int c = int(threadIdx.x + v * blockDim.x) * 8;
-        if (c < a.H) {
+      const int c = (tid + (v << a.t_log2)) * 8;
+      if (on && c < a.H) {
+        if (a.gate_kind != NTP_GATE_NONE) {
           float g[8];
-          if (a.gate_kind != NTP_GATE_NONE) {
-            load8(a.gate + (a.gate_kind == NTP_GATE_TOKEN ? row * a.ldgate : 0) + c, g);
+          load8(a.gate + (a.gate_kind == NTP_GATE_TOKEN ? row * a.ldgate : 0) + c, g);
 #pragma unroll
-            for (int i = 0; i < 8; ++i) z[v][i] *= g[i];
-          }
-#pragma unroll
-          for (int i = 0; i < 8; ++i) x[v][i] = fmaf(a.a, x[v][i], a.b * z[v][i]);
-          if (a.Xout) store8x(a.Xout, row * a.ldxo + c, a.xf32, x[v]);
+          for (int i = 0; i < 8; ++i) z[v][i] *= g[i];
         }
+#pragma unroll
+        for (int i = 0; i < 8; ++i) x[v][i] = fmaf(a.a, x[v][i], a.b * z[v][i]);
+        if (a.Xout) store8x<XF32>(a.Xout, row * a.ldxo + c, x[v]);
       }
     }
-    if (a.ng) {
-      float mean, rstd;
-      row_stats<V>(a, x, mean, rstd, slots, turn);
-      if (a.Stats && threadIdx.x == 0) {
-        a.Stats[2 * a.M + row] = mean;
-        a.Stats[3 * a.M + row] = rstd;
-      }
+  }
+  if (a.ng) {
+    float mean, rstd;
+    row_stats<V>(a, tid, x, mean, rstd, slots, turn);
+    if (a.Stats && on && tid == 0) {
+      a.Stats[2 * a.M + row] = mean;
+      a.Stats[3 * a.M + row] = rstd;
+    }
 #pragma unroll
-      for (int v = 0; v < V; ++v) {
-        const int c = int(threadIdx.x + v * blockDim.x) * 8;
-        if (c < a.H) {
-          float g[8], b[8] = {}, y[8];
-          load8(a.ng + c, g);
-          if (a.nb) load8(a.nb + c, b);
+    for (int v = 0; v < V; ++v) {
+      const int c = (tid + (v << a.t_log2)) * 8;
+      if (on && c < a.H) {
+        float g[8], b[8] = {}, y[8];
+        load8(a.ng + c, g);
+        if (a.nb) load8(a.nb + c, b);
 #pragma unroll
-          for (int i = 0; i < 8; ++i) y[i] = fmaf((x[v][i] - mean) * rstd, g[i], b[i]);
-          store8(a.Y + row * a.ldy + c, y);
-        }
+        for (int i = 0; i < 8; ++i) y[i] = fmaf((x[v][i] - mean) * rstd, g[i], b[i]);
+        store8(a.Y + row * a.ldy + c, y);
       }
     }
   }
 }
 
-// Rows row0 .. row1 - 1 of a group; the sums over them stay in registers until the end.
-template <int V>
-__global__ __launch_bounds__(kMaxThreads) void block_norm_bwd_kernel(const NormArgs a) {
+// Which sums over the rows a backward kernel holds, by kind: 0 nothing behind the block (no norm, no gate: Z is not read), 1 anything without
+// betas, 2 anything.  Numbers into NormArgs::sums.
+constexpr int kSums[3] = {2, 3, 5};
+__device__ constexpr int kSumOf[3][kVectors] = {{3, 4, -1, -1, -1}, {0, 2, 3, -1, -1}, {0, 1, 2, 3, 4}};
+
+// Workgroup = a contiguous share of the rows, blockDim.x / T at a time.
+template <int V, bool XF32, int KIND>
+__device__ __forceinline__ void bwd_body(const NormArgs& a) {
+  constexpr bool BRANCH = KIND > 0, BIAS = KIND == 2 || KIND == 0;
+  constexpr int PG = 0, PB = 1, GT = KIND == 1 ? 1 : 2, NG = KIND == 0 ? 0 : KIND == 1 ? 2 : 3, NB = KIND == 0 ? 1 : 4;
   __shared__ float slots[2][kMaxWaves][2];
+  __shared__ float rows_lds[kBwdThreads][8];
   int turn = 0;
-  float acc[kVectors][V][8] = {};
+  const int T = 1 << a.t_log2, tid = threadIdx.x & (T - 1), lane_row = threadIdx.x >> a.t_log2, n_rows = blockDim.x >> a.t_log2;
+  float acc[kSums[KIND]][V][8] = {};
   const int64_t row0 = a.M * blockIdx.x / gridDim.x, row1 = a.M * (blockIdx.x + 1) / gridDim.x;
-  for (int64_t row = row0; row < row1; ++row) {
-    float G[V][8], x[V][8], z[V][8];
-    float s[2] = {0.f, 0.f};
-    const float mz = a.pg ? a.Stats[row] : 0.f, rz = a.pg ? a.Stats[a.M + row] : 1.f;
-    const float mx = a.ng ? a.Stats[2 * a.M + row] : 0.f, rx = a.ng ? a.Stats[3 * a.M + row] : 0.f;
+  Raw<XF32> rx[V], rd[V];
+  u32x4 ry[V];
+  float st[4] = {0.f, 1.f, 0.f, 1.f}, nst[4] = {0.f, 1.f, 0.f, 1.f};
+  auto load_row = [&](int64_t row) {
+    if (row >= row1) return;
+    if (BRANCH && a.pg) nst[0] = a.Stats[row], nst[1] = a.Stats[a.M + row];
+    if (a.ng) nst[2] = a.Stats[2 * a.M + row], nst[3] = a.Stats[3 * a.M + row];
 #pragma unroll
     for (int v = 0; v < V; ++v) {
-      const int c = int(threadIdx.x + v * blockDim.x) * 8;
-#pragma unroll
-      for (int i = 0; i < 8; ++i) G[v][i] = x[v][i] = z[v][i] = 0.f;
+      const int c = (tid + (v << a.t_log2)) * 8;
       if (c < a.H) {
-        if (a.dXout) load8x(a.dXout, row * a.lddxo + c, a.xf32, G[v]);
-        if (a.Z) load8(a.Z + row * a.ldz + c, z[v]);
+        if (a.dXout) rd[v].load(a.dXout, row * a.lddxo + c);
         if (a.ng) {
-          float dy[8], g[8];
-          load8(a.dY + row * a.lddy + c, dy);
-          load8x(a.X, row * a.ldx + c, a.xf32, x[v]);
-          load8(a.ng + c, g);
-#pragma unroll
-          for (int i = 0; i < 8; ++i) {
-            x[v][i] = (x[v][i] - mx) * rx;  // hat_x
-            acc[3][v][i] = fmaf(dy[i], x[v][i], acc[3][v][i]);
-            acc[4][v][i] += dy[i];
-            const float u = dy[i] * g[i];
-            s[0] += u;
-            s[1] = fmaf(u, x[v][i], s[1]);
-            G[v][i] = fmaf(u, rx, G[v][i]);
-          }
+          ry[v] = raw8(a.dY + row * a.lddy + c);
+          rx[v].load(a.X, row * a.ldx + c);
         }
       }
     }
+  };
+#pragma unroll
+  for (int v = 0; v < V; ++v) {
+    rx[v].zero();
+    rd[v].zero();
+    ry[v] = u32x4{0, 0, 0, 0};
+  }
+  load_row(row0 + lane_row);
+  for (int64_t base = row0; base < row1; base += n_rows) {
+    const int64_t row = base + lane_row;
+    const bool on = row < row1;
+    float G[V][8], s[2] = {0.f, 0.f};
+    u32x4 rz[V], rg[V];
+    Raw<XF32> hx[V];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) st[i] = nst[i];
+    if constexpr (BRANCH) {
+#pragma unroll
+      for (int v = 0; v < V; ++v) {
+        const int c = (tid + (v << a.t_log2)) * 8;
+        if (on && c < a.H) {
+          rz[v] = raw8(a.Z + row * a.ldz + c);
+          if (a.gate_kind != NTP_GATE_NONE) rg[v] = raw8(a.gate + (a.gate_kind == NTP_GATE_TOKEN ? row * a.ldgate : 0) + c);
+        }
+      }
+    }
+#pragma unroll
+    for (int v = 0; v < V; ++v) {
+      const int c = (tid + (v << a.t_log2)) * 8;
+      rd[v].get(G[v]);
+      hx[v] = rx[v];
+      if (a.ng && on && c < a.H) {
+        float dy[8], x[8], g[8];
+        unpack8(ry[v], dy);
+        rx[v].get(x);
+        load8(a.ng + c, g);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          const float h = (x[i] - st[2]) * st[3];  // hat_x
+          acc[NG][v][i] = fmaf(dy[i], h, acc[NG][v][i]);
+          if constexpr (BIAS) acc[NB][v][i] += dy[i];
+          const float u = dy[i] * g[i];
+          s[0] += u;
+          s[1] = fmaf(u, h, s[1]);
+          G[v][i] = fmaf(u, st[3], G[v][i]);
+        }
+      }
+    }
+    load_row(row + n_rows);
     if (a.ng) {
-      block_sum<2>(s, slots, turn);
-      const float m0 = a.layer ? s[0] * a.inv_h * rx : 0.f, m1 = s[1] * a.inv_h * rx;
+      row_sum<2>(a.t_log2, s, slots, turn);
+      const float m0 = a.layer ? s[0] * a.inv_h * st[3] : 0.f, m1 = s[1] * a.inv_h * st[3];
 #pragma unroll
-      for (int v = 0; v < V; ++v)
+      for (int v = 0; v < V; ++v) {
+        float x[8];
+        hx[v].get(x);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) G[v][i] -= fmaf(x[v][i], m1, m0);
+        for (int i = 0; i < 8; ++i) G[v][i] -= fmaf((x[i] - st[2]) * st[3], m1, m0);
+      }
     }
     s[0] = s[1] = 0.f;
 #pragma unroll
     for (int v = 0; v < V; ++v) {
-      const int c = int(threadIdx.x + v * blockDim.x) * 8;
-      if (c < a.H) {
+      const int c = (tid + (v << a.t_log2)) * 8;
+      if (on && c < a.H) {
         float o[8];
 #pragma unroll
         for (int i = 0; i < 8; ++i) o[i] = a.a * G[v][i];
-        store8x(a.Xout, row * a.ldxo + c, a.xf32, o);
-        if (a.Y) {
-          float g[8], p[8], q[8] = {};
+        store8x<XF32>(a.Xout, row * a.ldxo + c, o);
+        if (!BRANCH && a.Y) {
+#pragma unroll
+          for (int i = 0; i < 8; ++i) o[i] = a.b * G[v][i];
+          store8(a.Y + row * a.ldy + c, o);
+        }
+        if constexpr (BRANCH) {
+          float z[8], p[8], q[8] = {};
+          unpack8(rz[v], z);
 #pragma unroll
           for (int i = 0; i < 8; ++i) {
             G[v][i] *= a.b;
             p[i] = 1.f;
-            z[v][i] = (z[v][i] - mz) * rz;  // hat_z, or Z itself
+            z[i] = (z[i] - st[0]) * st[1];  // hat_z, or Z itself
           }
           if (a.pg) load8(a.pg + c, p);
-          if (a.pb) load8(a.pb + c, q);
+          if (KIND == 2 && a.pb) load8(a.pb + c, q);
           if (a.gate_kind != NTP_GATE_NONE) {
-            load8(a.gate + (a.gate_kind == NTP_GATE_TOKEN ? row * a.ldgate : 0) + c, g);
+            float g[8];
+            unpack8(rg[v], g);
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
-              const float dg = G[v][i] * fmaf(z[v][i], p[i], q[i]);
-              acc[2][v][i] += dg;
-              o[i] = dg;
+              o[i] = G[v][i] * fmaf(z[i], p[i], q[i]);
+              acc[GT][v][i] += o[i];
               G[v][i] *= g[i];  // dr
             }
             if (a.dgate_rows) store8(a.dgate_rows + row * a.lddgate + c, o);
@@ -313,47 +390,61 @@ __global__ __launch_bounds__(kMaxThreads) void block_norm_bwd_kernel(const NormA
           if (a.pg) {
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
-              acc[0][v][i] = fmaf(G[v][i], z[v][i], acc[0][v][i]);
-              acc[1][v][i] += G[v][i];
+              acc[PG][v][i] = fmaf(G[v][i], z[i], acc[PG][v][i]);
+              if constexpr (KIND == 2) acc[PB][v][i] += G[v][i];
               G[v][i] *= p[i];  // v
               s[0] += G[v][i];
-              s[1] = fmaf(G[v][i], z[v][i], s[1]);
+              s[1] = fmaf(G[v][i], z[i], s[1]);
             }
           }
         }
       }
     }
-    if (a.Y) {
+    if constexpr (BRANCH) {
       float m0 = 0.f, m1 = 0.f;
       if (a.pg) {
-        block_sum<2>(s, slots, turn);
+        row_sum<2>(a.t_log2, s, slots, turn);
         m0 = a.layer ? s[0] * a.inv_h : 0.f;
         m1 = s[1] * a.inv_h;
       }
 #pragma unroll
       for (int v = 0; v < V; ++v) {
-        const int c = int(threadIdx.x + v * blockDim.x) * 8;
-        if (c < a.H) {
-          float o[8];
+        const int c = (tid + (v << a.t_log2)) * 8;
+        if (on && c < a.H) {
+          float z[8], o[8];
+          unpack8(rz[v], z);
 #pragma unroll
-          for (int i = 0; i < 8; ++i) o[i] = (G[v][i] - fmaf(z[v][i], m1, m0)) * rz;
+          for (int i = 0; i < 8; ++i) o[i] = (G[v][i] - fmaf((z[i] - st[0]) * st[1], m1, m0)) * st[1];
           store8(a.Y + row * a.ldy + c, o);
         }
       }
     }
   }
+  // the rows side by side are added up in order, chunk by chunk; then the workgroup's sums go out
   int n = 0;
 #pragma unroll
-  for (int k = 0; k < kVectors; ++k) {
-    if (!a.sums[k]) continue;
-    float* dst = a.parts ? a.parts + (int64_t(blockIdx.x) * a.n_sums + n) * a.H : a.sums[k];
+  for (int k = 0; k < kSums[KIND]; ++k) {
+    float* const out = a.sums[kSumOf[KIND][k]];
+    if (!out) continue;
+    float* const dst = a.parts ? a.parts + (int64_t(blockIdx.x) * a.n_sums + n) * a.H : out;
     ++n;
 #pragma unroll
     for (int v = 0; v < V; ++v) {
-      const int c = int(threadIdx.x + v * blockDim.x) * 8;
-      if (c < a.H) {
+      const int c = (tid + (v << a.t_log2)) * 8;
+      f32x4 lo = {acc[k][v][0], acc[k][v][1], acc[k][v][2], acc[k][v][3]}, hi = {acc[k][v][4], acc[k][v][5], acc[k][v][6], acc[k][v][7]};
+      if (n_rows > 1) {
+        __syncthreads();
+        *reinterpret_cast<f32x4*>(&rows_lds[threadIdx.x % kBwdThreads][0]) = lo;
+        *reinterpret_cast<f32x4*>(&rows_lds[threadIdx.x % kBwdThreads][4]) = hi;
+        __syncthreads();
+        if (lane_row == 0)
+          for (int r = 1; r < n_rows; ++r) {
+            lo += *reinterpret_cast<const f32x4*>(&rows_lds[r * T + tid][0]);
+            hi += *reinterpret_cast<const f32x4*>(&rows_lds[r * T + tid][4]);
+          }
+      }
+      if (lane_row == 0 && c < a.H) {
         f32x4* q = reinterpret_cast<f32x4*>(dst + c);
-        f32x4 lo = {acc[k][v][0], acc[k][v][1], acc[k][v][2], acc[k][v][3]}, hi = {acc[k][v][4], acc[k][v][5], acc[k][v][6], acc[k][v][7]};
         if (!a.parts && a.accumulate) {
           lo += q[0];
           hi += q[1];
@@ -365,17 +456,35 @@ __global__ __launch_bounds__(kMaxThreads) void block_norm_bwd_kernel(const NormA
   }
 }
 
-// The groups' partial sums added up in order: thread = one column of one vector.
+template <int V, bool XF32, int KIND>
+__global__ __launch_bounds__(kBwdThreads) void block_norm_bwd_kernel(const NormArgs a) {
+  bwd_body<V, XF32, KIND>(a);
+}
+// rows of more than kBwdThreads * kMaxV chunks
+template <int V, bool XF32, int KIND>
+__global__ __launch_bounds__(kMaxThreads) void block_norm_bwd_long_kernel(const NormArgs a) {
+  bwd_body<V, XF32, KIND>(a);
+}
+
+// The groups' partial sums added up in a fixed order: 16 lanes hold 64 columns, 16 threads of a column take every 16th group; then these in order.
 __global__ __launch_bounds__(256) void block_norm_sum_kernel(const NormArgs a, int groups) {
-  const int64_t at = int64_t(blockIdx.x) * 256 + threadIdx.x;
-  if (at >= int64_t(a.n_sums) * a.H) return;
+  __shared__ f32x4 lds[16][16];
+  const int lane = threadIdx.x & 15, part = threadIdx.x >> 4;
+  const int64_t width = int64_t(a.n_sums) * a.H, at = (int64_t(blockIdx.x) * 16 + lane) * 4;
+  f32x4 s = {0.f, 0.f, 0.f, 0.f};
+  if (at < width)
+#pragma unroll 4
+    for (int g = part; g < groups; g += 16) s += *reinterpret_cast<const f32x4*>(a.parts + int64_t(g) * width + at);
+  lds[part][lane] = s;
+  __syncthreads();
+  if (part > 0 || at >= width) return;
+  for (int i = 1; i < 16; ++i) s += lds[i][lane];
   const int n = int(at / a.H), c = int(at % a.H);
-  float s = 0.f;
-  for (int g = 0; g < groups; ++g) s += a.parts[(int64_t(g) * a.n_sums + n) * a.H + c];
   int k = 0;
   for (int left = n; k < kVectors; ++k)
     if (a.sums[k] && left-- == 0) break;
-  a.sums[k][c] = a.accumulate ? a.sums[k][c] + s : s;
+  f32x4* q = reinterpret_cast<f32x4*>(a.sums[k] + c);
+  *q = a.accumulate ? *q + s : s;
 }
 
 int check_norm_shape(const ntp_block_norm_shape_t* s) {
@@ -397,14 +506,28 @@ int check_weights(const ntp_block_norm_shape_t* s, const ntp_block_norm_weights_
 
 bool off16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15) != 0; }
 
-// Rows are one workgroup's: at most two chunks of 8 columns a thread, four beyond 16384 columns.
-int norm_threads(int64_t H) {
-  const int64_t chunks = H / 8, v = chunks > 2 * kMaxThreads ? 4 : 2;
-  return int(((chunks + v - 1) / v + 63) / 64 * 64);
+// Threads of a row (their logarithm): as few as hold it with kMaxV chunks each.
+int norm_t_log2(int64_t H) {
+  int n = 6;
+  while ((int64_t(8 * kMaxV) << n) < H) ++n;
+  return n;
 }
+int norm_chunks(int64_t H, int t_log2) { return int((H / 8 + (int64_t(1) << t_log2) - 1) >> t_log2); }
 
 // Workgroups that share out the rows of a backward call, each with partial sums of its own: one per compute unit.
-int64_t norm_groups(const ntp_handle* h, const ntp_block_norm_shape_t* s) { return std::max<int64_t>(1, std::min<int64_t>(s->M, h->compute_units)); }
+int64_t norm_groups(const ntp_handle* h, const ntp_block_norm_shape_t* s) {
+  const int64_t at_once = std::max<int64_t>(1, kBwdThreads >> norm_t_log2(s->H));
+  return std::max<int64_t>(1, std::min<int64_t>((s->M + at_once - 1) / at_once, h->compute_units));
+}
+
+// f with the number of chunks a thread holds as a constant
+template <typename F>
+void by_chunks(int v, F&& f) {
+  if (v <= 1) f(std::integral_constant<int, 1>{});
+  else if (v == 2) f(std::integral_constant<int, 2>{});
+  else if (v == 3) f(std::integral_constant<int, 3>{});
+  else f(std::integral_constant<int, 4>{});
+}
 
 }  // namespace
 
@@ -442,9 +565,17 @@ extern "C" int ntp_block_norm_fwd(ntp_handle_t* h, const ntp_block_norm_shape_t*
     const double n = double(s->M) * double(s->H), rt = a.xf32 ? 4 : 2;
     ntp::timing_begin(h, stream, "block_norm_fwd", 0.0, n * (rt + (Z ? 2 : 0) + (Xout ? rt : 0) + (Y ? 2 : 0) + (s->gate == NTP_GATE_TOKEN ? 2 : 0)));
   }
-  const dim3 grid(uint32_t(s->M)), block(uint32_t(norm_threads(s->H)));
-  if (s->H > 2 * 8 * kMaxThreads) hipLaunchKernelGGL(block_norm_fwd_kernel<4>, grid, block, 0, hs, a);
-  else hipLaunchKernelGGL(block_norm_fwd_kernel<2>, grid, block, 0, hs, a);
+  // few rows: more threads each, down to one chunk a thread, while the compute units have room for them
+  int t_log2 = norm_t_log2(s->H);
+  while (norm_chunks(s->H, t_log2) > 1 && (2 << t_log2) <= kMaxThreads && (s->M << t_log2) * 2 <= int64_t(h->compute_units) * kMaxThreads) ++t_log2;
+  a.t_log2 = t_log2;
+  const int threads = std::max(kFwdThreads, 1 << t_log2), rows = threads >> t_log2;
+  const dim3 grid(uint32_t((s->M + rows - 1) / rows)), block{uint32_t(threads)};
+  auto launch = [&](auto v) {
+    if (a.xf32) hipLaunchKernelGGL((block_norm_fwd_kernel<decltype(v)::value, true>), grid, block, 0, hs, a);
+    else hipLaunchKernelGGL((block_norm_fwd_kernel<decltype(v)::value, false>), grid, block, 0, hs, a);
+  };
+  by_chunks(norm_chunks(s->H, t_log2), launch);
   const bool ok = hipGetLastError() == hipSuccess;
   ntp::timing_end(h, stream);
   return ok ? NTP_OK : NTP_ERR_LAUNCH;
@@ -500,12 +631,29 @@ extern "C" int ntp_block_norm_bwd(ntp_handle_t* h, const ntp_block_norm_shape_t*
     ntp::timing_begin(h, stream, "block_norm_bwd", 0.0,
                       n * (rt + (dXout ? rt : 0) + (pre ? 2 + rt : 0) + (a.Z ? 2 : 0) + (dZ ? 2 : 0) + (token ? 2 : 0) + (a.dgate_rows ? 2 : 0)));
   }
-  const dim3 grid{uint32_t(groups)}, block(uint32_t(norm_threads(s->H)));
-  if (s->H > 2 * 8 * kMaxThreads) hipLaunchKernelGGL(block_norm_bwd_kernel<4>, grid, block, 0, hs, a);
-  else hipLaunchKernelGGL(block_norm_bwd_kernel<2>, grid, block, 0, hs, a);
+  a.t_log2 = norm_t_log2(s->H);
+  const bool bias = w->post_beta || w->pre_beta;
+  const int threads = std::max(kBwdThreads, 1 << a.t_log2);
+  const dim3 grid{uint32_t(groups)}, block{uint32_t(threads)};
+  auto launch = [&](auto v, auto f32, auto kind) {
+    constexpr int V = decltype(v)::value, KIND = decltype(kind)::value;
+    constexpr bool F32 = decltype(f32)::value;
+    if (threads > kBwdThreads) hipLaunchKernelGGL((block_norm_bwd_long_kernel<kMaxV, F32, KIND>), grid, block, 0, hs, a);
+    else hipLaunchKernelGGL((block_norm_bwd_kernel<V, F32, KIND>), grid, block, 0, hs, a);
+  };
+  using std::integral_constant;
+  by_chunks(norm_chunks(s->H, a.t_log2), [&](auto v) {
+    auto by_kind = [&](auto f32) {
+      if (!reads_z) launch(v, f32, integral_constant<int, 0>{});
+      else if (!bias) launch(v, f32, integral_constant<int, 1>{});
+      else launch(v, f32, integral_constant<int, 2>{});
+    };
+    if (a.xf32) by_kind(std::true_type{});
+    else by_kind(std::false_type{});
+  });
   bool ok = hipGetLastError() == hipSuccess;
   if (ok && a.parts) {
-    hipLaunchKernelGGL(block_norm_sum_kernel, dim3(uint32_t((int64_t(a.n_sums) * s->H + 255) / 256)), dim3(256), 0, hs, a, int(groups));
+    hipLaunchKernelGGL(block_norm_sum_kernel, dim3(uint32_t((int64_t(a.n_sums) * s->H + 63) / 64)), dim3(256), 0, hs, a, int(groups));
     ok = hipGetLastError() == hipSuccess;
   }
   ntp::timing_end(h, stream);
