@@ -262,71 +262,112 @@ __global__ __launch_bounds__(kMaxThreads) void block_norm_fwd_kernel(const NormA
 constexpr int kSums[3] = {2, 3, 5};
 __device__ constexpr int kSumOf[3][kVectors] = {{3, 4, -1, -1, -1}, {0, 2, 3, -1, -1}, {0, 1, 2, 3, 4}};
 
-// Workgroup = a contiguous share of the rows, blockDim.x / T at a time.
-template <int V, bool XF32, int KIND>
+// A row of a matrix as a buffer view: what lies behind its H columns reads as zeros and is not written, so that the loops below have no branches
+// (a wait for loads behind which a branch may or may not have issued stores would wait for these too).
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t row_view(const void* base, int64_t at, int elem, int columns) {
+  return __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(static_cast<const char*>(base) + at * elem), 0, columns * elem, 0x00020000);
+}
+__device__ __forceinline__ u32x4 load_16(__amdgpu_buffer_rsrc_t rs, uint32_t off) { return __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(rs, off, 0, 0)); }
+__device__ __forceinline__ void store_16(__amdgpu_buffer_rsrc_t rs, uint32_t off, u32x4 v) { __builtin_amdgcn_raw_buffer_store_b128(v, rs, off, 0, 0); }
+__device__ __forceinline__ u32x4 pack8(const float (&v)[8]) {
+  u32x4 r;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) r[i] = bf_pack(v[2 * i], v[2 * i + 1]);
+  return r;
+}
+template <bool F32>
+__device__ __forceinline__ void load_raw(Raw<F32>& r, __amdgpu_buffer_rsrc_t rs, int c) {
+  r.w[0] = load_16(rs, uint32_t(c) * (F32 ? 4 : 2));
+  if constexpr (F32) r.w[1] = load_16(rs, uint32_t(c) * 4 + 16);
+}
+template <bool F32>
+__device__ __forceinline__ void store_raw(__amdgpu_buffer_rsrc_t rs, int c, const float (&v)[8]) {
+  if constexpr (F32) {
+    u32x4 lo, hi;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      lo[i] = __builtin_bit_cast(uint32_t, v[i]);
+      hi[i] = __builtin_bit_cast(uint32_t, v[4 + i]);
+    }
+    store_16(rs, uint32_t(c) * 4, lo);
+    store_16(rs, uint32_t(c) * 4 + 16, hi);
+  } else {
+    store_16(rs, uint32_t(c) * 2, pack8(v));
+  }
+}
+
+// Workgroup = a contiguous share of the rows, blockDim.x / T at a time.  The vectors (gn, gp, the gate per channel, bp) lie in the LDS, for rows of at most
+// kBwdThreads * kMaxV chunks: loads of them from memory would be waited for together with the next row's, which are issued before.
+template <int V, bool XF32, int KIND, bool LONG>
 __device__ __forceinline__ void bwd_body(const NormArgs& a) {
   constexpr bool BRANCH = KIND > 0, BIAS = KIND == 2 || KIND == 0;
   constexpr int PG = 0, PB = 1, GT = KIND == 1 ? 1 : 2, NG = KIND == 0 ? 0 : KIND == 1 ? 2 : 3, NB = KIND == 0 ? 1 : 4;
+  constexpr int XB = XF32 ? 4 : 2;
   __shared__ float slots[2][kMaxWaves][2];
-  __shared__ float rows_lds[kBwdThreads][8];
+  __shared__ float rows_lds[LONG ? 1 : kBwdThreads][8];
+  extern __shared__ __attribute__((aligned(16))) u32x4 vectors[];  // [4][V * T] chunks: gn, gp, gate, bp
   int turn = 0;
-  const int T = 1 << a.t_log2, tid = threadIdx.x & (T - 1), lane_row = threadIdx.x >> a.t_log2, n_rows = blockDim.x >> a.t_log2;
+  const int T = 1 << a.t_log2, tid = threadIdx.x & (T - 1), n_rows = blockDim.x >> a.t_log2;
+  const int lane_row = __builtin_amdgcn_readfirstlane(threadIdx.x >> a.t_log2);  // (T is a multiple of the wavefront)
+  const uint16_t* const vec_ptr[4] = {a.ng, a.pg, a.gate_kind == NTP_GATE_CHANNEL ? a.gate : nullptr, a.pb};
+  auto vec = [&](int which, int v, float (&o)[8]) {
+    if constexpr (LONG) unpack8(load_16(row_view(vec_ptr[which], 0, 2, a.H), uint32_t(tid + (v << a.t_log2)) * 16), o);
+    else unpack8(vectors[(which * V + v) * T + tid], o);
+  };
+  if constexpr (!LONG) {
+    for (int which = 0; which < (KIND == 0 ? 1 : KIND == 1 ? 3 : 4); ++which)
+      if (vec_ptr[which])
+        for (int c = threadIdx.x; c < V * T; c += blockDim.x) vectors[which * V * T + c] = load_16(row_view(vec_ptr[which], 0, 2, a.H), uint32_t(c) * 16);
+    __syncthreads();
+  }
   float acc[kSums[KIND]][V][8] = {};
   const int64_t row0 = a.M * blockIdx.x / gridDim.x, row1 = a.M * (blockIdx.x + 1) / gridDim.x;
   Raw<XF32> rx[V], rd[V];
   u32x4 ry[V];
   float st[4] = {0.f, 1.f, 0.f, 1.f}, nst[4] = {0.f, 1.f, 0.f, 1.f};
   auto load_row = [&](int64_t row) {
-    if (row >= row1) return;
+    const bool there = row < row1;
+    const int width = there ? a.H : 0;
+    row = there ? row : 0;
     if (BRANCH && a.pg) nst[0] = a.Stats[row], nst[1] = a.Stats[a.M + row];
     if (a.ng) nst[2] = a.Stats[2 * a.M + row], nst[3] = a.Stats[3 * a.M + row];
+    const __amdgpu_buffer_rsrc_t vd = row_view(a.dXout, row * a.lddxo, XB, a.dXout ? width : 0), vy = row_view(a.dY, row * a.lddy, 2, a.ng ? width : 0),
+                                 vx = row_view(a.X, row * a.ldx, XB, a.ng ? width : 0);
 #pragma unroll
     for (int v = 0; v < V; ++v) {
       const int c = (tid + (v << a.t_log2)) * 8;
-      if (c < a.H) {
-        if (a.dXout) rd[v].load(a.dXout, row * a.lddxo + c);
-        if (a.ng) {
-          ry[v] = raw8(a.dY + row * a.lddy + c);
-          rx[v].load(a.X, row * a.ldx + c);
-        }
-      }
+      load_raw<XF32>(rd[v], vd, c);
+      ry[v] = load_16(vy, uint32_t(c) * 2);
+      load_raw<XF32>(rx[v], vx, c);
     }
   };
-#pragma unroll
-  for (int v = 0; v < V; ++v) {
-    rx[v].zero();
-    rd[v].zero();
-    ry[v] = u32x4{0, 0, 0, 0};
-  }
-  load_row(row0 + lane_row);
+  if (row0 < row1) load_row(row0 + lane_row);  // (without rows nothing may be read)
   for (int64_t base = row0; base < row1; base += n_rows) {
     const int64_t row = base + lane_row;
-    const bool on = row < row1;
+    const int width = row < row1 ? a.H : 0;
     float G[V][8], s[2] = {0.f, 0.f};
     u32x4 rz[V], rg[V];
     Raw<XF32> hx[V];
 #pragma unroll
     for (int i = 0; i < 4; ++i) st[i] = nst[i];
     if constexpr (BRANCH) {
+      const __amdgpu_buffer_rsrc_t vz = row_view(a.Z, row * a.ldz, 2, width), vg = row_view(a.gate, row * a.ldgate, 2, a.gate_kind == NTP_GATE_TOKEN ? width : 0);
 #pragma unroll
       for (int v = 0; v < V; ++v) {
-        const int c = (tid + (v << a.t_log2)) * 8;
-        if (on && c < a.H) {
-          rz[v] = raw8(a.Z + row * a.ldz + c);
-          if (a.gate_kind != NTP_GATE_NONE) rg[v] = raw8(a.gate + (a.gate_kind == NTP_GATE_TOKEN ? row * a.ldgate : 0) + c);
-        }
+        const uint32_t off = uint32_t(tid + (v << a.t_log2)) * 16;
+        rz[v] = load_16(vz, off);
+        if (a.gate_kind == NTP_GATE_TOKEN) rg[v] = load_16(vg, off);
       }
     }
 #pragma unroll
     for (int v = 0; v < V; ++v) {
-      const int c = (tid + (v << a.t_log2)) * 8;
       rd[v].get(G[v]);
       hx[v] = rx[v];
-      if (a.ng && on && c < a.H) {
+      if (a.ng) {
         float dy[8], x[8], g[8];
         unpack8(ry[v], dy);
         rx[v].get(x);
-        load8(a.ng + c, g);
+        vec(0, v, g);
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
           const float h = (x[i] - st[2]) * st[3];  // hat_x
@@ -352,50 +393,51 @@ __device__ __forceinline__ void bwd_body(const NormArgs& a) {
       }
     }
     s[0] = s[1] = 0.f;
+    const __amdgpu_buffer_rsrc_t vdx = row_view(a.Xout, row * a.ldxo, XB, width), vdz = row_view(a.Y, row * a.ldy, 2, a.Y ? width : 0),
+                                 vdg = row_view(a.dgate_rows, row * a.lddgate, 2, a.dgate_rows ? width : 0);
 #pragma unroll
     for (int v = 0; v < V; ++v) {
       const int c = (tid + (v << a.t_log2)) * 8;
-      if (on && c < a.H) {
-        float o[8];
+      float o[8];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) o[i] = a.a * G[v][i];
-        store8x<XF32>(a.Xout, row * a.ldxo + c, o);
-        if (!BRANCH && a.Y) {
+      for (int i = 0; i < 8; ++i) o[i] = a.a * G[v][i];
+      store_raw<XF32>(vdx, c, o);
+      if (!BRANCH && a.Y) {
 #pragma unroll
-          for (int i = 0; i < 8; ++i) o[i] = a.b * G[v][i];
-          store8(a.Y + row * a.ldy + c, o);
+        for (int i = 0; i < 8; ++i) o[i] = a.b * G[v][i];
+        store_16(vdz, uint32_t(c) * 2, pack8(o));
+      }
+      if constexpr (BRANCH) {
+        float z[8], p[8], q[8] = {};
+        unpack8(rz[v], z);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          G[v][i] *= a.b;
+          p[i] = 1.f;
+          z[i] = (z[i] - st[0]) * st[1];  // hat_z, or Z itself
         }
-        if constexpr (BRANCH) {
-          float z[8], p[8], q[8] = {};
-          unpack8(rz[v], z);
+        if (a.pg) vec(1, v, p);
+        if (KIND == 2 && a.pb) vec(3, v, q);
+        if (a.gate_kind != NTP_GATE_NONE) {
+          float g[8];
+          if (a.gate_kind == NTP_GATE_TOKEN) unpack8(rg[v], g);
+          else vec(2, v, g);
 #pragma unroll
           for (int i = 0; i < 8; ++i) {
-            G[v][i] *= a.b;
-            p[i] = 1.f;
-            z[i] = (z[i] - st[0]) * st[1];  // hat_z, or Z itself
+            o[i] = G[v][i] * fmaf(z[i], p[i], q[i]);
+            acc[GT][v][i] += o[i];
+            G[v][i] *= g[i];  // dr
           }
-          if (a.pg) load8(a.pg + c, p);
-          if (KIND == 2 && a.pb) load8(a.pb + c, q);
-          if (a.gate_kind != NTP_GATE_NONE) {
-            float g[8];
-            unpack8(rg[v], g);
+          if (a.dgate_rows) store_16(vdg, uint32_t(c) * 2, pack8(o));
+        }
+        if (a.pg) {
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-              o[i] = G[v][i] * fmaf(z[i], p[i], q[i]);
-              acc[GT][v][i] += o[i];
-              G[v][i] *= g[i];  // dr
-            }
-            if (a.dgate_rows) store8(a.dgate_rows + row * a.lddgate + c, o);
-          }
-          if (a.pg) {
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
-              acc[PG][v][i] = fmaf(G[v][i], z[i], acc[PG][v][i]);
-              if constexpr (KIND == 2) acc[PB][v][i] += G[v][i];
-              G[v][i] *= p[i];  // v
-              s[0] += G[v][i];
-              s[1] = fmaf(G[v][i], z[i], s[1]);
-            }
+          for (int i = 0; i < 8; ++i) {
+            acc[PG][v][i] = fmaf(G[v][i], z[i], acc[PG][v][i]);
+            if constexpr (KIND == 2) acc[PB][v][i] += G[v][i];
+            G[v][i] *= p[i];  // v
+            s[0] += G[v][i];
+            s[1] = fmaf(G[v][i], z[i], s[1]);
           }
         }
       }
@@ -409,14 +451,11 @@ __device__ __forceinline__ void bwd_body(const NormArgs& a) {
       }
 #pragma unroll
       for (int v = 0; v < V; ++v) {
-        const int c = (tid + (v << a.t_log2)) * 8;
-        if (on && c < a.H) {
-          float z[8], o[8];
-          unpack8(rz[v], z);
+        float z[8], o[8];
+        unpack8(rz[v], z);
 #pragma unroll
-          for (int i = 0; i < 8; ++i) o[i] = (G[v][i] - fmaf((z[i] - st[0]) * st[1], m1, m0)) * st[1];
-          store8(a.Y + row * a.ldy + c, o);
-        }
+        for (int i = 0; i < 8; ++i) o[i] = (G[v][i] - fmaf((z[i] - st[0]) * st[1], m1, m0)) * st[1];
+        store_16(vdz, uint32_t(tid + (v << a.t_log2)) * 16, pack8(o));
       }
     }
   }
@@ -432,10 +471,10 @@ __device__ __forceinline__ void bwd_body(const NormArgs& a) {
     for (int v = 0; v < V; ++v) {
       const int c = (tid + (v << a.t_log2)) * 8;
       f32x4 lo = {acc[k][v][0], acc[k][v][1], acc[k][v][2], acc[k][v][3]}, hi = {acc[k][v][4], acc[k][v][5], acc[k][v][6], acc[k][v][7]};
-      if (n_rows > 1) {
+      if (!LONG && n_rows > 1) {
         __syncthreads();
-        *reinterpret_cast<f32x4*>(&rows_lds[threadIdx.x % kBwdThreads][0]) = lo;
-        *reinterpret_cast<f32x4*>(&rows_lds[threadIdx.x % kBwdThreads][4]) = hi;
+        *reinterpret_cast<f32x4*>(&rows_lds[threadIdx.x][0]) = lo;
+        *reinterpret_cast<f32x4*>(&rows_lds[threadIdx.x][4]) = hi;
         __syncthreads();
         if (lane_row == 0)
           for (int r = 1; r < n_rows; ++r) {
@@ -458,12 +497,12 @@ __device__ __forceinline__ void bwd_body(const NormArgs& a) {
 
 template <int V, bool XF32, int KIND>
 __global__ __launch_bounds__(kBwdThreads) void block_norm_bwd_kernel(const NormArgs a) {
-  bwd_body<V, XF32, KIND>(a);
+  bwd_body<V, XF32, KIND, false>(a);
 }
 // rows of more than kBwdThreads * kMaxV chunks
 template <int V, bool XF32, int KIND>
 __global__ __launch_bounds__(kMaxThreads) void block_norm_bwd_long_kernel(const NormArgs a) {
-  bwd_body<V, XF32, KIND>(a);
+  bwd_body<V, XF32, KIND, true>(a);
 }
 
 // The groups' partial sums added up in a fixed order: 16 lanes hold 64 columns, 16 threads of a column take every 16th group; then these in order.
@@ -639,7 +678,7 @@ extern "C" int ntp_block_norm_bwd(ntp_handle_t* h, const ntp_block_norm_shape_t*
     constexpr int V = decltype(v)::value, KIND = decltype(kind)::value;
     constexpr bool F32 = decltype(f32)::value;
     if (threads > kBwdThreads) hipLaunchKernelGGL((block_norm_bwd_long_kernel<kMaxV, F32, KIND>), grid, block, 0, hs, a);
-    else hipLaunchKernelGGL((block_norm_bwd_kernel<V, F32, KIND>), grid, block, 0, hs, a);
+    else hipLaunchKernelGGL((block_norm_bwd_kernel<V, F32, KIND>), grid, block, uint32_t(KIND == 0 ? 1 : KIND == 1 ? 3 : 4) * (V << a.t_log2) * 16u, hs, a);
   };
   using std::integral_constant;
   by_chunks(norm_chunks(s->H, a.t_log2), [&](auto v) {
