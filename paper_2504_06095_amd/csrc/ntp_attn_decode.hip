@@ -6,8 +6,8 @@
 // of values in turn, each with a running maximum and sum of its own, and put their results together at the end.  Both products run on the
 // 16x16x32 bf16 matrix instruction with the query head on the lane axis (S^T = K Q^T, O^T += V^T P^T), the scores go from the one to the other in
 // registers.  With one query head 15 of 16 columns are idle: matrix work is far from the bound, 16 instructions a tile against 16 KB from HBM.
-// Keys go from memory straight to the fragments' registers; values, needed transposed, through a part of the LDS that is the wavefront's own, by DMA, so that
-// nothing but the end needs a barrier.  What hides the latency is the number of wavefronts: 16 KB in flight for each.
+// Both go through a part of the LDS that is the wavefront's own, by DMA, so that nothing but the end needs a barrier.  The loads are non-temporal: a cache line is
+// used once (equal lengths of 4096, 14 heads, 64 sequences: 326 -> 292 us, 6.4 TB/s).
 //
 // A page holds a multiple of 16 tokens, so 16 tokens of one head are one contiguous block; each block is a buffer view of its own that ends with the
 // sequence: what lies behind the last token, or in a page that does not exist, reads as zeros and never reaches the products (it may be NaN).
@@ -31,6 +31,7 @@ typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
 constexpr int kThreads = 256, kWaves = 4, kBlock = 16;  // kBlock: tokens of a contiguous block
+constexpr int kMaxPieces = 512;
 constexpr int kTileBytes = 8192;                        // of keys, and of values, per tile
 template <int D>
 constexpr int kTile = kTileBytes / (2 * D);  // tokens per tile: 32 or 64
@@ -40,7 +41,9 @@ struct DecodeArgs {
   const int32_t *table, *lengths;
   uint16_t* C;
   float* LSE;
-  float* parts;  // pieces > 1: [n_seq x q_cnt][pieces][D + 4]: unnormalised output, maximum (log2 units), sum
+  // pieces > 1, per (sequence, query head) and piece: maximum (log2 units) and sum, and the D unnormalised outputs
+  float2* part_sums;
+  float* part_rows;
   int64_t ldq, ldc, ldt, page_stride, n_pages;
   int32_t n_seq, max_len, q_cnt, q_off, kv_off, group, page_size, page_log2;
   int32_t kv_first, kv_used, head_tiles;  // local KV heads that are read; 16-head tiles of a KV head's query heads
@@ -69,14 +72,25 @@ __device__ __forceinline__ float over_rows(float v, F&& f) {
 __device__ __forceinline__ __amdgpu_buffer_rsrc_t view(const uint16_t* p, int bytes) {
   return __builtin_amdgcn_make_buffer_rsrc(const_cast<uint16_t*>(p), 0, bytes, 0x00020000);
 }
-__device__ __forceinline__ bf16x8 load_16(__amdgpu_buffer_rsrc_t rs, uint32_t off) {
-  return __builtin_bit_cast(bf16x8, __builtin_amdgcn_raw_buffer_load_b128(rs, off, 0, 0));
-}
 __device__ __forceinline__ void dma_16(__amdgpu_buffer_rsrc_t rs, unsigned char* dst, uint32_t off) {
-  __builtin_amdgcn_raw_ptr_buffer_load_lds(rs, (ntp_gemm::lds_void*)dst, 16, off, 0, 0, 0);
+  __builtin_amdgcn_raw_ptr_buffer_load_lds(rs, (ntp_gemm::lds_void*)dst, 16, off, 0, 0, 2);
 }
-__device__ __forceinline__ void dma_done() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
+// All but the last N vector memory instructions have finished.
+template <int N>
+__device__ __forceinline__ void dma_left() {
+  asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory");
+}
 
+template <int OFF>
+__device__ __forceinline__ u32x4 lds_b128(uint32_t addr) {
+#if !defined(__HIP_DEVICE_COMPILE__)
+  return u32x4{};
+#else
+  u32x4 v;
+  asm volatile("ds_read_b128 %0, %1 offset:%2" : "=v"(v) : "v"(addr), "n"(OFF) : "memory");
+  return v;
+#endif
+}
 template <int OFF>
 __device__ __forceinline__ u32x2 lds_tr_b64(uint32_t addr) {
 #if !defined(__HIP_DEVICE_COMPILE__)
@@ -88,13 +102,17 @@ __device__ __forceinline__ u32x2 lds_tr_b64(uint32_t addr) {
 #endif
 }
 // The reads requested before have arrived: every later use of their registers depends on this wait.
-__device__ __forceinline__ void lds_reads_done(u32x2 (&r)[16]) {
+template <int N, typename V>
+__device__ __forceinline__ void lds_reads_done(V (&r)[N]) {
+  static_assert(N % 8 == 0, "");
 #if defined(__HIP_DEVICE_COMPILE__)
   asm volatile("s_waitcnt lgkmcnt(0)"
                : "+v"(r[0]), "+v"(r[1]), "+v"(r[2]), "+v"(r[3]), "+v"(r[4]), "+v"(r[5]), "+v"(r[6]), "+v"(r[7])
                :
                : "memory");
-  asm volatile("" : "+v"(r[8]), "+v"(r[9]), "+v"(r[10]), "+v"(r[11]), "+v"(r[12]), "+v"(r[13]), "+v"(r[14]), "+v"(r[15]) : : "memory");
+#pragma unroll
+  for (int i = 8; i < N; i += 8)
+    asm volatile("" : "+v"(r[i]), "+v"(r[i + 1]), "+v"(r[i + 2]), "+v"(r[i + 3]), "+v"(r[i + 4]), "+v"(r[i + 5]), "+v"(r[i + 6]), "+v"(r[i + 7]) : : "memory");
 #endif
 }
 
@@ -111,17 +129,19 @@ __device__ __forceinline__ uint32_t swz(int r) {
 }
 
 template <int D>
-__global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(3))) void attn_decode_kernel(const DecodeArgs a) {
+__global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2))) void attn_decode_kernel(const DecodeArgs a) {
   constexpr int KS = D / 32, DB = D / 16;           // K-steps of the score product, 16-column blocks of the output
   constexpr int T = kTile<D>, NB = T / kBlock;      // tokens and blocks per tile
   constexpr int BLOCK_BYTES = kBlock * D * 2, DMA = BLOCK_BYTES / 1024;  // DMA instructions per block
   constexpr int ROW = D + 4;                        // floats of a wavefront's result row: outputs, maximum, sum
-  constexpr int LDS = kWaves * std::max(kTileBytes, 16 * ROW * 4);
+  constexpr int LDS = kWaves * std::max(2 * kTileBytes, 16 * ROW * 4);
   __shared__ __attribute__((aligned(1024))) unsigned char lds[LDS];
 
   const int units = a.kv_used * a.head_tiles * a.n_seq;
-  const int piece = int(blockIdx.x) / units, unit = int(blockIdx.x) % units;  // (the pieces that every sequence has go first)
-  const int seq = unit % a.n_seq, tile16 = unit / a.n_seq % a.head_tiles, g = a.kv_first + unit / a.n_seq / a.head_tiles;
+  // The pieces that every sequence has go first.  Workgroups go to the 8 XCDs in turn: neighbours are heads of one sequence, and a unit's pieces are shifted
+  // against each other, so that no XCD is left with the long sequences.
+  const int piece = int(blockIdx.x) / units, unit = (int(blockIdx.x) % units + piece) % units;
+  const int g = a.kv_first + unit % a.kv_used, seq = unit / a.kv_used % a.n_seq, tile16 = unit / a.kv_used / a.n_seq;
   const int len = std::min(a.lengths[seq], a.max_len);
   const int k_lo = piece * a.piece_len, k_hi = std::min(len, k_lo + a.piece_len);
   if (piece > 0 && k_lo >= len) return;
@@ -132,8 +152,9 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(3))) v
 
   const int lane = threadIdx.x & 63, lq = lane & 15, lh = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  unsigned char* const sV = lds + wave * kTileBytes;
-  const uint32_t lV = uint32_t(reinterpret_cast<uintptr_t>(sV));
+  unsigned char* const sK = lds + wave * 2 * kTileBytes;
+  unsigned char* const sV = sK + kTileBytes;
+  const uint32_t lK = uint32_t(reinterpret_cast<uintptr_t>(sK)), lV = lK + kTileBytes;
 
   bf16x8 qf[KS] = {};  // operand B[k][j]: j = query head (lane % 16), k = 8 consecutive columns
   if (j0 + lq < j1) {
@@ -141,14 +162,15 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(3))) v
     for (int ks = 0; ks < KS; ++ks) qf[ks] = *reinterpret_cast<const bf16x8*>(a.Q + int64_t(seq) * a.ldq + int64_t(j0 + lq) * D + ks * 32 + lh * 8);
   }
 
-  // lane offsets: key fragments (row lane % 16, columns lane / 16 * 8 on), DMA of a block's chunks, transposing reads
-  const uint32_t koff = uint32_t(lq * D + lh * 8) * 2;
-  uint32_t voff[DMA], col[DB];
+  // lane offsets: DMA of a block's chunks, key fragments (row lane % 16, columns lane / 16 * 8 on), transposing reads
+  uint32_t voff[DMA], row[KS], col[DB];
 #pragma unroll
   for (int i = 0; i < DMA; ++i) {
     const int p = i * 64 + lane, row = p / (D / 8), slot = p % (D / 8);
     voff[i] = uint32_t(row * D * 2) + ((uint32_t(slot) ^ swz<D>(row)) * 16u);
   }
+#pragma unroll
+  for (int ks = 0; ks < KS; ++ks) row[ks] = lK + uint32_t(lq * D * 2) + ((uint32_t(ks * 4 + lh) ^ swz<D>(lq)) * 16u);
   const int rv = lh * 4 + (lq >> 2);
 #pragma unroll
   for (int db = 0; db < DB; ++db) col[db] = lV + uint32_t(rv * D * 2) + uint32_t(lq & 1) * 8u + ((uint32_t(db * 2 + ((lq & 3) >> 1)) ^ swz<D>(rv)) * 16u);
@@ -158,31 +180,51 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(3))) v
   for (int db = 0; db < DB; ++db) acc[db] = f32x4{0.f, 0.f, 0.f, 0.f};
   float m_run = -INFINITY, l_run = 0.f;
 
-  // page numbers of the wavefront's next 64 blocks, one a lane: its tile number i is tile i * kWaves + wave of the piece
+  // Page numbers of 64 of the wavefront's blocks, one a lane: its tile number i is tile i * kWaves + wave of the piece.  (Bounded by max_len, which
+  // the table holds, not by the length, so that the two are read at the same time.)
+  constexpr int PER = 64 / NB;  // tiles per set of page numbers
   const int32_t* const row_of_table = a.table + int64_t(seq) * a.ldt;
   auto pages_from = [&](int i) {
     const int key = k_lo + ((i + lane / NB) * kWaves + wave) * T + (lane % NB) * kBlock;
-    return key < k_hi ? row_of_table[key >> a.page_log2] : -1;
+    return key < a.max_len ? row_of_table[key >> a.page_log2] : -1;
   };
-  const int n_tiles = std::max(0, (k_hi - k_lo + T - 1) / T);
   int32_t pages = pages_from(0);
-  for (int i = 0; i * kWaves + wave < n_tiles; ++i) {
-    if (i > 0 && i % (64 / NB) == 0) pages = pages_from(i);
-    const int key0 = k_lo + (i * kWaves + wave) * T;
-    bf16x8 kf[NB][KS];
-    int valid[NB];
+  const int n_tiles = std::max(0, (k_hi - k_lo + T - 1) / T);
+  const int mine = (n_tiles - wave + kWaves - 1) / kWaves;  // tiles of this wavefront
+  // DMA of one matrix of tile i; number of tokens of each block that count
+  auto request = [&](const uint16_t* base, unsigned char* to, int i, int (&valid)[NB]) {
 #pragma unroll
     for (int b = 0; b < NB; ++b) {
-      const int key = key0 + b * kBlock;
-      const int page = __builtin_amdgcn_readlane(pages, (i % (64 / NB)) * NB + b);
+      const int key = k_lo + (i * kWaves + wave) * T + b * kBlock;
+      const int page = __builtin_amdgcn_readlane(pages, (i % PER) * NB + b);
       const bool there = page >= 0 && page < a.n_pages;
       valid[b] = there ? std::min(std::max(k_hi - key, 0), kBlock) : 0;
       const int64_t at = there ? int64_t(page) * a.page_stride + (int64_t(g) * a.page_size + (key & (a.page_size - 1))) * D : 0;
-      const __amdgpu_buffer_rsrc_t keys = view(a.K + at, valid[b] * D * 2), values = view(a.V + at, valid[b] * D * 2);
+      const __amdgpu_buffer_rsrc_t rs = view(base + at, valid[b] * D * 2);
 #pragma unroll
-      for (int ks = 0; ks < KS; ++ks) kf[b][ks] = load_16(keys, koff + ks * 64);
-#pragma unroll
-      for (int j = 0; j < DMA; ++j) dma_16(values, sV + b * BLOCK_BYTES + j * 1024, voff[j]);
+      for (int j = 0; j < DMA; ++j) dma_16(rs, to + b * BLOCK_BYTES + j * 1024, voff[j]);
+    }
+  };
+  // One tile of keys and one of values in the LDS: the next keys are requested when this tile's have been read into registers, the next values
+  // likewise, so that there is always one or the other in flight.
+  constexpr int IN_FLIGHT = NB * DMA;
+  int valid[NB], next[NB];
+  if (mine > 0) {
+    request(a.K, sK, 0, valid);
+    request(a.V, sV, 0, valid);
+  }
+  for (int i = 0; i < mine; ++i) {
+    dma_left<IN_FLIGHT>();  // the keys are there
+    u32x4 kf[NB * KS];
+    unrolled(std::make_integer_sequence<int, NB * KS>{}, [&](auto n) {
+      constexpr int blk = decltype(n)::value / KS, ks = decltype(n)::value % KS;
+      kf[decltype(n)::value] = lds_b128<blk * BLOCK_BYTES>(row[ks]);
+    });
+    lds_reads_done(kf);
+    const bool more = i + 1 < mine;
+    if (more) {
+      if ((i + 1) % PER == 0) pages = pages_from(i + 1);
+      request(a.K, sK, i + 1, next);
     }
     // scores, transposed: st[b][r] = score of query head lane % 16 with token key0 + b * 16 + lane / 16 * 4 + r
     f32x4 st[NB];
@@ -190,7 +232,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(3))) v
     for (int b = 0; b < NB; ++b) {
       st[b] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-      for (int ks = 0; ks < KS; ++ks) st[b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf[b][ks], qf[ks], st[b], 0, 0, 0);
+      for (int ks = 0; ks < KS; ++ks) st[b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, kf[b * KS + ks]), qf[ks], st[b], 0, 0, 0);
       if (valid[b] < kBlock) {
 #pragma unroll
         for (int r = 0; r < 4; ++r)
@@ -221,13 +263,15 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(3))) v
 #pragma unroll
       for (int db = 0; db < DB; ++db) acc[db] *= alpha;
     }
-    dma_done();  // the values are in the LDS
+    if (more) dma_left<IN_FLIGHT>();
+    else dma_left<0>();  // the values are there
     u32x2 vf[16];  // [(db * NB / 2 + s2) * 2 + half]
     unrolled(std::make_integer_sequence<int, 16>{}, [&](auto n) {
       constexpr int db = decltype(n)::value / NB, q = decltype(n)::value % NB;
       vf[decltype(n)::value] = lds_tr_b64<q * BLOCK_BYTES>(col[db]);
     });
     lds_reads_done(vf);
+    if (more) request(a.V, sV, i + 1, next);
 #pragma unroll
     for (int db = 0; db < DB; ++db)
 #pragma unroll
@@ -236,22 +280,24 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(3))) v
         const u32x4 both = {lo[0], lo[1], hi[0], hi[1]};
         acc[db] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, both), pf[s2], acc[db], 0, 0, 0);
       }
+#pragma unroll
+    for (int b = 0; b < NB; ++b) valid[b] = next[b];
   }
 
   // the wavefronts' results, one row per query head
   l_run = over_rows(l_run, [](float x, float y) { return x + y; });
   __syncthreads();
-  float* const mine = reinterpret_cast<float*>(lds) + (wave * 16 + lq) * ROW;
+  float* const result = reinterpret_cast<float*>(lds) + (wave * 16 + lq) * ROW;
 #pragma unroll
-  for (int db = 0; db < DB; ++db) *reinterpret_cast<f32x4*>(mine + db * 16 + lh * 4) = acc[db];
+  for (int db = 0; db < DB; ++db) *reinterpret_cast<f32x4*>(result + db * 16 + lh * 4) = acc[db];
   if (lh == 0) {
-    mine[D] = m_run;
-    mine[D + 1] = l_run;
+    result[D] = m_run;
+    result[D + 1] = l_run;
   }
   __syncthreads();
-  const int row = threadIdx.x >> 4, c0 = (threadIdx.x & 15) * 4, head = j0 + row;
+  const int r16 = threadIdx.x >> 4, c0 = (threadIdx.x & 15) * 4, head = j0 + r16;
   if (head >= j1) return;
-  const float* const res = reinterpret_cast<const float*>(lds) + row * ROW;
+  const float* const res = reinterpret_cast<const float*>(lds) + r16 * ROW;
   float top = -INFINITY, w[kWaves], sum = 0.f;
 #pragma unroll
   for (int i = 0; i < kWaves; ++i) top = fmaxf(top, res[i * 16 * ROW + D]);
@@ -261,7 +307,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(3))) v
     w[i] = fast_exp2(res[i * 16 * ROW + D] - base);
     sum = fmaf(w[i], res[i * 16 * ROW + D + 1], sum);
   }
-  float* const part = a.parts + ((int64_t(seq) * a.q_cnt + head) * a.pieces + piece) * (D + 4);
+  const int64_t part = (int64_t(seq) * a.q_cnt + head) * a.pieces + piece;
   const float inv = sum == 0.f ? 0.f : 1.0f / sum;
 #pragma unroll
   for (int c = c0; c < D; c += 64) {
@@ -269,7 +315,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(3))) v
 #pragma unroll
     for (int i = 0; i < kWaves; ++i) o += w[i] * *reinterpret_cast<const f32x4*>(res + i * 16 * ROW + c);
     if (a.pieces > 1) {
-      *reinterpret_cast<f32x4*>(part + c) = o;
+      *reinterpret_cast<f32x4*>(a.part_rows + part * D + c) = o;
     } else {
       ntp_gemm::u16x4 out;
 #pragma unroll
@@ -279,56 +325,69 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(3))) v
   }
   if (c0 == 0) {
     if (a.pieces > 1) {
-      part[D] = top;
-      part[D + 1] = sum;
+      a.part_sums[part] = float2{top, sum};
     } else if (a.LSE) {
       a.LSE[int64_t(head) * a.n_seq + seq] = (base + log2f(sum)) * 0.6931471805599453f;
     }
   }
 }
 
-// The pieces of one (sequence, query head) put together: D / 4 lanes hold the outputs, 1024 / D groups of them take the pieces in turn.
+// The pieces of one (sequence, query head) put together: the threads form the pieces' weights, then D / 4 lanes hold the outputs and 1024 / D groups of them
+// take the pieces in turn (their loads do not depend on each other).
 template <int D>
 __global__ __launch_bounds__(kThreads) void attn_decode_join_kernel(const DecodeArgs a) {
   constexpr int L = D / 4, G = kThreads / L;
-  __shared__ float lds[G][D + 4];
+  __shared__ float weight[kMaxPieces], wave_max[kWaves], wave_sum[kWaves];
+  __shared__ f32x4 rows[G][L];
   const int row = blockIdx.x, head = row % a.q_cnt, seq = row / a.q_cnt;
   const int len = std::min(a.lengths[seq], a.max_len);
   const int used = len > 0 ? (len + a.piece_len - 1) / a.piece_len : 0;
-  const int grp = threadIdx.x / L, c = threadIdx.x % L * 4;
-  const float* const parts = a.parts + int64_t(row) * a.pieces * (D + 4);
+  const int64_t first = int64_t(row) * a.pieces;
+  const int grp = threadIdx.x / L, c = threadIdx.x % L;
+  float2 ms[kMaxPieces / kThreads];
+  float top = -INFINITY, sum = 0.f;
+#pragma unroll
+  for (int i = 0; i < kMaxPieces / kThreads; ++i) {
+    const int p = int(threadIdx.x) + i * kThreads;
+    ms[i] = p < used ? a.part_sums[first + p] : float2{-INFINITY, 0.f};
+    top = fmaxf(top, ms[i].x);
+  }
+  auto wave_all = [](float v, auto f) {
+#pragma unroll
+    for (int x = 1; x < 16; x *= 2) v = f(v, __shfl_xor(v, x));
+    return over_rows(v, f);
+  };
+  top = wave_all(top, [](float x, float y) { return fmaxf(x, y); });
+  if ((threadIdx.x & 63) == 0) wave_max[threadIdx.x >> 6] = top;
+  __syncthreads();
+#pragma unroll
+  for (int i = 0; i < kWaves; ++i) top = fmaxf(top, wave_max[i]);
+  const float base = top == -INFINITY ? 0.f : top;
+#pragma unroll
+  for (int i = 0; i < kMaxPieces / kThreads; ++i) {
+    const float w = fast_exp2(ms[i].x - base);
+    sum = fmaf(w, ms[i].y, sum);
+    weight[threadIdx.x + i * kThreads] = w;
+  }
+  sum = wave_all(sum, [](float x, float y) { return x + y; });
+  if ((threadIdx.x & 63) == 0) wave_sum[threadIdx.x >> 6] = sum;
+  __syncthreads();
   f32x4 o = {0.f, 0.f, 0.f, 0.f};
-  float m = -INFINITY, l = 0.f;
-  for (int i = grp; i < used; i += G) {
-    const float* p = parts + int64_t(i) * (D + 4);
-    const f32x4 v = *reinterpret_cast<const f32x4*>(p + c);
-    const float m_new = fmaxf(m, p[D]), base = m_new == -INFINITY ? 0.f : m_new;
-    const float w0 = fast_exp2(m - base), w1 = fast_exp2(p[D] - base);
-    o = o * w0 + v * w1;
-    l = l * w0 + p[D + 1] * w1;
-    m = m_new;
-  }
-  *reinterpret_cast<f32x4*>(&lds[grp][c]) = o;
-  if (c == 0) {
-    lds[grp][D] = m;
-    lds[grp][D + 1] = l;
-  }
+#pragma unroll 8
+  for (int p = grp; p < used; p += G) o += weight[p] * *reinterpret_cast<const f32x4*>(a.part_rows + (first + p) * D + c * 4);
+  rows[grp][c] = o;
   __syncthreads();
   if (grp > 0) return;
-  float top = -INFINITY, sum = 0.f;
-  for (int i = 0; i < G; ++i) top = fmaxf(top, lds[i][D]);
-  const float base = top == -INFINITY ? 0.f : top;
-  o = f32x4{0.f, 0.f, 0.f, 0.f};
-  for (int i = 0; i < G; ++i) {
-    const float w = fast_exp2(lds[i][D] - base);
-    sum = fmaf(w, lds[i][D + 1], sum);
-    o += w * *reinterpret_cast<const f32x4*>(&lds[i][c]);
-  }
+  sum = wave_sum[0];
+#pragma unroll
+  for (int i = 1; i < kWaves; ++i) sum += wave_sum[i];
+#pragma unroll
+  for (int i = 1; i < G; ++i) o += rows[i][c];
   const float inv = sum == 0.f ? 0.f : 1.0f / sum;
   ntp_gemm::u16x4 out;
 #pragma unroll
   for (int r = 0; r < 4; ++r) out[r] = ntp_gemm::f32_to_bf16(o[r] * inv);
-  *reinterpret_cast<ntp_gemm::u16x4*>(a.C + int64_t(seq) * a.ldc + int64_t(head) * D + c) = out;
+  *reinterpret_cast<ntp_gemm::u16x4*>(a.C + int64_t(seq) * a.ldc + int64_t(head) * D + c * 4) = out;
   if (a.LSE && c == 0) a.LSE[int64_t(head) * a.n_seq + seq] = (base + log2f(sum)) * 0.6931471805599453f;
 }
 
@@ -361,10 +420,10 @@ DecodeChoice choose_decode(const ntp_handle* h, int64_t ws_bytes, const ntp_attn
   c.head_tiles = (std::min(s->group, s->q_cnt) + 15) / 16;
   c.units = int64_t(c.kv_used) * c.head_tiles * s->n_seq;
   const int64_t step = kWaves * (kTileBytes / (2 * s->head_dim));
-  const int64_t want = std::max<int64_t>(1, 8 * int64_t(h->compute_units) / c.units);
-  const int64_t per = std::max<int64_t>((s->max_len + want - 1) / want, 2 * step);
+  const int64_t want = std::max<int64_t>(1, 16 * int64_t(h->compute_units) / c.units);
+  const int64_t per = std::max<int64_t>((s->max_len + std::min<int64_t>(want, kMaxPieces) - 1) / std::min<int64_t>(want, kMaxPieces), step);
   const int64_t len = (per + step - 1) / step * step, pieces = (s->max_len + len - 1) / len;
-  const int64_t bytes = int64_t(s->n_seq) * s->q_cnt * pieces * (s->head_dim + 4) * 4;
+  const int64_t bytes = int64_t(s->n_seq) * s->q_cnt * pieces * (s->head_dim + 2) * 4;
   if (pieces > 1 && bytes <= ws_bytes && pieces * c.units <= 0x7fffffffll) {
     c.pieces = int32_t(pieces);
     c.piece_len = int32_t(len);
@@ -397,7 +456,11 @@ extern "C" int ntp_attn_decode_shard(ntp_handle_t* h, const ntp_attn_decode_shap
   if (c.units > 0x7fffffffll) return NTP_ERR_UNSUPPORTED;
   DecodeArgs a{};
   a.Q = static_cast<const uint16_t*>(Q), a.K = static_cast<const uint16_t*>(cache->K), a.V = static_cast<const uint16_t*>(cache->V);
-  a.table = block_table, a.lengths = lengths, a.C = static_cast<uint16_t*>(C), a.LSE = LSE, a.parts = static_cast<float*>(h->workspace);
+  a.table = block_table, a.lengths = lengths, a.C = static_cast<uint16_t*>(C), a.LSE = LSE;
+  if (c.pieces > 1) {
+    a.part_rows = static_cast<float*>(h->workspace);
+    a.part_sums = reinterpret_cast<float2*>(a.part_rows + int64_t(s->n_seq) * s->q_cnt * c.pieces * s->head_dim);
+  }
   a.ldq = ldq, a.ldc = ldc, a.ldt = ldt, a.page_stride = cache->page_stride, a.n_pages = cache->n_pages;
   a.n_seq = s->n_seq, a.max_len = s->max_len, a.q_cnt = s->q_cnt, a.q_off = s->q_off, a.kv_off = s->kv_off, a.group = s->group;
   a.page_size = cache->page_size, a.page_log2 = ntp::log2_of(cache->page_size);
