@@ -2,11 +2,16 @@
 //   C[s, j] = sum_t p_t V[t] / sum_t p_t,   p_t = exp(q_j . K[t] / sqrt(d) - max),   t over the sequence's tokens.
 // One pass over the keys with a running maximum and sum.  Every key and value is read once, 4 d bytes for 4 d operations a query head: HBM bounds it.
 //
-// A workgroup takes a piece of one sequence's tokens for (up to) 16 query heads of one KV head; its four wavefronts take its tiles of 8 KB of keys and 8 KB
-// of values in turn, each with a running maximum and sum of its own, and put their results together at the end.  Both products run on the
+// The work of a call is a line of steps, sequence by sequence, in it unit by unit (a KV head with up to 16 of its query heads), a unit's steps along its tokens; a step is
+// one tile (8 KB of keys, 8 KB of values) for each of a workgroup's four wavefronts.  With a workspace the line is cut into equal shares, two workgroups per compute
+// unit, from the lengths on the device: lengths that differ, or that lie far below max_len, leave no workgroup idle.  A workgroup writes the units that lie wholly in
+// its share and leaves partial results of the one it begins inside and the one it ends inside, which a second kernel joins.  Without a workspace
+// a workgroup takes one unit.
+//
+// The wavefronts of a workgroup have a running maximum and sum of their own and put their results together at the end of a unit.  Both products run on the
 // 16x16x32 bf16 matrix instruction with the query head on the lane axis (S^T = K Q^T, O^T += V^T P^T), the scores go from the one to the other in
 // registers.  With one query head 15 of 16 columns are idle: matrix work is far from the bound, 16 instructions a tile against 16 KB from HBM.
-// Both go through a part of the LDS that is the wavefront's own, by DMA, so that nothing but the end needs a barrier.  The loads are non-temporal: a cache line is
+// Both matrices go through a part of the LDS that is the wavefront's own, by DMA, so that nothing but a unit's end needs a barrier.  The loads are non-temporal: a cache line is
 // used once (equal lengths of 4096, 14 heads, 64 sequences: 326 -> 292 us, 6.4 TB/s).
 //
 // A page holds a multiple of 16 tokens, so 16 tokens of one head are one contiguous block; each block is a buffer view of its own that ends with the
@@ -31,23 +36,26 @@ typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
 constexpr int kThreads = 256, kWaves = 4, kBlock = 16;  // kBlock: tokens of a contiguous block
-constexpr int kMaxPieces = 512;
+constexpr int kMaxShares = 1024;
 constexpr int kTileBytes = 8192;                        // of keys, and of values, per tile
 template <int D>
 constexpr int kTile = kTileBytes / (2 * D);  // tokens per tile: 32 or 64
+template <int D>
+constexpr int kStep = kWaves * kTile<D>;     // tokens per step
 
 struct DecodeArgs {
   const uint16_t *Q, *K, *V;
   const int32_t *table, *lengths;
   uint16_t* C;
   float* LSE;
-  // pieces > 1, per (sequence, query head) and piece: maximum (log2 units) and sum, and the D unnormalised outputs
+  // shares of the line of steps: per workgroup two partial results (of the unit it begins inside and the one it ends inside) of 16 query heads each:
+  // maximum (log2 units) and sum, and the D unnormalised outputs.  NULL: workgroup = unit
   float2* part_sums;
   float* part_rows;
   int64_t ldq, ldc, ldt, page_stride, n_pages;
   int32_t n_seq, max_len, q_cnt, q_off, kv_off, group, page_size, page_log2;
   int32_t kv_first, kv_used, head_tiles;  // local KV heads that are read; 16-head tiles of a KV head's query heads
-  int32_t pieces, piece_len;              // a sequence is cut into pieces of piece_len tokens
+  int32_t shares;
   float scale_log2;                       // log2(e) / sqrt(d)
 };
 
@@ -128,6 +136,77 @@ __device__ __forceinline__ uint32_t swz(int r) {
   return D == 128 ? uint32_t((r & 7) << 1) : uint32_t(((r >> 1) & 3) << 1);
 }
 
+// Steps of a sequence's unit: at least one, which writes the zeros of a sequence without tokens.
+template <int D>
+__device__ __forceinline__ int steps_of(const DecodeArgs& a, int len) {
+  return std::max(1, (std::min(len, a.max_len) + kStep<D> - 1) / kStep<D>);
+}
+// Inclusive sum over the wavefront's lanes: inside rows of 16 lanes, then the rows' last values are passed on.
+template <int CTRL, int ROWS>
+__device__ __forceinline__ int dpp_add(int v) {
+  return v + __builtin_amdgcn_update_dpp(0, v, CTRL, ROWS, 0xf, false);
+}
+__device__ __forceinline__ int sum_upto(int v) {
+  v = dpp_add<0x111, 0xf>(v);  // shifted by 1, 2, 4, 8 lanes
+  v = dpp_add<0x112, 0xf>(v);
+  v = dpp_add<0x114, 0xf>(v);
+  v = dpp_add<0x118, 0xf>(v);
+  v = dpp_add<0x142, 0xa>(v);  // lane 15 of a row to the next one: rows 1 and 3
+  v = dpp_add<0x143, 0xc>(v);  // lane 31 to rows 2 and 3
+  return v;
+}
+
+// The line of steps: 64 sequences at a time in the lanes of a wavefront (every wavefront for itself).
+template <int D>
+struct Line {
+  int len, upto;        // of this lane's sequence base + lane: its length, and the steps of a unit up to and with it
+  int base, before;     // the first of the 64, and the steps of the sequences before it
+  int per_seq, total;   // units of a sequence; steps of the line
+  int shares, q, r;     // share w has q steps, the first r shares one more
+  __device__ __forceinline__ void load(const DecodeArgs& a, int from) {
+    const int i = from + int(threadIdx.x & 63);
+    base = from;
+    len = i < a.n_seq ? a.lengths[i] : 0;
+    upto = sum_upto(i < a.n_seq ? steps_of<D>(a, len) : 0);
+  }
+  __device__ __forceinline__ int last() const { return __builtin_amdgcn_readlane(upto, 63); }
+  // the whole line; then the first 64 sequences
+  __device__ __forceinline__ void measure(const DecodeArgs& a) {
+    before = 0;
+    for (int from = 0; from < a.n_seq; from += 64) {
+      if (from > 0) before += last();
+      load(a, from);
+    }
+    total = (before + last()) * per_seq;
+    shares = std::min(a.shares, total);  // (one step at least for each)
+    q = total / shares;
+    r = total % shares;
+    before = 0;
+    if (base > 0) load(a, 0);
+  }
+  __device__ __forceinline__ int begin(int w) const { return w * q + std::min(w, r); }
+  __device__ __forceinline__ int share_of(int x) const { return x < r * (q + 1) ? x / (q + 1) : r + (x - r * (q + 1)) / q; }
+  __device__ __forceinline__ void next64(const DecodeArgs& a) {
+    before += last();
+    load(a, base + 64);
+  }
+  __device__ __forceinline__ int length(int seq) const { return __builtin_amdgcn_readlane(len, seq - base); }
+  // steps of the sequences before seq, one of the 64
+  __device__ __forceinline__ int steps_before(int seq) const { return before + (seq > base ? __builtin_amdgcn_readlane(upto, seq - base - 1) : 0); }
+};
+
+// This unit's KV head and its local query heads j0 .. j1 - 1.
+struct Heads {
+  int g, j0, j1;
+  __device__ __forceinline__ Heads(const DecodeArgs& a, int unit) {
+    const int tile = unit % a.head_tiles;
+    g = a.kv_first + unit / a.head_tiles;
+    const int64_t first = int64_t(a.kv_off + g) * a.group - a.q_off;
+    j0 = int(std::max<int64_t>(first, 0)) + tile * 16;
+    j1 = int(std::min<int64_t>(std::min<int64_t>(first + a.group, a.q_cnt), j0 + 16));
+  }
+};
+
 template <int D>
 __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2))) void attn_decode_kernel(const DecodeArgs a) {
   constexpr int KS = D / 32, DB = D / 16;           // K-steps of the score product, 16-column blocks of the output
@@ -137,30 +216,11 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2))) v
   constexpr int LDS = kWaves * std::max(2 * kTileBytes, 16 * ROW * 4);
   __shared__ __attribute__((aligned(1024))) unsigned char lds[LDS];
 
-  const int units = a.kv_used * a.head_tiles * a.n_seq;
-  // The pieces that every sequence has go first.  Workgroups go to the 8 XCDs in turn: neighbours are heads of one sequence, and a unit's pieces are shifted
-  // against each other, so that no XCD is left with the long sequences.
-  const int piece = int(blockIdx.x) / units, unit = (int(blockIdx.x) % units + piece) % units;
-  const int g = a.kv_first + unit % a.kv_used, seq = unit / a.kv_used % a.n_seq, tile16 = unit / a.kv_used / a.n_seq;
-  const int len = std::min(a.lengths[seq], a.max_len);
-  const int k_lo = piece * a.piece_len, k_hi = std::min(len, k_lo + a.piece_len);
-  if (piece > 0 && k_lo >= len) return;
-  // this KV head's local query heads, and the 16 (or fewer) of this workgroup
-  const int64_t first = int64_t(a.kv_off + g) * a.group - a.q_off;
-  const int j0 = int(std::max<int64_t>(first, 0)) + tile16 * 16, j1 = int(std::min<int64_t>(std::min<int64_t>(first + a.group, a.q_cnt), j0 + 16));
-  if (j0 >= j1) return;
-
   const int lane = threadIdx.x & 63, lq = lane & 15, lh = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   unsigned char* const sK = lds + wave * 2 * kTileBytes;
   unsigned char* const sV = sK + kTileBytes;
   const uint32_t lK = uint32_t(reinterpret_cast<uintptr_t>(sK)), lV = lK + kTileBytes;
-
-  bf16x8 qf[KS] = {};  // operand B[k][j]: j = query head (lane % 16), k = 8 consecutive columns
-  if (j0 + lq < j1) {
-#pragma unroll
-    for (int ks = 0; ks < KS; ++ks) qf[ks] = *reinterpret_cast<const bf16x8*>(a.Q + int64_t(seq) * a.ldq + int64_t(j0 + lq) * D + ks * 32 + lh * 8);
-  }
 
   // lane offsets: DMA of a block's chunks, key fragments (row lane % 16, columns lane / 16 * 8 on), transposing reads
   uint32_t voff[DMA], row[KS], col[DB];
@@ -175,21 +235,56 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2))) v
 #pragma unroll
   for (int db = 0; db < DB; ++db) col[db] = lV + uint32_t(rv * D * 2) + uint32_t(lq & 1) * 8u + ((uint32_t(db * 2 + ((lq & 3) >> 1)) ^ swz<D>(rv)) * 16u);
 
+  // this workgroup's steps x .. x_end - 1 of the line; x lies in unit `unit` of sequence seq, `step` steps behind the unit's first
+  Line<D> line;
+  line.per_seq = a.kv_used * a.head_tiles;
+  int x, x_end, seq, unit, step;
+  if (a.part_rows) {
+    line.measure(a);
+    if (int(blockIdx.x) >= line.shares) return;
+    x = line.begin(blockIdx.x);
+    x_end = line.begin(blockIdx.x + 1);
+    uint64_t behind;
+    while ((behind = __ballot((line.before + line.upto) * line.per_seq > x)) == 0) line.next64(a);
+    seq = line.base + __builtin_ctzll(behind);
+    const int steps = steps_of<D>(a, line.length(seq)), rest = x - line.steps_before(seq) * line.per_seq;
+    unit = rest / steps;
+    step = rest % steps;
+  } else {
+    seq = int(blockIdx.x) / line.per_seq;
+    unit = int(blockIdx.x) % line.per_seq;
+    line.before = 0;
+    line.load(a, seq & ~63);
+    x = step = 0;
+    x_end = steps_of<D>(a, line.length(seq));
+  }
+
+  for (bool first = true; x < x_end; first = false) {
+  const int len = std::min(line.length(seq), a.max_len), steps = steps_of<D>(a, len), n_steps = std::min(steps - step, x_end - x);
+  const int k_lo = step * kStep<D>, k_hi = std::min(len, k_lo + n_steps * kStep<D>);
+  const Heads hd(a, unit);
+  const int g = hd.g, j0 = hd.j0, j1 = hd.j1;  // (j0 >= j1: a last tile of 16 that a part of a group does not reach)
+
+  bf16x8 qf[KS] = {};  // operand B[k][j]: j = query head (lane % 16), k = 8 consecutive columns
+  if (j0 + lq < j1) {
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) qf[ks] = *reinterpret_cast<const bf16x8*>(a.Q + int64_t(seq) * a.ldq + int64_t(j0 + lq) * D + ks * 32 + lh * 8);
+  }
+
   f32x4 acc[DB];
 #pragma unroll
   for (int db = 0; db < DB; ++db) acc[db] = f32x4{0.f, 0.f, 0.f, 0.f};
   float m_run = -INFINITY, l_run = 0.f;
 
-  // Page numbers of 64 of the wavefront's blocks, one a lane: its tile number i is tile i * kWaves + wave of the piece.  (Bounded by max_len, which
-  // the table holds, not by the length, so that the two are read at the same time.)
+  // Page numbers of 64 of the wavefront's blocks, one a lane: its tile number i is tile i * kWaves + wave of the share's tokens.
   constexpr int PER = 64 / NB;  // tiles per set of page numbers
   const int32_t* const row_of_table = a.table + int64_t(seq) * a.ldt;
   auto pages_from = [&](int i) {
     const int key = k_lo + ((i + lane / NB) * kWaves + wave) * T + (lane % NB) * kBlock;
-    return key < a.max_len ? row_of_table[key >> a.page_log2] : -1;
+    return key < k_hi ? row_of_table[key >> a.page_log2] : -1;
   };
   int32_t pages = pages_from(0);
-  const int n_tiles = std::max(0, (k_hi - k_lo + T - 1) / T);
+  const int n_tiles = j0 < j1 ? std::max(0, (k_hi - k_lo + T - 1) / T) : 0;
   const int mine = (n_tiles - wave + kWaves - 1) / kWaves;  // tiles of this wavefront
   // DMA of one matrix of tile i; number of tokens of each block that count
   auto request = [&](const uint16_t* base, unsigned char* to, int i, int (&valid)[NB]) {
@@ -295,86 +390,106 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2))) v
     result[D + 1] = l_run;
   }
   __syncthreads();
+  const bool whole = n_steps == steps;
+  const int64_t slot = (int64_t(blockIdx.x) * 2 + !first) * 16;
   const int r16 = threadIdx.x >> 4, c0 = (threadIdx.x & 15) * 4, head = j0 + r16;
-  if (head >= j1) return;
-  const float* const res = reinterpret_cast<const float*>(lds) + r16 * ROW;
-  float top = -INFINITY, w[kWaves], sum = 0.f;
+  if (head < j1) {
+    const float* const res = reinterpret_cast<const float*>(lds) + r16 * ROW;
+    float top = -INFINITY, w[kWaves], sum = 0.f;
 #pragma unroll
-  for (int i = 0; i < kWaves; ++i) top = fmaxf(top, res[i * 16 * ROW + D]);
-  const float base = top == -INFINITY ? 0.f : top;
+    for (int i = 0; i < kWaves; ++i) top = fmaxf(top, res[i * 16 * ROW + D]);
+    const float base = top == -INFINITY ? 0.f : top;
 #pragma unroll
-  for (int i = 0; i < kWaves; ++i) {
-    w[i] = fast_exp2(res[i * 16 * ROW + D] - base);
-    sum = fmaf(w[i], res[i * 16 * ROW + D + 1], sum);
-  }
-  const int64_t part = (int64_t(seq) * a.q_cnt + head) * a.pieces + piece;
-  const float inv = sum == 0.f ? 0.f : 1.0f / sum;
+    for (int i = 0; i < kWaves; ++i) {
+      w[i] = fast_exp2(res[i * 16 * ROW + D] - base);
+      sum = fmaf(w[i], res[i * 16 * ROW + D + 1], sum);
+    }
+    const float inv = sum == 0.f ? 0.f : 1.0f / sum;
 #pragma unroll
-  for (int c = c0; c < D; c += 64) {
-    f32x4 o = {0.f, 0.f, 0.f, 0.f};
+    for (int c = c0; c < D; c += 64) {
+      f32x4 o = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-    for (int i = 0; i < kWaves; ++i) o += w[i] * *reinterpret_cast<const f32x4*>(res + i * 16 * ROW + c);
-    if (a.pieces > 1) {
-      *reinterpret_cast<f32x4*>(a.part_rows + part * D + c) = o;
-    } else {
-      ntp_gemm::u16x4 out;
+      for (int i = 0; i < kWaves; ++i) o += w[i] * *reinterpret_cast<const f32x4*>(res + i * 16 * ROW + c);
+      if (!whole) {
+        *reinterpret_cast<f32x4*>(a.part_rows + (slot + r16) * D + c) = o;
+      } else {
+        ntp_gemm::u16x4 out;
 #pragma unroll
-      for (int r = 0; r < 4; ++r) out[r] = ntp_gemm::f32_to_bf16(o[r] * inv);
-      *reinterpret_cast<ntp_gemm::u16x4*>(a.C + int64_t(seq) * a.ldc + int64_t(head) * D + c) = out;
+        for (int r = 0; r < 4; ++r) out[r] = ntp_gemm::f32_to_bf16(o[r] * inv);
+        *reinterpret_cast<ntp_gemm::u16x4*>(a.C + int64_t(seq) * a.ldc + int64_t(head) * D + c) = out;
+      }
+    }
+    if (c0 == 0) {
+      if (!whole) a.part_sums[slot + r16] = float2{top, sum};
+      else if (a.LSE) a.LSE[int64_t(head) * a.n_seq + seq] = (base + log2f(sum)) * 0.6931471805599453f;
     }
   }
-  if (c0 == 0) {
-    if (a.pieces > 1) {
-      a.part_sums[part] = float2{top, sum};
-    } else if (a.LSE) {
-      a.LSE[int64_t(head) * a.n_seq + seq] = (base + log2f(sum)) * 0.6931471805599453f;
-    }
+  x += n_steps;
+  step = 0;
+  if (++unit == line.per_seq) {
+    unit = 0;
+    if (++seq == line.base + 64 && x < x_end) line.next64(a);
+  }
+  __syncthreads();  // the results have been read: the next unit's tiles may come
   }
 }
 
-// The pieces of one (sequence, query head) put together: the threads form the pieces' weights, then D / 4 lanes hold the outputs and 1024 / D groups of them
-// take the pieces in turn (their loads do not depend on each other).
+// The partial results of one (sequence, query head) put together, where its unit does not lie in one share: the threads form the parts' weights, then D / 4 lanes hold
+// the outputs and 1024 / D groups of them take the parts in turn (their loads do not depend on each other).
 template <int D>
 __global__ __launch_bounds__(kThreads) void attn_decode_join_kernel(const DecodeArgs a) {
-  constexpr int L = D / 4, G = kThreads / L;
-  __shared__ float weight[kMaxPieces], wave_max[kWaves], wave_sum[kWaves];
+  constexpr int L = D / 4, G = kThreads / L, N = kMaxShares / kThreads;
+  __shared__ float weight[kMaxShares], wave_max[kWaves], wave_sum[kWaves];
   __shared__ f32x4 rows[G][L];
-  const int row = blockIdx.x, head = row % a.q_cnt, seq = row / a.q_cnt;
-  const int len = std::min(a.lengths[seq], a.max_len);
-  const int used = len > 0 ? (len + a.piece_len - 1) / a.piece_len : 0;
-  const int64_t first = int64_t(row) * a.pieces;
+  const int seq = blockIdx.x / a.q_cnt, head = blockIdx.x % a.q_cnt;
+  // the head's unit and its row in the unit's 16
+  const int kv = (a.q_off + head) / a.group - a.kv_off, unit0 = (kv - a.kv_first) * a.head_tiles;
+  const int in_group = head - Heads(a, unit0).j0, unit = unit0 + in_group / 16, r16 = in_group % 16;
+  Line<D> line;
+  line.per_seq = a.kv_used * a.head_tiles;
+  line.measure(a);
+  while (seq >= line.base + 64) line.next64(a);
+  const int steps = steps_of<D>(a, line.length(seq)), begin = line.steps_before(seq) * line.per_seq + unit * steps;
+  const int w0 = line.share_of(begin), used = line.share_of(begin + steps - 1) - w0 + 1;
+  if (used == 1) return;  // written whole
+  // part p is what share w0 + p left: of the unit that it begins inside, but for a first share that begins before the unit
+  const int late = line.begin(w0) < begin;
+  auto slot = [&](int p) { return (int64_t(w0 + p) * 2 + (p == 0 ? late : 0)) * 16 + r16; };
   const int grp = threadIdx.x / L, c = threadIdx.x % L;
-  float2 ms[kMaxPieces / kThreads];
+  auto part_row = [&](int p) { return *reinterpret_cast<const f32x4*>(a.part_rows + slot(p) * D + c * 4); };
+  f32x4 o = {0.f, 0.f, 0.f, 0.f};
+  if (grp < used) o = part_row(grp);  // (on its way while the weights are formed)
+  float2 ms[N];
   float top = -INFINITY, sum = 0.f;
 #pragma unroll
-  for (int i = 0; i < kMaxPieces / kThreads; ++i) {
+  for (int i = 0; i < N; ++i) {
     const int p = int(threadIdx.x) + i * kThreads;
-    ms[i] = p < used ? a.part_sums[first + p] : float2{-INFINITY, 0.f};
+    ms[i] = p < used ? a.part_sums[slot(p)] : float2{-INFINITY, 0.f};
     top = fmaxf(top, ms[i].x);
   }
   auto wave_all = [](float v, auto f) {
 #pragma unroll
-    for (int x = 1; x < 16; x *= 2) v = f(v, __shfl_xor(v, x));
+    for (int d = 1; d < 16; d *= 2) v = f(v, __shfl_xor(v, d));
     return over_rows(v, f);
   };
-  top = wave_all(top, [](float x, float y) { return fmaxf(x, y); });
+  top = wave_all(top, [](float p, float q) { return fmaxf(p, q); });
   if ((threadIdx.x & 63) == 0) wave_max[threadIdx.x >> 6] = top;
   __syncthreads();
 #pragma unroll
   for (int i = 0; i < kWaves; ++i) top = fmaxf(top, wave_max[i]);
   const float base = top == -INFINITY ? 0.f : top;
 #pragma unroll
-  for (int i = 0; i < kMaxPieces / kThreads; ++i) {
+  for (int i = 0; i < N; ++i) {
     const float w = fast_exp2(ms[i].x - base);
     sum = fmaf(w, ms[i].y, sum);
     weight[threadIdx.x + i * kThreads] = w;
   }
-  sum = wave_all(sum, [](float x, float y) { return x + y; });
+  sum = wave_all(sum, [](float p, float q) { return p + q; });
   if ((threadIdx.x & 63) == 0) wave_sum[threadIdx.x >> 6] = sum;
   __syncthreads();
-  f32x4 o = {0.f, 0.f, 0.f, 0.f};
+  if (grp < used) o *= weight[grp];
 #pragma unroll 8
-  for (int p = grp; p < used; p += G) o += weight[p] * *reinterpret_cast<const f32x4*>(a.part_rows + (first + p) * D + c * 4);
+  for (int p = grp + G; p < used; p += G) o += weight[p] * part_row(p);
   rows[grp][c] = o;
   __syncthreads();
   if (grp > 0) return;
@@ -404,29 +519,25 @@ int check_decode_shape(const ntp_attn_decode_shape_t* s) {
 }
 
 struct DecodeChoice {
-  int32_t kv_first, kv_used, head_tiles, pieces, piece_len;
+  int32_t kv_first, kv_used, head_tiles, shares;  // shares: 0 where workgroup = unit
   int64_t units, ws_bytes;
 };
 
-// How a call is cut.  One workgroup per unit (sequence, KV head, 16 query heads) and piece; pieces are cut so that a launch has some workgroups for
-// every compute unit, but not below one tile for each wavefront.
+// How a call is cut: into two shares per compute unit (a workgroup's tiles take 64 KB of the LDS), but no more than there can be steps; not at all where no unit
+// can have more than one step, or more workgroups than that would have nothing to do.
 DecodeChoice choose_decode(const ntp_handle* h, int64_t ws_bytes, const ntp_attn_decode_shape_t* s) {
   DecodeChoice c{};
-  c.pieces = 1;
-  c.piece_len = std::max(s->max_len, 1);
   if (s->q_cnt == 0 || s->n_seq == 0) return c;
   c.kv_first = s->q_off / s->group - s->kv_off;
   c.kv_used = (s->q_off + s->q_cnt - 1) / s->group - s->kv_off - c.kv_first + 1;
   c.head_tiles = (std::min(s->group, s->q_cnt) + 15) / 16;
   c.units = int64_t(c.kv_used) * c.head_tiles * s->n_seq;
-  const int64_t step = kWaves * (kTileBytes / (2 * s->head_dim));
-  const int64_t want = std::max<int64_t>(1, 16 * int64_t(h->compute_units) / c.units);
-  const int64_t per = std::max<int64_t>((s->max_len + std::min<int64_t>(want, kMaxPieces) - 1) / std::min<int64_t>(want, kMaxPieces), step);
-  const int64_t len = (per + step - 1) / step * step, pieces = (s->max_len + len - 1) / len;
-  const int64_t bytes = int64_t(s->n_seq) * s->q_cnt * pieces * (s->head_dim + 2) * 4;
-  if (pieces > 1 && bytes <= ws_bytes && pieces * c.units <= 0x7fffffffll) {
-    c.pieces = int32_t(pieces);
-    c.piece_len = int32_t(len);
+  const int64_t step = s->head_dim == 128 ? kStep<128> : kStep<64>, steps = std::max<int64_t>((s->max_len + step - 1) / step, 1);
+  if (steps == 1 || steps * c.units > 0x7fffffffll) return c;
+  const int64_t shares = std::min<int64_t>(std::min(2 * int64_t(h->compute_units), steps * c.units), kMaxShares);
+  const int64_t bytes = shares * 2 * 16 * (s->head_dim + 2) * 4;
+  if (bytes <= ws_bytes) {
+    c.shares = int32_t(shares);
     c.ws_bytes = bytes;
   }
   return c;
@@ -457,23 +568,23 @@ extern "C" int ntp_attn_decode_shard(ntp_handle_t* h, const ntp_attn_decode_shap
   DecodeArgs a{};
   a.Q = static_cast<const uint16_t*>(Q), a.K = static_cast<const uint16_t*>(cache->K), a.V = static_cast<const uint16_t*>(cache->V);
   a.table = block_table, a.lengths = lengths, a.C = static_cast<uint16_t*>(C), a.LSE = LSE;
-  if (c.pieces > 1) {
+  if (c.shares > 0) {
     a.part_rows = static_cast<float*>(h->workspace);
-    a.part_sums = reinterpret_cast<float2*>(a.part_rows + int64_t(s->n_seq) * s->q_cnt * c.pieces * s->head_dim);
+    a.part_sums = reinterpret_cast<float2*>(a.part_rows + int64_t(c.shares) * 2 * 16 * s->head_dim);
   }
   a.ldq = ldq, a.ldc = ldc, a.ldt = ldt, a.page_stride = cache->page_stride, a.n_pages = cache->n_pages;
   a.n_seq = s->n_seq, a.max_len = s->max_len, a.q_cnt = s->q_cnt, a.q_off = s->q_off, a.kv_off = s->kv_off, a.group = s->group;
   a.page_size = cache->page_size, a.page_log2 = ntp::log2_of(cache->page_size);
-  a.kv_first = c.kv_first, a.kv_used = c.kv_used, a.head_tiles = c.head_tiles, a.pieces = c.pieces, a.piece_len = c.piece_len;
+  a.kv_first = c.kv_first, a.kv_used = c.kv_used, a.head_tiles = c.head_tiles, a.shares = c.shares;
   a.scale_log2 = float(1.4426950408889634 / std::sqrt(double(s->head_dim)));
   hipStream_t hs = static_cast<hipStream_t>(stream);
   if (ntp::timing_on(h))
-    ntp::timing_begin(h, stream, c.pieces > 1 ? "attn_decode_cut" : "attn_decode", 4.0 * s->n_seq * double(s->max_len) * s->head_dim * s->q_cnt, 0.0);
-  const dim3 grid(uint32_t(c.units * c.pieces)), joins(uint32_t(int64_t(s->n_seq) * s->q_cnt));
+    ntp::timing_begin(h, stream, c.shares > 0 ? "attn_decode_cut" : "attn_decode", 4.0 * s->n_seq * double(s->max_len) * s->head_dim * s->q_cnt, 0.0);
+  const dim3 grid(uint32_t(c.shares > 0 ? c.shares : c.units)), joins(uint32_t(int64_t(s->n_seq) * s->q_cnt));
   if (s->head_dim == 128) hipLaunchKernelGGL(attn_decode_kernel<128>, grid, dim3(kThreads), 0, hs, a);
   else hipLaunchKernelGGL(attn_decode_kernel<64>, grid, dim3(kThreads), 0, hs, a);
   bool ok = hipGetLastError() == hipSuccess;
-  if (ok && c.pieces > 1) {
+  if (ok && c.shares > 0) {
     if (s->head_dim == 128) hipLaunchKernelGGL(attn_decode_join_kernel<128>, joins, dim3(kThreads), 0, hs, a);
     else hipLaunchKernelGGL(attn_decode_join_kernel<64>, joins, dim3(kThreads), 0, hs, a);
     ok = hipGetLastError() == hipSuccess;

@@ -116,6 +116,18 @@ def test_lengths_behind_max_len_are_cut(d, workspace):
     c.check(*c.run(workspace))
 
 
+@pytest.mark.parametrize("lengths", [[5, 0, 300, 1000], [129], [0], [40000, 1, 128, 256, 257] + [7] * 300])
+@pytest.mark.parametrize("d", [64, 128])
+def test_lengths_far_below_max_len(d, lengths):
+    """As in a captured graph: the launch is sized for max_len, and gives what it gives for any other max_len that does not cut them."""
+    c = Case(lengths, 5, 2, d, 64, 1, 0, 4, max_len=60000)
+    C, LSE = c.run(True)
+    c.check(C, LSE)
+    c.shape.max_len = max(1, *lengths)
+    C1, LSE1 = c.run(False)
+    c.check(C1, LSE1)
+
+
 @pytest.mark.parametrize("workspace", [False, True], ids=["whole", "cut"])
 def test_entries_that_name_no_page_are_left_out(workspace):
     c = Case([500, 40, 33, 2000], 6, 3, 128, 16, 0, 0, 2, seed=3)
