@@ -60,26 +60,31 @@ __device__ __forceinline__ void unpack8(u32x4 r, float (&v)[8]) {
     v[2 * i + 1] = bf_hi(r[i]);
   }
 }
-__device__ __forceinline__ u32x4 raw8(const uint16_t* p) { return *reinterpret_cast<const u32x4*>(p); }
-__device__ __forceinline__ void load8(const uint16_t* p, float (&v)[8]) { unpack8(raw8(p), v); }
+// Rows of bf16 go past the caches (NT: non-temporal) where a thread has more than one chunk: large launches, whose matrices no cache holds until they are used again.
+// (8192 x 16384 forward 225 -> 202 us, backward 456 -> 376 us.  Not fp32 rows: a thread's 32 bytes come by two instructions that each take half of every
+// cache line, which would then be fetched twice, 4099 x 6144 backward 113 -> 117 us.)
+template <bool NT = false>
+__device__ __forceinline__ void load8(const uint16_t* p, float (&v)[8]) {
+  const u32x4* q = reinterpret_cast<const u32x4*>(p);
+  unpack8(NT ? __builtin_nontemporal_load(q) : *q, v);
+}
+template <bool NT = false>
 __device__ __forceinline__ void store8(uint16_t* p, const float (&v)[8]) {
   u32x4 r;
 #pragma unroll
   for (int i = 0; i < 4; ++i) r[i] = bf_pack(v[2 * i], v[2 * i + 1]);
-  *reinterpret_cast<u32x4*>(p) = r;
+  if constexpr (NT) __builtin_nontemporal_store(r, reinterpret_cast<u32x4*>(p));
+  else *reinterpret_cast<u32x4*>(p) = r;
 }
 // Eight elements of the residual stream, bf16 or fp32, as they lie in memory.
 template <bool F32>
 struct Raw {
   u32x4 w[F32 ? 2 : 1];
+  template <bool NT>
   __device__ __forceinline__ void load(const void* p, int64_t at) {
     const u32x4* q = reinterpret_cast<const u32x4*>(static_cast<const char*>(p) + at * (F32 ? 4 : 2));
-    w[0] = q[0];
+    w[0] = NT && !F32 ? __builtin_nontemporal_load(q) : q[0];
     if constexpr (F32) w[1] = q[1];
-  }
-  __device__ __forceinline__ void zero() {
-    w[0] = u32x4{0, 0, 0, 0};
-    if constexpr (F32) w[1] = w[0];
   }
   __device__ __forceinline__ void get(float (&v)[8]) const {
     if constexpr (F32) {
@@ -94,14 +99,14 @@ struct Raw {
     }
   }
 };
-template <bool F32>
+template <bool F32, bool NT>
 __device__ __forceinline__ void store8x(void* p, int64_t at, const float (&v)[8]) {
   if constexpr (F32) {
     f32x4* q = reinterpret_cast<f32x4*>(static_cast<float*>(p) + at);
     q[0] = f32x4{v[0], v[1], v[2], v[3]};
     q[1] = f32x4{v[4], v[5], v[6], v[7]};
   } else {
-    store8(static_cast<uint16_t*>(p) + at, v);
+    store8<NT>(static_cast<uint16_t*>(p) + at, v);
   }
 }
 
@@ -194,9 +199,9 @@ __global__ __launch_bounds__(kMaxThreads) void block_norm_fwd_kernel(const NormA
     for (int i = 0; i < 8; ++i) x[v][i] = z[v][i] = 0.f;
     if (on && c < a.H) {
       Raw<XF32> r;
-      r.load(a.X, row * a.ldx + c);
+      r.template load<(V > 1)>(a.X, row * a.ldx + c);
       r.get(x[v]);
-      if (a.Z) load8(a.Z + row * a.ldz + c, z[v]);
+      if (a.Z) load8<(V > 1)>(a.Z + row * a.ldz + c, z[v]);
     }
   }
   if (a.Z) {
@@ -231,7 +236,7 @@ __global__ __launch_bounds__(kMaxThreads) void block_norm_fwd_kernel(const NormA
         }
 #pragma unroll
         for (int i = 0; i < 8; ++i) x[v][i] = fmaf(a.a, x[v][i], a.b * z[v][i]);
-        if (a.Xout) store8x<XF32>(a.Xout, row * a.ldxo + c, x[v]);
+        if (a.Xout) store8x<XF32, (V > 1)>(a.Xout, row * a.ldxo + c, x[v]);
       }
     }
   }
@@ -251,7 +256,7 @@ __global__ __launch_bounds__(kMaxThreads) void block_norm_fwd_kernel(const NormA
         if (a.nb) load8(a.nb + c, b);
 #pragma unroll
         for (int i = 0; i < 8; ++i) y[i] = fmaf((x[v][i] - mean) * rstd, g[i], b[i]);
-        store8(a.Y + row * a.ldy + c, y);
+        store8<(V > 1)>(a.Y + row * a.ldy + c, y);
       }
     }
   }
@@ -267,20 +272,26 @@ __device__ constexpr int kSumOf[3][kVectors] = {{3, 4, -1, -1, -1}, {0, 2, 3, -1
 __device__ __forceinline__ __amdgpu_buffer_rsrc_t row_view(const void* base, int64_t at, int elem, int columns) {
   return __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(static_cast<const char*>(base) + at * elem), 0, columns * elem, 0x00020000);
 }
-__device__ __forceinline__ u32x4 load_16(__amdgpu_buffer_rsrc_t rs, uint32_t off) { return __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(rs, off, 0, 0)); }
-__device__ __forceinline__ void store_16(__amdgpu_buffer_rsrc_t rs, uint32_t off, u32x4 v) { __builtin_amdgcn_raw_buffer_store_b128(v, rs, off, 0, 0); }
+template <bool NT = false>
+__device__ __forceinline__ u32x4 load_16(__amdgpu_buffer_rsrc_t rs, uint32_t off) {
+  return __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(rs, off, 0, NT ? 2 : 0));
+}
+template <bool NT = false>
+__device__ __forceinline__ void store_16(__amdgpu_buffer_rsrc_t rs, uint32_t off, u32x4 v) {
+  __builtin_amdgcn_raw_buffer_store_b128(v, rs, off, 0, NT ? 2 : 0);
+}
 __device__ __forceinline__ u32x4 pack8(const float (&v)[8]) {
   u32x4 r;
 #pragma unroll
   for (int i = 0; i < 4; ++i) r[i] = bf_pack(v[2 * i], v[2 * i + 1]);
   return r;
 }
-template <bool F32>
+template <bool F32, bool NT>
 __device__ __forceinline__ void load_raw(Raw<F32>& r, __amdgpu_buffer_rsrc_t rs, int c) {
-  r.w[0] = load_16(rs, uint32_t(c) * (F32 ? 4 : 2));
+  r.w[0] = load_16<NT && !F32>(rs, uint32_t(c) * (F32 ? 4 : 2));
   if constexpr (F32) r.w[1] = load_16(rs, uint32_t(c) * 4 + 16);
 }
-template <bool F32>
+template <bool F32, bool NT>
 __device__ __forceinline__ void store_raw(__amdgpu_buffer_rsrc_t rs, int c, const float (&v)[8]) {
   if constexpr (F32) {
     u32x4 lo, hi;
@@ -292,7 +303,7 @@ __device__ __forceinline__ void store_raw(__amdgpu_buffer_rsrc_t rs, int c, cons
     store_16(rs, uint32_t(c) * 4, lo);
     store_16(rs, uint32_t(c) * 4 + 16, hi);
   } else {
-    store_16(rs, uint32_t(c) * 2, pack8(v));
+    store_16<NT>(rs, uint32_t(c) * 2, pack8(v));
   }
 }
 
@@ -303,6 +314,7 @@ __device__ __forceinline__ void bwd_body(const NormArgs& a) {
   constexpr bool BRANCH = KIND > 0, BIAS = KIND == 2 || KIND == 0;
   constexpr int PG = 0, PB = 1, GT = KIND == 1 ? 1 : 2, NG = KIND == 0 ? 0 : KIND == 1 ? 2 : 3, NB = KIND == 0 ? 1 : 4;
   constexpr int XB = XF32 ? 4 : 2;
+  constexpr bool NT = V > 1;
   __shared__ float slots[2][kMaxWaves][2];
   __shared__ float rows_lds[LONG ? 1 : kBwdThreads][8];
   extern __shared__ __attribute__((aligned(16))) u32x4 vectors[];  // [4][V * T] chunks: gn, gp, gate, bp
@@ -336,9 +348,9 @@ __device__ __forceinline__ void bwd_body(const NormArgs& a) {
 #pragma unroll
     for (int v = 0; v < V; ++v) {
       const int c = (tid + (v << a.t_log2)) * 8;
-      load_raw<XF32>(rd[v], vd, c);
-      ry[v] = load_16(vy, uint32_t(c) * 2);
-      load_raw<XF32>(rx[v], vx, c);
+      load_raw<XF32, NT>(rd[v], vd, c);
+      ry[v] = load_16<NT>(vy, uint32_t(c) * 2);
+      load_raw<XF32, NT>(rx[v], vx, c);
     }
   };
   if (row0 < row1) load_row(row0 + lane_row);  // (without rows nothing may be read)
@@ -355,8 +367,8 @@ __device__ __forceinline__ void bwd_body(const NormArgs& a) {
 #pragma unroll
       for (int v = 0; v < V; ++v) {
         const uint32_t off = uint32_t(tid + (v << a.t_log2)) * 16;
-        rz[v] = load_16(vz, off);
-        if (a.gate_kind == NTP_GATE_TOKEN) rg[v] = load_16(vg, off);
+        rz[v] = load_16<NT>(vz, off);
+        if (a.gate_kind == NTP_GATE_TOKEN) rg[v] = load_16<NT>(vg, off);
       }
     }
 #pragma unroll
@@ -401,11 +413,11 @@ __device__ __forceinline__ void bwd_body(const NormArgs& a) {
       float o[8];
 #pragma unroll
       for (int i = 0; i < 8; ++i) o[i] = a.a * G[v][i];
-      store_raw<XF32>(vdx, c, o);
+      store_raw<XF32, NT>(vdx, c, o);
       if (!BRANCH && a.Y) {
 #pragma unroll
         for (int i = 0; i < 8; ++i) o[i] = a.b * G[v][i];
-        store_16(vdz, uint32_t(c) * 2, pack8(o));
+        store_16<NT>(vdz, uint32_t(c) * 2, pack8(o));
       }
       if constexpr (BRANCH) {
         float z[8], p[8], q[8] = {};
@@ -428,7 +440,7 @@ __device__ __forceinline__ void bwd_body(const NormArgs& a) {
             acc[GT][v][i] += o[i];
             G[v][i] *= g[i];  // dr
           }
-          if (a.dgate_rows) store_16(vdg, uint32_t(c) * 2, pack8(o));
+          if (a.dgate_rows) store_16<NT>(vdg, uint32_t(c) * 2, pack8(o));
         }
         if (a.pg) {
 #pragma unroll
@@ -455,7 +467,7 @@ __device__ __forceinline__ void bwd_body(const NormArgs& a) {
         unpack8(rz[v], z);
 #pragma unroll
         for (int i = 0; i < 8; ++i) o[i] = (G[v][i] - fmaf((z[i] - st[0]) * st[1], m1, m0)) * st[1];
-        store_16(vdz, uint32_t(tid + (v << a.t_log2)) * 16, pack8(o));
+        store_16<NT>(vdz, uint32_t(tid + (v << a.t_log2)) * 16, pack8(o));
       }
     }
   }
