@@ -337,23 +337,28 @@ __device__ __forceinline__ void bwd_body(const NormArgs& a) {
   Raw<XF32> rx[V], rd[V];
   u32x4 ry[V];
   float st[4] = {0.f, 1.f, 0.f, 1.f}, nst[4] = {0.f, 1.f, 0.f, 1.f};
-  auto load_row = [&](int64_t row) {
+  __amdgpu_buffer_rsrc_t vd, vy, vx;
+  auto next_row = [&](int64_t row) {
     const bool there = row < row1;
     const int width = there ? a.H : 0;
     row = there ? row : 0;
     if (BRANCH && a.pg) nst[0] = a.Stats[row], nst[1] = a.Stats[a.M + row];
     if (a.ng) nst[2] = a.Stats[2 * a.M + row], nst[3] = a.Stats[3 * a.M + row];
-    const __amdgpu_buffer_rsrc_t vd = row_view(a.dXout, row * a.lddxo, XB, a.dXout ? width : 0), vy = row_view(a.dY, row * a.lddy, 2, a.ng ? width : 0),
-                                 vx = row_view(a.X, row * a.ldx, XB, a.ng ? width : 0);
-#pragma unroll
-    for (int v = 0; v < V; ++v) {
-      const int c = (tid + (v << a.t_log2)) * 8;
-      load_raw<XF32, NT>(rd[v], vd, c);
-      ry[v] = load_16<NT>(vy, uint32_t(c) * 2);
-      load_raw<XF32, NT>(rx[v], vx, c);
-    }
+    vd = row_view(a.dXout, row * a.lddxo, XB, a.dXout ? width : 0);
+    vy = row_view(a.dY, row * a.lddy, 2, a.ng ? width : 0);
+    vx = row_view(a.X, row * a.ldx, XB, a.ng ? width : 0);
   };
-  if (row0 < row1) load_row(row0 + lane_row);  // (without rows nothing may be read)
+  auto load_chunk = [&](int v) {
+    const int c = (tid + (v << a.t_log2)) * 8;
+    load_raw<XF32, NT>(rd[v], vd, c);
+    ry[v] = load_16<NT>(vy, uint32_t(c) * 2);
+    load_raw<XF32, NT>(rx[v], vx, c);
+  };
+  if (row0 < row1) {  // (without rows nothing may be read)
+    next_row(row0 + lane_row);
+#pragma unroll
+    for (int v = 0; v < V; ++v) load_chunk(v);
+  }
   for (int64_t base = row0; base < row1; base += n_rows) {
     const int64_t row = base + lane_row;
     const int width = row < row1 ? a.H : 0;
@@ -371,8 +376,9 @@ __device__ __forceinline__ void bwd_body(const NormArgs& a) {
         if (a.gate_kind == NTP_GATE_TOKEN) rg[v] = load_16<NT>(vg, off);
       }
     }
+    next_row(row + n_rows);
 #pragma unroll
-    for (int v = 0; v < V; ++v) {
+    for (int v = 0; v < V; ++v) {  // a chunk's loads of the next row go out as soon as it is taken from its registers
       rd[v].get(G[v]);
       hx[v] = rx[v];
       if (a.ng) {
@@ -391,8 +397,8 @@ __device__ __forceinline__ void bwd_body(const NormArgs& a) {
           G[v][i] = fmaf(u, st[3], G[v][i]);
         }
       }
+      load_chunk(v);
     }
-    load_row(row + n_rows);
     if (a.ng) {
       row_sum<2>(a.t_log2, s, slots, turn);
       const float m0 = a.layer ? s[0] * a.inv_h * st[3] : 0.f, m1 = s[1] * a.inv_h * st[3];
