@@ -459,25 +459,29 @@ def ntp_attn_core_shard_bwd(shape: AttnCoreShape, QKV, C_, dC, LSE, Delta, dQKV,
                                          _stream()), "ntp_attn_core_shard_bwd")
 
 
-def _vec(t, dtype, n=None):
-    """Device pointer of a contiguous device tensor (of n elements), or None."""
+def _vec(t, dtype, n):
+    """Device pointer of a contiguous device tensor of n elements, or None."""
     if t is None:
         return None
     if t.dtype is not dtype:
         raise TypeError(f"expected {dtype}, got {t.dtype}")
     if not t.is_cuda or not t.is_contiguous():
         raise ValueError("expected a contiguous device tensor")
-    if n is not None and t.numel() != n:
+    if t.numel() != n:
         raise ValueError(f"expected {n} elements, got {t.numel()}")
     return t.data_ptr()
 
 
 def _rows(t, dtype, m, n, name):
     """_mat of a tensor that must have m rows of n elements."""
-    if t is not None and tuple(t.size()) != (m, n):
-        raise ValueError(f"{name}: expected {m} x {n}, got {tuple(t.size())}")
-    p, ld = _mat(t, dtype)
-    return p, max(ld, n) if t is not None and m <= 1 else ld  # (the stride of a single row does not count)
+    if t is None:
+        return None, 0
+    stride = t.stride()
+    if t.size() != (m, n) or t.dtype is not dtype or not t.is_cuda or stride[1] != 1:  # (one test for what is nearly always right)
+        if tuple(t.size()) != (m, n):
+            raise ValueError(f"{name}: expected {m} x {n}, got {tuple(t.size())}")
+        _mat(t, dtype)
+    return t.data_ptr(), stride[0] if m > 1 else max(stride[0], n)  # (the stride of a single row does not count)
 
 
 def block_norm_shape(M, H, norm: int = NTP_NORM_RMS, gate: int = NTP_GATE_NONE, residual_fp32: bool = False, eps: float = 1e-5,
@@ -499,8 +503,8 @@ def ntp_block_norm_fwd(shape: BlockNormShape, X, Z=None, Xout=None, Y=None, Stat
     torch = _torch or _bind_torch()
     bf, rt, M, H = torch.bfloat16, torch.float32 if shape.residual_fp32 else torch.bfloat16, shape.M, shape.H
     w = _norm_weights(shape, torch, post_gamma, post_beta, gate, pre_gamma, pre_beta)
-    args = [*_rows(X, rt, M, H, "X"), *_rows(Z, bf, M, H, "Z"), *_rows(Xout, rt, M, H, "Xout"), *_rows(Y, bf, M, H, "Y")]
-    _check(lib().ntp_block_norm_fwd(_h(handle), C.byref(shape), C.byref(w), *args, _vec(Stats, torch.float32, 4 * M), _stream()), "ntp_block_norm_fwd")
+    _check(lib().ntp_block_norm_fwd(_h(handle), C.byref(shape), C.byref(w), *_rows(X, rt, M, H, "X"), *_rows(Z, bf, M, H, "Z"), *_rows(Xout, rt, M, H, "Xout"),
+                                    *_rows(Y, bf, M, H, "Y"), _vec(Stats, torch.float32, 4 * M), _stream()), "ntp_block_norm_fwd")
 
 
 def ntp_block_norm_bwd(shape: BlockNormShape, dXout, dY, Xout, Z, Stats, dX, dZ, post_gamma=None, post_beta=None, gate=None, pre_gamma=None,
@@ -552,9 +556,10 @@ def ntp_kv_append_shard(shape: KvAppendShape, cache: KvCache | None, QKV, positi
     bf, M, d = torch.bfloat16, shape.M, shape.head_dim
     if cache is not None:
         _fits_cache(cache, shape)
-    args = [*_rows(QKV, bf, M, (shape.q_cnt + 2 * shape.kv_cnt) * d, "QKV"), _vec(positions, torch.int32, M), _vec(slots, torch.int64, M),
-            _vec(inv_freq, torch.float64, shape.rotary_dim // 2), *_rows(Qout, bf, M, shape.q_cnt * d, "Qout"), *_rows(Kout, bf, M, shape.kv_cnt * d, "Kout")]
-    _check(lib().ntp_kv_append_shard(_h(handle), C.byref(shape), C.byref(cache) if cache is not None else None, *args, _stream()), "ntp_kv_append_shard")
+    wq, wk = shape.q_cnt * d, shape.kv_cnt * d
+    _check(lib().ntp_kv_append_shard(_h(handle), C.byref(shape), C.byref(cache) if cache is not None else None, *_rows(QKV, bf, M, wq + 2 * wk, "QKV"),
+                                     _vec(positions, torch.int32, M), _vec(slots, torch.int64, M), _vec(inv_freq, torch.float64, shape.rotary_dim // 2),
+                                     *_rows(Qout, bf, M, wq, "Qout"), *_rows(Kout, bf, M, wk, "Kout"), _stream()), "ntp_kv_append_shard")
 
 
 def attn_decode_shape(n_seq, max_len, plan: dict, group: int) -> AttnDecodeShape:
