@@ -343,14 +343,18 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2))) v
     const float m_new = fmaxf(m_run, mx), m_use = m_new == -INFINITY ? 0.f : m_new;  // (no score above -inf so far: weights of 0)
     const float alpha = fast_exp2(m_run - m_use);
     float ls = 0.f;
-    bf16x8 pf[NB / 2];  // weights as operand B of the second product, per 32 tokens (rounded to bf16 for it; their sum is not)
+    // weights as operand B of the second product, per 32 tokens: bf16, and what that leaves, in a product of its own (no rounding of the weights is left in
+    // the result, and the matrix pipe has the room)
+    bf16x8 pf[NB / 2], pr[NB / 2];
 #pragma unroll
     for (int b = 0; b < NB; ++b)
 #pragma unroll
       for (int r = 0; r < 4; ++r) {
         const float p = fast_exp2(fmaf(st[b][r], a.scale_log2, -m_use));
         ls += p;
-        pf[b / 2][(b & 1) * 4 + r] = static_cast<__bf16>(p);
+        const __bf16 top = static_cast<__bf16>(p);
+        pf[b / 2][(b & 1) * 4 + r] = top;
+        pr[b / 2][(b & 1) * 4 + r] = static_cast<__bf16>(p - static_cast<float>(top));
       }
     l_run = l_run * alpha + ls;  // of this lane's tokens; the four lane groups are added at the end
     m_run = m_new;
@@ -374,6 +378,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2))) v
         const u32x2 lo = vf[db * NB + s2 * 2], hi = vf[db * NB + s2 * 2 + 1];
         const u32x4 both = {lo[0], lo[1], hi[0], hi[1]};
         acc[db] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, both), pf[s2], acc[db], 0, 0, 0);
+        acc[db] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, both), pr[s2], acc[db], 0, 0, 0);
       }
 #pragma unroll
     for (int b = 0; b < NB; ++b) valid[b] = next[b];
