@@ -150,9 +150,15 @@ __device__ __forceinline__ void row_sum(int t_log2, float (&v)[N], float (*slots
   __syncthreads();
 #pragma unroll
   for (int n = 0; n < N; ++n) v[n] = 0.f;
-  for (int w = 0; w < waves; ++w)
-#pragma unroll
-    for (int n = 0; n < N; ++n) v[n] += slots[turn][first + w][n];
+  for (int w = 0; w < waves; w += 2) {  // (two wavefronts a read)
+    const f32x4 s = *reinterpret_cast<const f32x4*>(&slots[turn][first + w][0]);
+    v[0] += s[0];
+    v[0] += s[2];
+    if constexpr (N > 1) {
+      v[1] += s[1];
+      v[1] += s[3];
+    }
+  }
   turn ^= 1;
 }
 
@@ -186,7 +192,7 @@ __device__ __forceinline__ void row_stats(const NormArgs& a, int tid, const floa
 
 template <int V, bool XF32>
 __global__ __launch_bounds__(kMaxThreads) void block_norm_fwd_kernel(const NormArgs a) {
-  __shared__ float slots[2][kMaxWaves][2];
+  __shared__ __attribute__((aligned(16))) float slots[2][kMaxWaves][2];
   int turn = 0;
   const int tid = threadIdx.x & ((1 << a.t_log2) - 1);
   const int64_t row = (int64_t(blockIdx.x) * blockDim.x + threadIdx.x) >> a.t_log2;
@@ -315,7 +321,7 @@ __device__ __forceinline__ void bwd_body(const NormArgs& a) {
   constexpr int PG = 0, PB = 1, GT = KIND == 1 ? 1 : 2, NG = KIND == 0 ? 0 : KIND == 1 ? 2 : 3, NB = KIND == 0 ? 1 : 4;
   constexpr int XB = XF32 ? 4 : 2;
   constexpr bool NT = V > 1;
-  __shared__ float slots[2][kMaxWaves][2];
+  __shared__ __attribute__((aligned(16))) float slots[2][kMaxWaves][2];
   __shared__ float rows_lds[LONG ? 1 : kBwdThreads][8];
   extern __shared__ __attribute__((aligned(16))) u32x4 vectors[];  // [4][V * T] chunks: gn, gp, gate, bp
   int turn = 0;
@@ -333,7 +339,7 @@ __device__ __forceinline__ void bwd_body(const NormArgs& a) {
     __syncthreads();
   }
   float acc[kSums[KIND]][V][8] = {};
-  const int64_t row0 = a.M * blockIdx.x / gridDim.x, row1 = a.M * (blockIdx.x + 1) / gridDim.x;
+  const int64_t row0 = int64_t(blockIdx.x) * n_rows, row1 = a.M, stride = int64_t(gridDim.x) * n_rows;
   Raw<XF32> rx[V], rd[V];
   u32x4 ry[V];
   float st[4] = {0.f, 1.f, 0.f, 1.f}, nst[4] = {0.f, 1.f, 0.f, 1.f};
@@ -359,7 +365,7 @@ __device__ __forceinline__ void bwd_body(const NormArgs& a) {
 #pragma unroll
     for (int v = 0; v < V; ++v) load_chunk(v);
   }
-  for (int64_t base = row0; base < row1; base += n_rows) {
+  for (int64_t base = row0; base < row1; base += stride) {
     const int64_t row = base + lane_row;
     const int width = row < row1 ? a.H : 0;
     float G[V][8], s[2] = {0.f, 0.f};
@@ -376,7 +382,7 @@ __device__ __forceinline__ void bwd_body(const NormArgs& a) {
         if (a.gate_kind == NTP_GATE_TOKEN) rg[v] = load_16<NT>(vg, off);
       }
     }
-    next_row(row + n_rows);
+    next_row(row + stride);
 #pragma unroll
     for (int v = 0; v < V; ++v) {  // a chunk's loads of the next row go out as soon as it is taken from its registers
       rd[v].get(G[v]);
