@@ -21,6 +21,7 @@
 #include <algorithm>
 #include <cmath>
 #include <cstdint>
+#include <type_traits>
 
 #include "ntp_gemm_kernels.h"
 #include "ntp_gemm_ring.h"
@@ -52,8 +53,8 @@ struct DecodeArgs {
   // maximum (log2 units) and sum, and the D unnormalised outputs.  NULL: workgroup = unit
   float2* part_sums;
   float* part_rows;
-  int64_t ldq, ldc, ldt, page_stride, n_pages;
-  int32_t n_seq, max_len, q_cnt, q_off, kv_off, group, page_size, page_log2;
+  int64_t ldq, ldc, ldt, page_stride;
+  int32_t n_pages, n_seq, max_len, q_cnt, q_off, kv_off, group, page_size, page_log2;
   int32_t kv_first, kv_used, head_tiles;  // local KV heads that are read; 16-head tiles of a KV head's query heads
   int32_t shares;
   float scale_log2;                       // log2(e) / sqrt(d)
@@ -87,6 +88,15 @@ __device__ __forceinline__ void dma_16(__amdgpu_buffer_rsrc_t rs, unsigned char*
 template <int N>
 __device__ __forceinline__ void dma_left() {
   asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory");
+}
+
+__device__ __forceinline__ int uniform(int v) { return __builtin_amdgcn_readfirstlane(v); }
+// What was loaded is there: the compiler's own wait for it stands here and not in a loop, where it would take in the DMA that is in flight.
+template <typename V>
+__device__ __forceinline__ void arrived(V& v) {
+#if defined(__HIP_DEVICE_COMPILE__)
+  asm volatile("" : "+v"(v));
+#endif
 }
 
 template <int OFF>
@@ -259,6 +269,8 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2))) v
     x_end = steps_of<D>(a, line.length(seq));
   }
 
+  // (said to be the same in every lane: the buffer views below are made from them)
+  x = uniform(x), x_end = uniform(x_end), seq = uniform(seq), unit = uniform(unit), step = uniform(step);
   for (bool first = true; x < x_end; first = false) {
   const int len = std::min(line.length(seq), a.max_len), steps = steps_of<D>(a, len), n_steps = std::min(steps - step, x_end - x);
   const int k_lo = step * kStep<D>, k_hi = std::min(len, k_lo + n_steps * kStep<D>);
@@ -284,6 +296,9 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2))) v
     return key < k_hi ? row_of_table[key >> a.page_log2] : -1;
   };
   int32_t pages = pages_from(0);
+#pragma unroll
+  for (int ks = 0; ks < KS; ++ks) arrived(qf[ks]);
+  arrived(pages);
   const int n_tiles = j0 < j1 ? std::max(0, (k_hi - k_lo + T - 1) / T) : 0;
   const int mine = (n_tiles - wave + kWaves - 1) / kWaves;  // tiles of this wavefront
   // DMA of one matrix of tile i; number of tokens of each block that count
@@ -293,7 +308,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2))) v
       const int key = k_lo + (i * kWaves + wave) * T + b * kBlock;
       const int page = __builtin_amdgcn_readlane(pages, (i % PER) * NB + b);
       const bool there = page >= 0 && page < a.n_pages;
-      valid[b] = there ? std::min(std::max(k_hi - key, 0), kBlock) : 0;
+      valid[b] = uniform(there ? std::min(std::max(k_hi - key, 0), kBlock) : 0);
       const int64_t at = there ? int64_t(page) * a.page_stride + (int64_t(g) * a.page_size + (key & (a.page_size - 1))) * D : 0;
       const __amdgpu_buffer_rsrc_t rs = view(base + at, valid[b] * D * 2);
 #pragma unroll
@@ -308,7 +323,8 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2))) v
     request(a.K, sK, 0, valid);
     request(a.V, sV, 0, valid);
   }
-  for (int i = 0; i < mine; ++i) {
+  auto tile = [&](int i, auto last) {
+    constexpr bool MORE = !decltype(last)::value;
     dma_left<IN_FLIGHT>();  // the keys are there
     u32x4 kf[NB * KS];
     unrolled(std::make_integer_sequence<int, NB * KS>{}, [&](auto n) {
@@ -316,9 +332,11 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2))) v
       kf[decltype(n)::value] = lds_b128<blk * BLOCK_BYTES>(row[ks]);
     });
     lds_reads_done(kf);
-    const bool more = i + 1 < mine;
-    if (more) {
-      if ((i + 1) % PER == 0) pages = pages_from(i + 1);
+    if constexpr (MORE) {
+      if ((i + 1) % PER == 0) {
+        pages = pages_from(i + 1);
+        arrived(pages);
+      }
       request(a.K, sK, i + 1, next);
     }
     // scores, transposed: st[b][r] = score of query head lane % 16 with token key0 + b * 16 + lane / 16 * 4 + r
@@ -362,15 +380,14 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2))) v
 #pragma unroll
       for (int db = 0; db < DB; ++db) acc[db] *= alpha;
     }
-    if (more) dma_left<IN_FLIGHT>();
-    else dma_left<0>();  // the values are there
+    dma_left<MORE ? IN_FLIGHT : 0>();  // the values are there
     u32x2 vf[16];  // [(db * NB / 2 + s2) * 2 + half]
     unrolled(std::make_integer_sequence<int, 16>{}, [&](auto n) {
       constexpr int db = decltype(n)::value / NB, q = decltype(n)::value % NB;
       vf[decltype(n)::value] = lds_tr_b64<q * BLOCK_BYTES>(col[db]);
     });
     lds_reads_done(vf);
-    if (more) request(a.V, sV, i + 1, next);
+    if constexpr (MORE) request(a.V, sV, i + 1, next);
 #pragma unroll
     for (int db = 0; db < DB; ++db)
 #pragma unroll
@@ -380,9 +397,13 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2))) v
         acc[db] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, both), pf[s2], acc[db], 0, 0, 0);
         acc[db] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, both), pr[s2], acc[db], 0, 0, 0);
       }
+    if constexpr (MORE) {
 #pragma unroll
-    for (int b = 0; b < NB; ++b) valid[b] = next[b];
-  }
+      for (int b = 0; b < NB; ++b) valid[b] = next[b];
+    }
+  };
+  for (int i = 0; i + 1 < mine; ++i) tile(i, std::false_type{});
+  if (mine > 0) tile(mine - 1, std::true_type{});
 
   // the wavefronts' results, one row per query head
   l_run = over_rows(l_run, [](float x, float y) { return x + y; });
@@ -577,7 +598,7 @@ extern "C" int ntp_attn_decode_shard(ntp_handle_t* h, const ntp_attn_decode_shap
     a.part_rows = static_cast<float*>(h->workspace);
     a.part_sums = reinterpret_cast<float2*>(a.part_rows + int64_t(c.shares) * 2 * 16 * s->head_dim);
   }
-  a.ldq = ldq, a.ldc = ldc, a.ldt = ldt, a.page_stride = cache->page_stride, a.n_pages = cache->n_pages;
+  a.ldq = ldq, a.ldc = ldc, a.ldt = ldt, a.page_stride = cache->page_stride, a.n_pages = int32_t(cache->n_pages);
   a.n_seq = s->n_seq, a.max_len = s->max_len, a.q_cnt = s->q_cnt, a.q_off = s->q_off, a.kv_off = s->kv_off, a.group = s->group;
   a.page_size = cache->page_size, a.page_log2 = ntp::log2_of(cache->page_size);
   a.kv_first = c.kv_first, a.kv_used = c.kv_used, a.head_tiles = c.head_tiles, a.shares = c.shares;
