@@ -317,18 +317,18 @@ __global__ __launch_bounds__(kMaxThreads) void block_norm_fwd_kernel(const NormA
   }
 }
 
-// Which sums over the rows a backward kernel holds, by kind: 0 nothing behind the block (no norm, no gate: Z is not read), 1 anything without
-// betas, 2 anything.  Numbers into NormArgs::sums.
-constexpr int kSums[3] = {2, 3, 5};
-__device__ constexpr int kSumOf[3][kVectors] = {{3, 4, -1, -1, -1}, {0, 2, 3, -1, -1}, {0, 1, 2, 3, 4}};
+// Which sums over the rows a backward kernel holds, by kind: 0 nothing behind the block (no norm, no gate: Z is not read), 1 no gate or one per channel, no
+// betas, 2 the same with betas, 3 a gate per token.  Numbers into NormArgs::sums.
+constexpr int kSums[4] = {2, 3, 5, 4};
+__device__ constexpr int kSumOf[4][kVectors] = {{3, 4, -1, -1, -1}, {0, 2, 3, -1, -1}, {0, 1, 2, 3, 4}, {0, 1, 3, 4, -1}};
 
 // Workgroup = every gridDim.x-th set of blockDim.x / T rows (neighbouring workgroups read neighbouring rows at the same time: contiguous shares lay a power of two
 // apart in memory, 8192 x 12288 212 -> 185 us).  The vectors (gn, gp, the gate per channel, bp) lie in the LDS, for rows of at most
 // kBwdThreads * kMaxV chunks: loads of them from memory would be waited for together with the next row's, which are issued before.
 template <int V, bool XF32, int KIND, bool LONG>
 __device__ __forceinline__ void bwd_body(const NormArgs& a) {
-  constexpr bool BRANCH = KIND > 0, BIAS = KIND == 2 || KIND == 0;
-  constexpr int PG = 0, PB = 1, GT = KIND == 1 ? 1 : 2, NG = KIND == 0 ? 0 : KIND == 1 ? 2 : 3, NB = KIND == 0 ? 1 : 4;
+  constexpr bool BRANCH = KIND > 0, BIAS = KIND != 1, TOKEN = KIND == 3;
+  constexpr int PG = 0, PB = 1, GT = KIND == 1 ? 1 : 2, NG = KIND == 0 ? 0 : KIND == 2 ? 3 : 2, NB = KIND == 0 ? 1 : KIND == 2 ? 4 : 3;
   constexpr int XB = XF32 ? 4 : 2;
   constexpr bool NT = V > 1;
   __shared__ __attribute__((aligned(16))) float slots[2][kMaxWaves][2];
@@ -337,7 +337,7 @@ __device__ __forceinline__ void bwd_body(const NormArgs& a) {
   int turn = 0;
   const int T = 1 << a.t_log2, tid = threadIdx.x & (T - 1), n_rows = blockDim.x >> a.t_log2;
   const int lane_row = __builtin_amdgcn_readfirstlane(threadIdx.x >> a.t_log2);  // (T is a multiple of the wavefront)
-  const uint16_t* const vec_ptr[4] = {a.ng, a.pg, a.gate_kind == NTP_GATE_CHANNEL ? a.gate : nullptr, a.pb};
+  const uint16_t* const vec_ptr[4] = {a.ng, a.pg, TOKEN ? nullptr : a.gate, a.pb};
   auto vec = [&](int which, int v, float (&o)[8]) {
     if constexpr (LONG) unpack8(load_bf<XF32, false>(row_view(vec_ptr[which], 0, 2, a.H), Cols<XF32>(tid, v, a.t_log2)), o);
     else unpack8(vectors[(which * V + v) * T + tid], o);
@@ -368,35 +368,36 @@ __device__ __forceinline__ void bwd_body(const NormArgs& a) {
     const Cols<XF32> c(tid, v, a.t_log2);
     rd[v].template load<NT>(vd, c);
     ry[v] = load_bf<XF32, NT>(vy, c);
-    rx[v].template load<NT>(vx, c);
   };
+  auto load_x = [&](int v) { rx[v].template load<NT>(vx, Cols<XF32>(tid, v, a.t_log2)); };
   if (row0 < row1) {  // (without rows nothing may be read)
     next_row(row0 + lane_row);
 #pragma unroll
-    for (int v = 0; v < V; ++v) load_chunk(v);
+    for (int v = 0; v < V; ++v) {
+      load_chunk(v);
+      load_x(v);
+    }
   }
   for (int64_t base = row0; base < row1; base += stride) {
     const int64_t row = base + lane_row;
     const int width = row < row1 ? a.H : 0;
     float G[V][8], s[2] = {0.f, 0.f};
     u32x4 rz[V], rg[V];
-    Raw<XF32> hx[V];
 #pragma unroll
     for (int i = 0; i < 4; ++i) st[i] = nst[i];
     if constexpr (BRANCH) {
-      const __amdgpu_buffer_rsrc_t vz = row_view(a.Z, row * a.ldz, 2, width), vg = row_view(a.gate, row * a.ldgate, 2, a.gate_kind == NTP_GATE_TOKEN ? width : 0);
+      const __amdgpu_buffer_rsrc_t vz = row_view(a.Z, row * a.ldz, 2, width), vg = row_view(a.gate, row * a.ldgate, 2, TOKEN ? width : 0);
 #pragma unroll
       for (int v = 0; v < V; ++v) {
         const Cols<XF32> c(tid, v, a.t_log2);
         rz[v] = load_bf<XF32, NT>(vz, c);
-        if (a.gate_kind == NTP_GATE_TOKEN) rg[v] = load_bf<XF32, NT>(vg, c);
+        if constexpr (TOKEN) rg[v] = load_bf<XF32, NT>(vg, c);
       }
     }
     next_row(row + stride);
 #pragma unroll
     for (int v = 0; v < V; ++v) {  // a chunk's loads of the next row go out as soon as it is taken from its registers
       rd[v].get(G[v]);
-      hx[v] = rx[v];
       if (a.ng) {
         float dy[8], x[8], g[8];
         unpack8(ry[v], dy);
@@ -421,9 +422,10 @@ __device__ __forceinline__ void bwd_body(const NormArgs& a) {
 #pragma unroll
       for (int v = 0; v < V; ++v) {
         float x[8];
-        hx[v].get(x);
+        rx[v].get(x);
 #pragma unroll
         for (int i = 0; i < 8; ++i) G[v][i] -= fmaf((x[i] - st[2]) * st[3], m1, m0);
+        load_x(v);
       }
     }
     s[0] = s[1] = 0.f;
@@ -451,24 +453,24 @@ __device__ __forceinline__ void bwd_body(const NormArgs& a) {
           z[i] = (z[i] - st[0]) * st[1];  // hat_z, or Z itself
         }
         if (a.pg) vec(1, v, p);
-        if (KIND == 2 && a.pb) vec(3, v, q);
-        if (a.gate_kind != NTP_GATE_NONE) {
+        if (KIND != 1 && a.pb) vec(3, v, q);
+        if (TOKEN || a.gate) {
           float g[8];
-          if (a.gate_kind == NTP_GATE_TOKEN) unpack8(rg[v], g);
+          if constexpr (TOKEN) unpack8(rg[v], g);
           else vec(2, v, g);
 #pragma unroll
           for (int i = 0; i < 8; ++i) {
             o[i] = G[v][i] * fmaf(z[i], p[i], q[i]);
-            acc[GT][v][i] += o[i];
+            if constexpr (!TOKEN) acc[GT][v][i] += o[i];
             G[v][i] *= g[i];  // dr
           }
-          if (a.dgate_rows) store_bf<XF32, NT>(vdg, c, o);
+          if (TOKEN && a.dgate_rows) store_bf<XF32, NT>(vdg, c, o);
         }
         if (a.pg) {
 #pragma unroll
           for (int i = 0; i < 8; ++i) {
             acc[PG][v][i] = fmaf(G[v][i], z[i], acc[PG][v][i]);
-            if constexpr (KIND == 2) acc[PB][v][i] += G[v][i];
+            if constexpr (KIND != 1) acc[PB][v][i] += G[v][i];
             G[v][i] *= p[i];  // v
             s[0] += G[v][i];
             s[1] = fmaf(G[v][i], z[i], s[1]);
@@ -715,6 +717,7 @@ extern "C" int ntp_block_norm_bwd(ntp_handle_t* h, const ntp_block_norm_shape_t*
   by_chunks(norm_chunks(s->H, a.t_log2), [&](auto v) {
     auto by_kind = [&](auto f32) {
       if (!reads_z) launch(v, f32, integral_constant<int, 0>{});
+      else if (token) launch(v, f32, integral_constant<int, 3>{});
       else if (!bias) launch(v, f32, integral_constant<int, 1>{});
       else launch(v, f32, integral_constant<int, 2>{});
     };
