@@ -365,10 +365,9 @@ __device__ __forceinline__ void bwd_body(const NormArgs& a) {
     vx = row_view(a.X, row * a.ldx, XB, a.ng ? width : 0);
   };
   auto load_chunk = [&](int v) {
-    const Cols<XF32> c(tid, v, a.t_log2);
-    rd[v].template load<NT>(vd, c);
-    ry[v] = load_bf<XF32, NT>(vy, c);
+    ry[v] = load_bf<XF32, NT>(vy, Cols<XF32>(tid, v, a.t_log2));
   };
+  auto load_d = [&](int v) { rd[v].template load<NT>(vd, Cols<XF32>(tid, v, a.t_log2)); };
   auto load_x = [&](int v) { rx[v].template load<NT>(vx, Cols<XF32>(tid, v, a.t_log2)); };
   if (row0 < row1) {  // (without rows nothing may be read)
     next_row(row0 + lane_row);
@@ -376,6 +375,7 @@ __device__ __forceinline__ void bwd_body(const NormArgs& a) {
     for (int v = 0; v < V; ++v) {
       load_chunk(v);
       load_x(v);
+      load_d(v);
     }
   }
   for (int64_t base = row0; base < row1; base += stride) {
@@ -415,6 +415,7 @@ __device__ __forceinline__ void bwd_body(const NormArgs& a) {
         }
       }
       load_chunk(v);
+      if constexpr (!BRANCH) load_d(v);
     }
     if (a.ng) {
       row_sum<2>(a.t_log2, s, slots, turn);
@@ -488,6 +489,7 @@ __device__ __forceinline__ void bwd_body(const NormArgs& a) {
 #pragma unroll
       for (int v = 0; v < V; ++v) {
         float z[8], o[8];
+        load_d(v);
         unpack8(rz[v], z);
 #pragma unroll
         for (int i = 0; i < 8; ++i) o[i] = (G[v][i] - fmaf((z[i] - st[0]) * st[1], m1, m0)) * st[1];
