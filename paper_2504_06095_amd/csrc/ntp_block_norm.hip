@@ -369,7 +369,9 @@ __device__ __forceinline__ void bwd_body(const NormArgs& a) {
   };
   auto load_d = [&](int v) { rd[v].template load<NT>(vd, Cols<XF32>(tid, v, a.t_log2)); };
   auto load_x = [&](int v) { rx[v].template load<NT>(vx, Cols<XF32>(tid, v, a.t_log2)); };
-  if (row0 < row1) {  // (without rows nothing may be read)
+  // (four chunks with five sums, with a gate per token or in fp32 leave no registers for the next row: 4096 x 16384 with betas 390 -> 293 us)
+  constexpr bool AHEAD = V < 4 || (KIND < 2 && !XF32);
+  if (AHEAD && row0 < row1) {  // (without rows nothing may be read)
     next_row(row0 + lane_row);
 #pragma unroll
     for (int v = 0; v < V; ++v) {
@@ -383,6 +385,15 @@ __device__ __forceinline__ void bwd_body(const NormArgs& a) {
     const int width = row < row1 ? a.H : 0;
     float G[V][8], s[2] = {0.f, 0.f};
     u32x4 rz[V], rg[V];
+    if constexpr (!AHEAD) {
+      next_row(row);
+#pragma unroll
+      for (int v = 0; v < V; ++v) {
+        load_chunk(v);
+        load_x(v);
+        load_d(v);
+      }
+    }
 #pragma unroll
     for (int i = 0; i < 4; ++i) st[i] = nst[i];
     if constexpr (BRANCH) {
@@ -394,7 +405,7 @@ __device__ __forceinline__ void bwd_body(const NormArgs& a) {
         if constexpr (TOKEN) rg[v] = load_bf<XF32, NT>(vg, c);
       }
     }
-    next_row(row + stride);
+    if constexpr (AHEAD) next_row(row + stride);
 #pragma unroll
     for (int v = 0; v < V; ++v) {  // a chunk's loads of the next row go out as soon as it is taken from its registers
       rd[v].get(G[v]);
@@ -414,8 +425,8 @@ __device__ __forceinline__ void bwd_body(const NormArgs& a) {
           G[v][i] = fmaf(u, st[3], G[v][i]);
         }
       }
-      load_chunk(v);
-      if constexpr (!BRANCH) load_d(v);
+      if constexpr (AHEAD) load_chunk(v);
+      if constexpr (AHEAD && !BRANCH) load_d(v);
     }
     if (a.ng) {
       row_sum<2>(a.t_log2, s, slots, turn);
@@ -426,7 +437,7 @@ __device__ __forceinline__ void bwd_body(const NormArgs& a) {
         rx[v].get(x);
 #pragma unroll
         for (int i = 0; i < 8; ++i) G[v][i] -= fmaf((x[i] - st[2]) * st[3], m1, m0);
-        load_x(v);
+        if constexpr (AHEAD) load_x(v);
       }
     }
     s[0] = s[1] = 0.f;
@@ -489,7 +500,7 @@ __device__ __forceinline__ void bwd_body(const NormArgs& a) {
 #pragma unroll
       for (int v = 0; v < V; ++v) {
         float z[8], o[8];
-        load_d(v);
+        if constexpr (AHEAD) load_d(v);
         unpack8(rz[v], z);
 #pragma unroll
         for (int i = 0; i < 8; ++i) o[i] = (G[v][i] - fmaf((z[i] - st[0]) * st[1], m1, m0)) * st[1];
@@ -588,9 +599,16 @@ int norm_t_log2(int64_t H) {
 }
 int norm_chunks(int64_t H, int t_log2) { return int((H / 8 + (int64_t(1) << t_log2) - 1) >> t_log2); }
 
+// Backward: two chunks a thread rather than four where a workgroup has the threads (8192 x 8192: norm, gate and betas 375 -> 164 us, fp32 271 -> 211; without
+// either the same).
+int norm_bwd_t_log2(int64_t H) {
+  const int n = norm_t_log2(H);
+  return norm_chunks(H, n) == kMaxV && (2 << n) <= kBwdThreads ? n + 1 : n;
+}
+
 // Workgroups that share out the rows of a backward call, each with partial sums of its own: one per compute unit.
 int64_t norm_groups(const ntp_handle* h, const ntp_block_norm_shape_t* s) {
-  const int64_t at_once = std::max<int64_t>(1, kBwdThreads >> norm_t_log2(s->H));
+  const int64_t at_once = std::max<int64_t>(1, kBwdThreads >> norm_bwd_t_log2(s->H));
   return std::max<int64_t>(1, std::min<int64_t>((s->M + at_once - 1) / at_once, h->compute_units));
 }
 
@@ -705,7 +723,7 @@ extern "C" int ntp_block_norm_bwd(ntp_handle_t* h, const ntp_block_norm_shape_t*
     ntp::timing_begin(h, stream, "block_norm_bwd", 0.0,
                       n * (rt + (dXout ? rt : 0) + (pre ? 2 + rt : 0) + (a.Z ? 2 : 0) + (dZ ? 2 : 0) + (token ? 2 : 0) + (a.dgate_rows ? 2 : 0)));
   }
-  a.t_log2 = norm_t_log2(s->H);
+  a.t_log2 = norm_bwd_t_log2(s->H);
   const bool bias = w->post_beta || w->pre_beta;
   const int threads = std::max(kBwdThreads, 1 << a.t_log2);
   const dim3 grid{uint32_t(groups)}, block{uint32_t(threads)};

@@ -167,6 +167,31 @@ def test_scores_far_apart(workspace):
     assert (np.abs(f64(C) - want) <= BF * np.abs(want) + F32 * size).all() and (np.abs(f64(LSE) - lse) <= F32).all()
 
 
+def test_two_handles_on_two_streams():
+    """Two batches at once, cut, each on a stream with a handle and a workspace of its own."""
+    import torch
+    cases = [Case([3000, 17, 900], 8, 2, 128, 16, group=4, seed=1), Case([40, 5000], 6, 3, 64, 32, group=2, seed=2)]
+    N = cases[0].N
+    torch.cuda.synchronize()
+    outs = []
+    for c in cases:
+        h, st = N.ntp_create(), torch.cuda.Stream()
+        with torch.cuda.stream(st):
+            need = N.ntp_workspace_bytes(N.binding.NTP_CALL_ATTN_DECODE_SHARD, c.shape, handle=h)
+            N.ntp_set_workspace(torch.empty(need, dtype=torch.uint8, device="cuda"), handle=h)
+            runs = []
+            for _ in range(5):
+                C, LSE = torch.empty(len(c.lengths), c.q * c.d, dtype=torch.bfloat16, device="cuda"), torch.empty(c.q, len(c.lengths), device="cuda")
+                N.ntp_attn_decode_shard(c.shape, N.kv_cache(c.K, c.V), c.Q, c.table, c.len_dev, C, LSE, handle=h)
+                runs.append((C, LSE))
+            outs.append((h, runs))
+    torch.cuda.synchronize()
+    for c, (h, runs) in zip(cases, outs):
+        c.check(*runs[0])
+        assert all(torch.equal(C, runs[0][0]) and torch.equal(LSE, runs[0][1]) for C, LSE in runs)
+        N.ntp_destroy(h)
+
+
 def test_the_cache_reaches_behind_four_gigabytes():
     import torch
     import paper_2504_06095_amd as N

@@ -120,6 +120,13 @@ FWD = [
     (3, 16392, B.LAYER, True, True, "channel", True, True, 1.0, 1.0, 8),
     (2, 32768, B.RMS, True, True, "token", True, False, 1.0, 1.0, 0),
     (1031, 2048, B.LAYER, True, True, "channel", True, False, 1.0, 1.0, 0),
+    (5, 16384, B.LAYER, True, True, "channel", True, True, 1.0, 1.0, 0),       # the most registers and LDS that a row of 512 threads has
+    (4, 16384, B.RMS, True, True, "token", True, False, 1.0, 0.5, 0),
+    (9, 12288, B.LAYER, True, True, "channel", True, False, 1.0, 1.0, 0),
+    (70, 8192, B.RMS, True, True, "token", True, True, 1.0, 1.0, 0),
+    (2500, 1024, B.RMS, True, True, "channel", False, False, 1.0, 0.25, 0),    # several rows side by side, several turns
+    (2100, 512, B.LAYER, True, True, "token", False, True, 2.0, 1.0, 8),
+    (300, 6144, B.RMS, True, True, "channel", False, True, 1.0, 0.5, 0),
 ]
 
 
@@ -313,6 +320,28 @@ def test_gradients_that_are_not_wanted_and_no_rows():
         c0.N.ntp_block_norm_bwd(c0.shape, e(), e(), e(), e(), c.torch.empty(4, 0, device="cuda"), e(), e(), **c.w, **{"d_" + k: v for k, v in g.items()}, accumulate=acc)
         c.torch.cuda.synchronize()
         assert all(bool((v == want).all()) for v in g.values())
+
+
+def test_two_handles_on_two_streams():
+    """The same gradient on two streams with nothing ordering them, each with a handle and a workspace of its own."""
+    c = Case(700, 1032, B.LAYER, True, True, "channel", True, False)
+    torch, N = c.torch, c.N
+    dXo, dY, Xout, Z, Stats = _bwd_inputs(c)
+    need = N.ntp_workspace_bytes(N.binding.NTP_CALL_BLOCK_NORM, c.shape)
+    torch.cuda.synchronize()
+    runs = []
+    for _ in range(2):
+        h, st = N.ntp_create(), torch.cuda.Stream()
+        with torch.cuda.stream(st):
+            N.ntp_set_workspace(torch.empty(need, dtype=torch.uint8, device="cuda"), handle=h)
+            runs.append((h, st, [run_bwd(c, dXo, dY, Xout, Z, Stats, handle=h) for _ in range(4)]))
+    torch.cuda.synchronize()
+    first = runs[0][2][0]
+    check_bwd(c, dXo, dY, Xout, Z, Stats, *first)
+    for h, _, results in runs:
+        for dX, dZ, g in results:
+            assert torch.equal(dX, first[0]) and torch.equal(dZ, first[1]) and all(torch.equal(g[k], first[2][k]) for k in g)
+        N.ntp_destroy(h)
 
 
 def test_on_a_stream_and_in_a_graph():
