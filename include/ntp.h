@@ -350,7 +350,8 @@ int ntp_attn_core_shard_bwd(ntp_handle_t* h, const ntp_attn_core_shape_t* shape,
  * token) or NTP_GATE_TOKEN (gate = [M x H] with leading dimension ldgate).
  * Z, Y, the gate and the norm vectors are bf16; X and X' (and their gradients) are bf16, or fp32 where residual_fp32 != 0.  Sums are
  * fp32, each output is rounded once.  16-byte aligned base pointers; leading dimensions and H multiples of 8
- * (fp32 matrices: of 4); H <= 32768 (UNSUPPORTED beyond); eps > 0.
+ * (fp32 matrices: of 4); H <= 32768 (UNSUPPORTED beyond; forward also M T >= 2^32, T = H / 32 rounded up to a power of two in 64 .. 1024: threads of a
+ * launch); eps > 0.
  * Matrices without rows (M = 0) may be NULL.  No buffer may alias another, with two exceptions: Xout may be X, and dX may be dXout (same pointer and leading dimension). */
 #define NTP_NORM_RMS 0
 #define NTP_NORM_LAYER 1
@@ -414,7 +415,8 @@ int ntp_block_norm_bwd(ntp_handle_t* h, const ntp_block_norm_shape_t* shape, con
  *   Qout       [M x q_cnt head_dim] rotated queries, NULL: not wanted
  *   Kout       [M x kv_cnt head_dim] rotated keys beside the cache, NULL: not wanted
  * A prompt's rows go on to ntp_attn_core_shard_fwd, which reads packed QKV: Qout and Kout may be the query and key columns of QKV itself
- * (QKV with ldqkv, and QKV + q_cnt * head_dim with ldqkv); no other aliasing.  head_dim 64 or 128 (UNSUPPORTED otherwise). */
+ * (QKV with ldqkv, and QKV + q_cnt * head_dim with ldqkv); no other aliasing.  head_dim 64 or 128 (UNSUPPORTED otherwise,
+ * and for more tokens than a launch has room for: at least 2^24). */
 typedef struct ntp_kv_cache {
   void *K, *V;
   int64_t n_pages, page_stride;
@@ -437,11 +439,14 @@ int ntp_kv_append_shard(ntp_handle_t* h, const ntp_kv_append_shape_t* shape, con
  *                ceil(max_len / page_size) <= ldt entries, of which those past a sequence's end are not used.  Tokens of an entry outside
  *                [0, n_pages) are left out of the softmax
  *   lengths      DEVICE int32 [n_seq]; 0 or less: no tokens.  max_len (host) bounds them, longer sequences are cut to it: it sizes the
- *                launch, and a captured graph serves every length up to it.  At most 2^30 (UNSUPPORTED beyond)
+ *                launch, and a captured graph serves every length up to it.  At most 2^30, and n_seq q_cnt < 2^24
+ *                (UNSUPPORTED beyond)
  *   C            [n_seq x q_cnt head_dim] bf16; a sequence with no tokens gets zeros
  *   LSE          DEVICE fp32 [q_cnt x n_seq], may be NULL: natural logarithm of the sum of exp(score); -inf for no tokens
- * What lies in the cache behind a sequence's last token is not used (it may be NaN).  Few long sequences are cut along their length
- * where the handle's workspace has room for the pieces' fp32 partial results (ntp_workspace_bytes, NTP_CALL_ATTN_DECODE_SHARD). */
+ * What lies in the cache behind a sequence's last token is not used (it may be NaN).  Where the handle's workspace has room for partial results
+ * (ntp_workspace_bytes, NTP_CALL_ATTN_DECODE_SHARD), the tokens of all sequences and heads are shared out equally among the workgroups, by the lengths on the
+ * device; how a sequence is cut, and with it the order of its fp32 sums, then depends on the lengths of the whole batch (the same lengths
+ * give the same bits).  Without one a workgroup takes one sequence and KV head whole. */
 typedef struct ntp_attn_decode_shape {
   int32_t n_seq, max_len;
   int32_t q_cnt, kv_cnt;
@@ -612,6 +617,7 @@ int ntp_kernel_timing_read(ntp_handle_t* h, ntp_kernel_time_t* out, int64_t max_
  * heads of a long sequence is fewer workgroups than compute units): every workgroup's
  * walk over the key (or query) tiles is cut into parts that store fp32 partial results,
  * merged by a second kernel (forward: by running maximum and sum).
+ * The norms' gradient sums and the attention of one new token use it as their calls say.
  *   workspace  device pointer, 256-byte aligned; NULL with bytes == 0 removes it
  *   bytes      its size; a GEMM is split only if splits * M * round_up(N, 16) * 4 fits,
  *              a walk cut only if workgroups * parts * 64 rows * row bytes fits

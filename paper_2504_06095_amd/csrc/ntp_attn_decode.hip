@@ -38,6 +38,7 @@ typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
 constexpr int kThreads = 256, kWaves = 4, kBlock = 16;  // kBlock: tokens of a contiguous block
 constexpr int kMaxShares = 1024;
+constexpr int64_t kMaxGrid = 0xffffffffll / kThreads;   // workgroups: a launch counts its threads in 32 bits
 constexpr int kTileBytes = 8192;                        // of keys, and of values, per tile
 template <int D>
 constexpr int kTile = kTileBytes / (2 * D);  // tokens per tile: 32 or 64
@@ -56,7 +57,7 @@ struct DecodeArgs {
   int64_t ldq, ldc, ldt, page_stride;
   int32_t n_pages, n_seq, max_len, q_cnt, q_off, kv_off, group, page_size, page_log2;
   int32_t kv_first, kv_used, head_tiles;  // local KV heads that are read; 16-head tiles of a KV head's query heads
-  int32_t shares;
+  int32_t shares, join_rows;              // join_rows: see attn_decode_join_kernel
   float scale_log2;                       // log2(e) / sqrt(d)
 };
 
@@ -180,19 +181,52 @@ struct Line {
     upto = sum_upto(i < a.n_seq ? steps_of<D>(a, len) : 0);
   }
   __device__ __forceinline__ int last() const { return __builtin_amdgcn_readlane(upto, 63); }
-  // the whole line; then the first 64 sequences
+  // steps of a unit of kAtOnce sequences, this lane's and all lanes'; the loads go out together
+  static constexpr int kAtOnce = 512;
+  __device__ __forceinline__ static int lane_steps(const DecodeArgs& a, int from) {
+    int n[kAtOnce / 64], sum = 0;
+#pragma unroll
+    for (int k = 0; k < kAtOnce / 64; ++k) {
+      const int i = from + k * 64 + int(threadIdx.x & 63);
+      n[k] = i < a.n_seq ? a.lengths[i] : 0;
+    }
+#pragma unroll
+    for (int k = 0; k < kAtOnce / 64; ++k) sum += from + k * 64 + int(threadIdx.x & 63) < a.n_seq ? steps_of<D>(a, n[k]) : 0;
+    return sum;
+  }
+  __device__ __forceinline__ static int all_steps(int lane_sum) { return __builtin_amdgcn_readlane(sum_upto(lane_sum), 63); }
+  // the whole line, and how it is cut; the first 64 sequences
   __device__ __forceinline__ void measure(const DecodeArgs& a) {
     before = 0;
-    for (int from = 0; from < a.n_seq; from += 64) {
-      if (from > 0) before += last();
-      load(a, from);
+    load(a, 0);
+    int steps = last();
+    if (a.n_seq > 64) {
+      int sum = 0;
+      for (int from = 0; from < a.n_seq; from += kAtOnce) sum += lane_steps(a, from);
+      steps = all_steps(sum);
     }
-    total = (before + last()) * per_seq;
+    total = steps * per_seq;
     shares = std::min(a.shares, total);  // (one step at least for each)
     q = total / shares;
     r = total % shares;
-    before = 0;
-    if (base > 0) load(a, 0);
+  }
+  // from the first 64 sequences to the one with step x of the line, and its unit and the number in it: by kAtOnce, then by 64 (4096 sequences of up to
+  // 400 tokens, one KV head: 64 by 64, and every query head's workgroup joining, 470 us; so 133)
+  __device__ __forceinline__ void seek(const DecodeArgs& a, int x, int& seq, int& unit, int& step) {
+    int from = 0;
+    while (from < a.n_seq - kAtOnce) {
+      const int n = all_steps(lane_steps(a, from));
+      if ((before + n) * per_seq > x) break;
+      before += n;
+      from += kAtOnce;
+    }
+    if (from > 0) load(a, from);
+    uint64_t behind;
+    while ((behind = __ballot((before + upto) * per_seq > x)) == 0) next64(a);
+    seq = base + __builtin_ctzll(behind);
+    const int steps = steps_of<D>(a, length(seq)), rest = x - steps_before(seq) * per_seq;
+    unit = rest / steps;
+    step = rest % steps;
   }
   __device__ __forceinline__ int begin(int w) const { return w * q + std::min(w, r); }
   __device__ __forceinline__ int share_of(int x) const { return x < r * (q + 1) ? x / (q + 1) : r + (x - r * (q + 1)) / q; }
@@ -254,12 +288,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2))) v
     if (int(blockIdx.x) >= line.shares) return;
     x = line.begin(blockIdx.x);
     x_end = line.begin(blockIdx.x + 1);
-    uint64_t behind;
-    while ((behind = __ballot((line.before + line.upto) * line.per_seq > x)) == 0) line.next64(a);
-    seq = line.base + __builtin_ctzll(behind);
-    const int steps = steps_of<D>(a, line.length(seq)), rest = x - line.steps_before(seq) * line.per_seq;
-    unit = rest / steps;
-    step = rest % steps;
+    line.seek(a, x, seq, unit, step);
   } else {
     seq = int(blockIdx.x) / line.per_seq;
     unit = int(blockIdx.x) % line.per_seq;
@@ -467,16 +496,34 @@ __global__ __launch_bounds__(kThreads) void attn_decode_join_kernel(const Decode
   constexpr int L = D / 4, G = kThreads / L, N = kMaxShares / kThreads;
   __shared__ float weight[kMaxShares], wave_max[kWaves], wave_sum[kWaves];
   __shared__ f32x4 rows[G][L];
-  const int seq = blockIdx.x / a.q_cnt, head = blockIdx.x % a.q_cnt;
-  // the head's unit and its row in the unit's 16
-  const int kv = (a.q_off + head) / a.group - a.kv_off, unit0 = (kv - a.kv_first) * a.head_tiles;
-  const int in_group = head - Heads(a, unit0).j0, unit = unit0 + in_group / 16, r16 = in_group % 16;
   Line<D> line;
   line.per_seq = a.kv_used * a.head_tiles;
   line.measure(a);
-  while (seq >= line.base + 64) line.next64(a);
-  const int steps = steps_of<D>(a, line.length(seq)), begin = line.steps_before(seq) * line.per_seq + unit * steps;
-  const int w0 = line.share_of(begin), used = line.share_of(begin + steps - 1) - w0 + 1;
+  int seq, head, r16, w0, begin;  // the head's row in its unit's 16, the share in which the unit begins, and its first step
+  if (a.join_rows == 0) {  // workgroup = (sequence, query head)
+    seq = int(blockIdx.x) / a.q_cnt;
+    head = int(blockIdx.x) % a.q_cnt;
+    const int kv = (a.q_off + head) / a.group - a.kv_off, unit0 = (kv - a.kv_first) * a.head_tiles;
+    const int in_group = head - Heads(a, unit0).j0;
+    r16 = in_group % 16;
+    while (seq >= line.base + 64) line.next64(a);
+    begin = line.steps_before(seq) * line.per_seq + (unit0 + in_group / 16) * steps_of<D>(a, line.length(seq));
+    w0 = line.share_of(begin);
+  } else {  // workgroup = (border between two shares, row): the first border inside a unit
+    const int w = int(blockIdx.x) / a.join_rows + 1;
+    if (w >= line.shares) return;
+    const int x = line.begin(w);
+    int unit, step;
+    line.seek(a, x, seq, unit, step);
+    begin = x - step;
+    w0 = w - 1;
+    if (step == 0 || line.begin(w0) > begin) return;
+    const Heads hd(a, unit);
+    r16 = int(blockIdx.x) % a.join_rows;
+    head = hd.j0 + r16;
+    if (head >= hd.j1) return;
+  }
+  const int steps = steps_of<D>(a, line.length(seq)), used = line.share_of(begin + steps - 1) - w0 + 1;
   if (used == 1) return;  // written whole
   // part p is what share w0 + p left: of the unit that it begins inside, but for a first share that begins before the unit
   const int late = line.begin(w0) < begin;
@@ -550,7 +597,8 @@ struct DecodeChoice {
 };
 
 // How a call is cut: into two shares per compute unit (a workgroup's tiles take 64 KB of the LDS), but no more than there can be steps; not at all where no unit
-// can have more than one step, or more workgroups than that would have nothing to do.
+// can have more than one step, or more workgroups than that would have nothing to do.  Also where there are many units, since the lengths are not known here: 512
+// sequences, 8 KV heads, max_len 8192, in shares / in whole units: lengths of 1 .. 8192 1250 / 1337 us, 1 .. 400 86 / 69, 1 .. 200 and one of 8192 59 / 116.
 DecodeChoice choose_decode(const ntp_handle* h, int64_t ws_bytes, const ntp_attn_decode_shape_t* s) {
   DecodeChoice c{};
   if (s->q_cnt == 0 || s->n_seq == 0) return c;
@@ -584,13 +632,13 @@ extern "C" int ntp_attn_decode_shard(ntp_handle_t* h, const ntp_attn_decode_shap
   if (st != NTP_OK) return st;
   if (!h || (st = ntp::check_kv_cache(cache, s->kv_cnt, s->head_dim)) != NTP_OK) return h ? st : NTP_ERR_INVALID_ARG;
   if (s->n_seq == 0 || s->q_cnt == 0) return NTP_OK;
+  if (int64_t(s->n_seq) * s->q_cnt > kMaxGrid) return NTP_ERR_UNSUPPORTED;
   const int64_t w = int64_t(s->q_cnt) * s->head_dim, pages = (int64_t(s->max_len) + cache->page_size - 1) / cache->page_size;
   if (!Q || !C || !lengths || (!block_table && pages > 0) || ldq < w || ldc < w || ldt < pages) return NTP_ERR_INVALID_ARG;
   auto off4 = [](const void* p) { return (reinterpret_cast<uintptr_t>(p) & 3) != 0; };
   if (off16(Q) || off16(C) || ldq % 8 || ldc % 8 || off4(block_table) || off4(lengths) || off4(LSE)) return NTP_ERR_ALIGNMENT;
   if (h->device < 0) return NTP_ERR_NO_DEVICE;
   const DecodeChoice c = choose_decode(h, h->workspace ? h->workspace_bytes : 0, s);
-  if (c.units > 0x7fffffffll) return NTP_ERR_UNSUPPORTED;
   DecodeArgs a{};
   a.Q = static_cast<const uint16_t*>(Q), a.K = static_cast<const uint16_t*>(cache->K), a.V = static_cast<const uint16_t*>(cache->V);
   a.table = block_table, a.lengths = lengths, a.C = static_cast<uint16_t*>(C), a.LSE = LSE;
@@ -606,11 +654,19 @@ extern "C" int ntp_attn_decode_shard(ntp_handle_t* h, const ntp_attn_decode_shap
   hipStream_t hs = static_cast<hipStream_t>(stream);
   if (ntp::timing_on(h))
     ntp::timing_begin(h, stream, c.shares > 0 ? "attn_decode_cut" : "attn_decode", 4.0 * s->n_seq * double(s->max_len) * s->head_dim * s->q_cnt, 0.0);
-  const dim3 grid(uint32_t(c.shares > 0 ? c.shares : c.units)), joins(uint32_t(int64_t(s->n_seq) * s->q_cnt));
+  // Joined per (sequence, query head), or per border between shares where that is fewer workgroups: many sequences, of which few are cut
+  // (1024 sequences of 1 .. 400 tokens, 32 heads over 8 KV heads: 276 -> 170 us with the search of 512 sequences at a time).
+  const int32_t rows = std::min(16, std::min(s->group, s->q_cnt));
+  int64_t n_joins = int64_t(s->n_seq) * s->q_cnt;
+  if (c.shares > 0 && n_joins > int64_t(c.shares - 1) * rows) {
+    a.join_rows = rows;
+    n_joins = int64_t(c.shares - 1) * rows;
+  }
+  const dim3 grid{uint32_t(c.shares > 0 ? c.shares : c.units)}, joins{uint32_t(n_joins)};
   if (s->head_dim == 128) hipLaunchKernelGGL(attn_decode_kernel<128>, grid, dim3(kThreads), 0, hs, a);
   else hipLaunchKernelGGL(attn_decode_kernel<64>, grid, dim3(kThreads), 0, hs, a);
   bool ok = hipGetLastError() == hipSuccess;
-  if (ok && c.shares > 0) {
+  if (ok && c.shares > 1) {
     if (s->head_dim == 128) hipLaunchKernelGGL(attn_decode_join_kernel<128>, joins, dim3(kThreads), 0, hs, a);
     else hipLaunchKernelGGL(attn_decode_join_kernel<64>, joins, dim3(kThreads), 0, hs, a);
     ok = hipGetLastError() == hipSuccess;

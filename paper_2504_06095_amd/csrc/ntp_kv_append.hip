@@ -170,6 +170,8 @@ extern "C" int ntp_kv_append_shard(ntp_handle_t* h, const ntp_kv_append_shape_t*
   if ((overlap(Qout, ldq, wq, QKV, ldqkv, w, s->M) && (Qout != QKV || (ldq != ldqkv && !one))) ||
       (overlap(Kout, ldk, wk, QKV, ldqkv, w, s->M) && (Kout != in + wq || (ldk != ldqkv && !one))))
     return NTP_ERR_INVALID_ARG;
+  const int64_t per_row = (w / d) * (d / 16), most = std::max<int64_t>(1, std::min(int64_t(kMaxTokens), 384 / per_row));  // items of a row; tokens of a workgroup
+  if ((s->M + most - 1) / most * kThreads > 0xffffffffll) return NTP_ERR_UNSUPPORTED;  // a launch counts its threads in 32 bits
   if (h->device < 0) return NTP_ERR_NO_DEVICE;
   AppendArgs a{};
   a.QKV = in, a.Qout = static_cast<uint16_t*>(Qout), a.Kout = static_cast<uint16_t*>(Kout);
@@ -183,8 +185,7 @@ extern "C" int ntp_kv_append_shard(ntp_handle_t* h, const ntp_kv_append_shape_t*
   a.q_cnt = s->q_cnt, a.kv_cnt = s->kv_cnt, a.head_dim = s->head_dim, a.rotary_dim = s->rotary_dim, a.interleaved = s->interleaved != 0;
   // at least an item for every thread where rows are short, as long as there are two workgroups for every compute unit (8192 tokens, 5 heads: 1 / 4 / 8 tokens a
   // workgroup 10.3 / 6.4 / 6.7 us, 20 heads: 1 / 2 / 4 tokens 16.6 / 15.7 / 16.0 us, 42 heads: 32 / 35 / 36 us)
-  const int64_t per_row = (w / d) * (d / 16);
-  a.tokens = int32_t(std::max<int64_t>(1, std::min({int64_t(kMaxTokens), 384 / per_row, s->M / (2 * h->compute_units)})));
+  a.tokens = int32_t(std::max<int64_t>(1, std::min(most, s->M / (2 * h->compute_units))));
   hipStream_t hs = static_cast<hipStream_t>(stream);
   if (ntp::timing_on(h))
     ntp::timing_begin(h, stream, "kv_append", 0.0, 2.0 * double(s->M) * double(w + (Qout ? wq : 0) + (Kout ? wk : 0) + (cache ? 2 * wk : 0)));

@@ -127,6 +127,21 @@ def test_lengths_far_below_max_len(d, lengths):
     c.check(C1, LSE1)
 
 
+@pytest.mark.parametrize("q,kv,d,q_off,group", [(5, 2, 128, 1, 4), (5, 2, 64, 1, 4), (40, 2, 64, 0, 20), (1, 1, 128, 3, 16)])
+@pytest.mark.parametrize("n", [65, 513, 1300])
+def test_many_sequences(n, q, kv, d, q_off, group):
+    """More than the 64 and the 512 whose lengths are taken at once, some of them cut by several shares, most of them by none."""
+    rng = np.random.default_rng(n + q)
+    lengths = rng.integers(0, 150, n)
+    for at, length in ((0, 3000), (63, 700), (64, 2100), (n // 2, 5000), (n - 2, 1030), (n - 1, 2500)):
+        lengths[at] = length
+    c = Case(lengths.tolist(), q, kv, d, 64, q_off, 0, group, max_len=20000, seed=n)
+    C, LSE = c.run(True)
+    c.check(C, LSE)
+    again, LSE2 = c.run(True)
+    assert c.torch.equal(C, again) and c.torch.equal(LSE, LSE2)
+
+
 @pytest.mark.parametrize("workspace", [False, True], ids=["whole", "cut"])
 def test_entries_that_name_no_page_are_left_out(workspace):
     c = Case([500, 40, 33, 2000], 6, 3, 128, 16, 0, 0, 2, seed=3)

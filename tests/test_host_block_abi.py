@@ -18,6 +18,11 @@ def h():
     N.ntp_destroy(handle)
 
 
+def _has_gpu():
+    import torch
+    return torch.cuda.is_available()
+
+
 def _norm_fwd(h, shape=None, w=None, **k):
     s = dict(M=4, H=64, norm=0, gate=0, residual_fp32=0, eps=1e-5, residual_scale=1.0, branch_scale=1.0)
     s.update(shape or {})
@@ -145,6 +150,17 @@ def test_decode_refuses(h):
         assert _decode(h, **k) == ALIGN, k
     assert _decode(None) == INV
     assert _decode(h, dict(n_seq=0)) == 0 and _decode(h, dict(q_cnt=0)) == 0
+
+
+def test_launches_that_count_more_than_32_bits_of_threads_are_refused(h):
+    for H, M in ((64, 1 << 26), (2048, 1 << 26), (32768, 1 << 22)):
+        wide = {k: H for k in ("ldx", "ldz", "ldxo", "ldy")}
+        assert _norm_fwd(h, dict(M=M, H=H), **wide) == UNSUP, (H, M)
+        if not _has_gpu():  # (with one, the call would run)
+            assert _norm_fwd(h, dict(M=M - 4, H=H), **wide) == Bd.NTP_ERR_NO_DEVICE
+    far = dict(Qout=1 << 45, Kout=1 << 46)  # (not inside QKV's rows)
+    assert _append(h, dict(M=(1 << 31) - 1), **far) == UNSUP
+    assert _decode(h, dict(n_seq=1 << 24, q_cnt=1)) == UNSUP and _decode(h, dict(n_seq=(1 << 24) // 3 + 1)) == UNSUP
 
 
 def test_workspace_sizes(h):
