@@ -446,7 +446,7 @@ int ntp_kv_append_shard(ntp_handle_t* h, const ntp_kv_append_shape_t* shape, con
  * What lies in the cache behind a sequence's last token is not used (it may be NaN).  Where the handle's workspace has room for partial results
  * (ntp_workspace_bytes, NTP_CALL_ATTN_DECODE_SHARD), the tokens of all sequences and heads are shared out equally among the workgroups, by the lengths on the
  * device; how a sequence is cut, and with it the order of its fp32 sums, then depends on the lengths of the whole batch (the same lengths
- * give the same bits).  Without one a workgroup takes one sequence and KV head whole. */
+ * give the same bits).  Without one, and at a max_len of a few hundred tokens (ntp_workspace_bytes gives 0), a workgroup takes one sequence and KV head whole. */
 typedef struct ntp_attn_decode_shape {
   int32_t n_seq, max_len;
   int32_t q_cnt, kv_cnt;

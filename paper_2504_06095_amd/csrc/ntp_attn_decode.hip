@@ -600,9 +600,11 @@ struct DecodeChoice {
   int64_t units, ws_bytes;
 };
 
-// How a call is cut: into two shares per compute unit (a workgroup's tiles take 64 KB of the LDS), but no more than there can be steps; not at all where no unit
-// can have more than one step, or more workgroups than that would have nothing to do.  Also where there are many units, since the lengths are not known here: 512
-// sequences, 8 KV heads, max_len 8192, in shares / in whole units: lengths of 1 .. 8192 1250 / 1337 us, 1 .. 400 86 / 69, 1 .. 200 and one of 8192 59 / 116.
+// How a call is cut: into two shares per compute unit (a workgroup's tiles take 64 KB of the LDS), but no more than there can be steps.  Not where units are too short
+// for the join's launch to pay: of at most 4 steps, or 8 where half the compute units have one (one sequence, one KV head, 512 tokens 7.2 us whole and 8.2 cut, 1021
+// tokens 10.5 / 8.3; 8 KV heads, 1024 tokens: 16 sequences 15.3 / 17.1, 64 42.4 / 45.7, of up to 1024 29.2 / 33.7; 2048 tokens: 16 sequences of up to 2048 24.9 / 19.2).
+// Longer units are cut also where there are many, since the lengths are not known here: 512 sequences, 8 KV heads, max_len 8192: lengths of 1 .. 8192 1337 / 1250 us,
+// 1 .. 400 69 / 86, 1 .. 200 and one of 8192 116 / 59.
 DecodeChoice choose_decode(const ntp_handle* h, int64_t ws_bytes, const ntp_attn_decode_shape_t* s) {
   DecodeChoice c{};
   if (s->q_cnt == 0 || s->n_seq == 0) return c;
@@ -611,7 +613,7 @@ DecodeChoice choose_decode(const ntp_handle* h, int64_t ws_bytes, const ntp_attn
   c.head_tiles = (std::min(s->group, s->q_cnt) + 15) / 16;
   c.units = int64_t(c.kv_used) * c.head_tiles * s->n_seq;
   const int64_t step = s->head_dim == 128 ? kStep<128> : kStep<64>, steps = std::max<int64_t>((s->max_len + step - 1) / step, 1);
-  if (steps == 1 || steps * c.units > 0x7fffffffll) return c;
+  if (steps <= 4 || (steps <= 8 && c.units >= h->compute_units / 2) || steps * c.units > 0x7fffffffll) return c;
   const int64_t shares = std::min<int64_t>(std::min(2 * int64_t(h->compute_units), steps * c.units), kMaxShares);
   const int64_t bytes = shares * 2 * 16 * (s->head_dim + 2) * 4;
   if (bytes <= ws_bytes) {
