@@ -370,8 +370,9 @@ __device__ __forceinline__ void bwd_body(const NormArgs& a) {
   };
   auto load_d = [&](int v) { rd[v].template load<NT>(vd, Cols<XF32>(tid, v, a.t_log2)); };
   auto load_x = [&](int v) { rx[v].template load<NT>(vx, Cols<XF32>(tid, v, a.t_log2)); };
-  // (four chunks with five sums, with a gate per token or in fp32 leave no registers for the next row: 4096 x 16384 with betas 390 -> 293 us)
-  constexpr bool AHEAD = V < 4 || (KIND < 2 && !XF32);
+  // (four chunks with five sums, with a gate per token or in fp32 leave no registers for the next row, and three in fp32 with one of the others: 4096 x 16384 with
+  // betas 390 -> 293 us, 4096 x 12288 in fp32 with betas 214 -> 193, with a gate per token 217 -> 209)
+  constexpr bool AHEAD = V < 3 || (V == 3 ? KIND < 2 || !XF32 : KIND < 2 && !XF32);
   if (AHEAD && row0 < row1) {  // (without rows nothing may be read)
     next_row(row0 + lane_row);
 #pragma unroll

@@ -127,6 +127,8 @@ FWD = [
     (2500, 1024, B.RMS, True, True, "channel", False, False, 1.0, 0.25, 0),    # several rows side by side, several turns
     (2100, 512, B.LAYER, True, True, "token", False, True, 2.0, 1.0, 8),
     (300, 6144, B.RMS, True, True, "channel", False, True, 1.0, 0.5, 0),
+    (11, 12288, B.LAYER, True, True, "channel", True, True, 1.0, 0.5, 8),      # three chunks that are not loaded ahead
+    (530, 5640, B.RMS, True, True, "token", True, True, 1.0, 1.0, 8),
 ]
 
 
