@@ -30,6 +30,7 @@ typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 constexpr int kMaxThreads = 1024, kMaxWaves = kMaxThreads / 64;
 constexpr int kFwdThreads = 256, kBwdThreads = 512;  // of a workgroup, where a row has no more of its own
 constexpr int kMaxV = 4;
+constexpr int kSideBySide = 4;  // chunks of column sums in the LDS together (64 KB)
 constexpr int kVectors = 5;  // gradients that are sums over the rows: gp, bp, gate, gn, bn
 constexpr int64_t kMaxH = int64_t(kMaxThreads) * kMaxV * 8;
 
@@ -333,8 +334,7 @@ __device__ __forceinline__ void bwd_body(const NormArgs& a) {
   constexpr int XB = XF32 ? 4 : 2;
   constexpr bool NT = V > 1;
   __shared__ __attribute__((aligned(16))) float slots[2][kMaxWaves][2];
-  __shared__ __attribute__((aligned(16))) float rows_lds[LONG ? 1 : kBwdThreads][8];
-  extern __shared__ __attribute__((aligned(16))) u32x4 vectors[];  // [4][V * T] chunks: gn, gp, gate, bp
+  extern __shared__ __attribute__((aligned(16))) u32x4 vectors[];  // [4][V * T] chunks: gn, gp, gate, bp; behind the rows: kSideBySide sums of each thread's chunk
   int turn = 0;
   const int T = 1 << a.t_log2, tid = threadIdx.x & (T - 1), n_rows = blockDim.x >> a.t_log2;
   const int lane_row = __builtin_amdgcn_readfirstlane(threadIdx.x >> a.t_log2);  // (T is a multiple of the wavefront)
@@ -343,10 +343,23 @@ __device__ __forceinline__ void bwd_body(const NormArgs& a) {
     if constexpr (LONG) unpack8(load_bf<XF32, false>(row_view(vec_ptr[which], 0, 2, a.H), Cols<XF32>(tid, v, a.t_log2)), o);
     else unpack8(vectors[(which * V + v) * T + tid], o);
   };
-  if constexpr (!LONG) {
-    for (int which = 0; which < (KIND == 0 ? 1 : KIND == 1 ? 3 : 4); ++which)
-      if (vec_ptr[which])
-        for (int c = threadIdx.x; c < V * T; c += blockDim.x) vectors[which * V * T + c] = load_bf<XF32, false>(row_view(vec_ptr[which], 0, 2, a.H), Cols<XF32>(c & (T - 1), c >> a.t_log2, a.t_log2));
+  if constexpr (!LONG) {  // (all on their way before the first goes to the LDS: 4096 x 16384 with betas 290 -> 264 us with what that does to the registers, 8192 x 8192 163 -> 159)
+    constexpr int N = KIND == 0 ? 1 : KIND == 1 ? 3 : 4;
+    u32x4 r[N][V];
+#pragma unroll
+    for (int which = 0; which < N; ++which)
+#pragma unroll
+      for (int i = 0; i < V; ++i) {
+        const int c = threadIdx.x + i * kBwdThreads;
+        if (i * kBwdThreads < V * T) r[which][i] = load_bf<XF32, false>(row_view(vec_ptr[which], 0, 2, vec_ptr[which] ? a.H : 0), Cols<XF32>(c & (T - 1), c >> a.t_log2, a.t_log2));
+      }
+#pragma unroll
+    for (int which = 0; which < N; ++which)
+#pragma unroll
+      for (int i = 0; i < V; ++i) {
+        const int c = threadIdx.x + i * kBwdThreads;
+        if (c < V * T) vectors[which * V * T + c] = r[which][i];
+      }
     __syncthreads();
   }
   float acc[kSums[KIND]][V][8] = {};
@@ -510,36 +523,54 @@ __device__ __forceinline__ void bwd_body(const NormArgs& a) {
       }
     }
   }
-  // the rows side by side are added up in order, chunk by chunk; then the workgroup's sums go out
+  // the workgroup's sums go out; where rows lie side by side they are added up in order before, kSideBySide chunks at a time by all threads (one at a time by the
+  // first row's threads: 12075 x 1016 41.4 us, so 40.4; 4096 x 16384 264, so 256)
+  if (a.n_sums == 0) return;
+  float* dst[kSums[KIND]];
   int n = 0;
 #pragma unroll
   for (int k = 0; k < kSums[KIND]; ++k) {
     float* const out = a.sums[kSumOf[KIND][k]];
-    if (!out) continue;
-    float* const dst = a.parts ? a.parts + (int64_t(blockIdx.x) * a.n_sums + n) * a.H : out;
-    ++n;
+    dst[k] = out && a.parts ? a.parts + (int64_t(blockIdx.x) * a.n_sums + n) * a.H : out;
+    n += out != nullptr;
+  }
+  auto put = [&](float* to, int at, f32x4 s) {
+    f32x4* q = reinterpret_cast<f32x4*>(to + at);
+    if (to && at < a.H) *q = !a.parts && a.accumulate ? *q + s : s;
+  };
+  if (LONG || n_rows == 1) {
 #pragma unroll
-    for (int v = 0; v < V; ++v) {
-      const Cols<XF32> c(tid, v, a.t_log2);
-      f32x4 lo = {acc[k][v][0], acc[k][v][1], acc[k][v][2], acc[k][v][3]}, hi = {acc[k][v][4], acc[k][v][5], acc[k][v][6], acc[k][v][7]};
-      if (!LONG && n_rows > 1) {
-        __syncthreads();
-        *reinterpret_cast<f32x4*>(&rows_lds[threadIdx.x][0]) = lo;
-        *reinterpret_cast<f32x4*>(&rows_lds[threadIdx.x][4]) = hi;
-        __syncthreads();
-        if (lane_row == 0)
-          for (int r = 1; r < n_rows; ++r) {
-            lo += *reinterpret_cast<const f32x4*>(&rows_lds[r * T + tid][0]);
-            hi += *reinterpret_cast<const f32x4*>(&rows_lds[r * T + tid][4]);
-          }
+    for (int k = 0; k < kSums[KIND]; ++k)
+#pragma unroll
+      for (int v = 0; v < V; ++v) {
+        const Cols<XF32> c(tid, v, a.t_log2);
+        put(dst[k], c.c0, f32x4{acc[k][v][0], acc[k][v][1], acc[k][v][2], acc[k][v][3]});
+        put(dst[k], c.c1, f32x4{acc[k][v][4], acc[k][v][5], acc[k][v][6], acc[k][v][7]});
       }
-      auto put = [&](int at, f32x4 s) {
-        f32x4* q = reinterpret_cast<f32x4*>(dst + at);
-        if (lane_row == 0 && at < a.H) *q = !a.parts && a.accumulate ? *q + s : s;
-      };
-      put(c.c0, lo);
-      put(c.c1, hi);
-    }
+    return;
+  }
+  f32x4* const side = reinterpret_cast<f32x4*>(vectors);  // [kSideBySide][2][threads]
+#pragma unroll
+  for (int first = 0; first < kSums[KIND] * V; first += kSideBySide) {
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < kSideBySide; ++i)
+      if (first + i < kSums[KIND] * V) {
+        const float* const s = acc[(first + i) / V][(first + i) % V];
+        side[(i * 2 + 0) * kBwdThreads + threadIdx.x] = f32x4{s[0], s[1], s[2], s[3]};
+        side[(i * 2 + 1) * kBwdThreads + threadIdx.x] = f32x4{s[4], s[5], s[6], s[7]};
+      }
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < kSideBySide; ++i)
+      if (first + i < kSums[KIND] * V && dst[(first + i) / V])
+        for (int o = threadIdx.x; o < 2 * T; o += kBwdThreads) {
+          const int half = o >> a.t_log2, at = o & (T - 1);
+          f32x4 s = side[(i * 2 + half) * kBwdThreads + at];
+          for (int r = 1; r < n_rows; ++r) s += side[(i * 2 + half) * kBwdThreads + r * T + at];
+          const Cols<XF32> c(at, (first + i) % V, a.t_log2);
+          put(dst[(first + i) / V], half ? c.c1 : c.c0, s);
+        }
   }
 }
 
@@ -734,7 +765,7 @@ extern "C" int ntp_block_norm_bwd(ntp_handle_t* h, const ntp_block_norm_shape_t*
     constexpr int V = decltype(v)::value, KIND = decltype(kind)::value;
     constexpr bool F32 = decltype(f32)::value;
     if (threads > kBwdThreads) hipLaunchKernelGGL((block_norm_bwd_long_kernel<kMaxV, F32, KIND>), grid, block, 0, hs, a);
-    else hipLaunchKernelGGL((block_norm_bwd_kernel<V, F32, KIND>), grid, block, uint32_t(KIND == 0 ? 1 : KIND == 1 ? 3 : 4) * (V << a.t_log2) * 16u, hs, a);
+    else hipLaunchKernelGGL((block_norm_bwd_kernel<V, F32, KIND>), grid, block, uint32_t(std::max((KIND == 0 ? 1 : KIND == 1 ? 3 : 4) * (V << a.t_log2) * 16, (1 << a.t_log2) < threads ? kSideBySide * kBwdThreads * 32 : 0)), hs, a);
   };
   using std::integral_constant;
   by_chunks(norm_chunks(s->H, a.t_log2), [&](auto v) {
