@@ -8,6 +8,7 @@
 
 #include <algorithm>
 #include <cstdint>
+#include <cstdlib>
 
 #include "ntp_internal.h"
 #include "ntp_kv_cache.h"
@@ -140,10 +141,17 @@ __global__ __launch_bounds__(kThreads) void kv_append_kernel(const AppendArgs a)
   }
 }
 
-// Two views of rows may share memory only by being the same columns.
+// Whether two views of bf16 rows share an element.  With one leading dimension their columns are compared, modulo it: row i of a lies i - j leading dimensions
+// and the bases' distance from row j of b.  With two of them the whole spans are.
 bool overlap(const void* a, int64_t lda, int64_t wa, const void* b, int64_t ldb, int64_t wb, int64_t rows) {
   const char *p = static_cast<const char*>(a), *q = static_cast<const char*>(b);
-  return p && q && p < q + ((rows - 1) * ldb + wb) * 2 && q < p + ((rows - 1) * lda + wa) * 2;
+  if (!p || !q || wa == 0 || wb == 0 || p >= q + ((rows - 1) * ldb + wb) * 2 || q >= p + ((rows - 1) * lda + wa) * 2) return false;
+  if (lda != ldb || rows == 1) return true;
+  const int64_t off = (p - q) / 2;
+  int64_t column = off % lda, row = off / lda;  // of a's first element in b
+  if (column < 0) column += lda, --row;
+  // a's rows begin in b's at that column (row 0 of a in row `row` of b), and reach into the next ones' where they pass the leading dimension
+  return (column < wb && std::abs(row) < rows) || (column + wa > lda && std::abs(row + 1) < rows);
 }
 
 }  // namespace
@@ -168,7 +176,7 @@ extern "C" int ntp_kv_append_shard(ntp_handle_t* h, const ntp_kv_append_shape_t*
   const uint16_t* in = static_cast<const uint16_t*>(QKV);
   const bool one = s->M == 1;  // (a leading dimension does not count then)
   if ((overlap(Qout, ldq, wq, QKV, ldqkv, w, s->M) && (Qout != QKV || (ldq != ldqkv && !one))) ||
-      (overlap(Kout, ldk, wk, QKV, ldqkv, w, s->M) && (Kout != in + wq || (ldk != ldqkv && !one))))
+      (overlap(Kout, ldk, wk, QKV, ldqkv, w, s->M) && (Kout != in + wq || (ldk != ldqkv && !one))) || overlap(Qout, ldq, wq, Kout, ldk, wk, s->M))
     return NTP_ERR_INVALID_ARG;
   const int64_t per_row = (w / d) * (d / 16), most = std::max<int64_t>(1, std::min(int64_t(kMaxTokens), 384 / per_row));  // items of a row; tokens of a workgroup
   if ((s->M + most - 1) / most * kThreads > 0xffffffffll) return NTP_ERR_UNSUPPORTED;  // a launch counts its threads in 32 bits

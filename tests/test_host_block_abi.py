@@ -190,3 +190,20 @@ def test_the_binding_checks_its_tensors():
         N.kv_cache(t(2, 1, 16, 64), t(2, 1, 16, 64))
     with pytest.raises(TypeError):
         N.kv_cache(t(2, 1, 16, 64, dt=torch.float16), t(2, 1, 16, 64, dt=torch.float16))
+
+
+def test_append_compares_columns_where_leading_dimensions_agree(h):
+    """Columns of one wide matrix beside QKV's share no element with it; two outputs may not share one either."""
+    if not _has_gpu():  # (with one, the calls would run)
+        wide = dict(ldqkv=576, ldq=576, ldk=576)  # 320 columns of QKV, 192 and 64 beside them
+        for k in (dict(Qout=3 * P + 2 * 320, Kout=3 * P + 2 * 512), dict(QKV=3 * P + 2 * 256, Qout=3 * P, Kout=3 * P + 2 * 192), dict(Qout=3 * P, Kout=3 * P + 2 * 192),
+                  # the rows of one matrix behind the other's, in the same columns
+                  dict(Qout=3 * P + 2 * 4 * 576, Kout=3 * P - 2 * 4 * 576)):
+            assert _append(h, **{**wide, **k}) == Bd.NTP_ERR_NO_DEVICE, k
+        assert _append(h, dict(M=1), Qout=3 * P, ldq=192, Kout=3 * P + 2 * 192, ldk=64) == Bd.NTP_ERR_NO_DEVICE  # one row: in place whatever the leading dimension says
+    for k in (dict(Qout=3 * P + 2 * 312, Kout=3 * P + 2 * 512), dict(Qout=3 * P + 2 * 392), dict(Qout=3 * P - 2 * 576 + 2 * 312), dict(Kout=3 * P + 2 * 3 * 576 + 2 * 312)):
+        k = {**dict(Qout=9 * P, Kout=10 * P), **k}
+        assert _append(h, ldqkv=576, ldq=576, ldk=576, **k) == INV, k
+    # queries and keys in the same place
+    for k in (dict(Qout=7 * P, Kout=7 * P, ldq=192, ldk=64), dict(Qout=7 * P, Kout=7 * P + 2 * 128, ldq=256, ldk=256), dict(Qout=7 * P, Kout=7 * P + 2 * 3 * 192 + 2 * 64, ldq=192, ldk=64)):
+        assert _append(h, **k) == INV, k
