@@ -506,20 +506,24 @@ __device__ __forceinline__ void bwd_body(const NormArgs& a) {
       }
     }
     if constexpr (BRANCH) {
-      float m0 = 0.f, m1 = 0.f;
       if (a.pg) {
         row_sum<2>(a.t_log2, s, slots, turn);
-        m0 = a.layer ? s[0] * a.inv_h : 0.f;
-        m1 = s[1] * a.inv_h;
-      }
+        const float m0 = a.layer ? s[0] * a.inv_h : 0.f, m1 = s[1] * a.inv_h;
 #pragma unroll
-      for (int v = 0; v < V; ++v) {
-        float z[8], o[8];
-        if constexpr (AHEAD) load_d(v);
-        unpack8(rz[v], z);
+        for (int v = 0; v < V; ++v) {
+          float z[8], o[8];
+          if constexpr (AHEAD) load_d(v);
+          unpack8(rz[v], z);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) o[i] = (G[v][i] - fmaf((z[i] - st[0]) * st[1], m1, m0)) * st[1];
-        store_bf<XF32, NT>(vdz, Cols<XF32>(tid, v, a.t_log2), o);
+          for (int i = 0; i < 8; ++i) o[i] = (G[v][i] - fmaf((z[i] - st[0]) * st[1], m1, m0)) * st[1];
+          store_bf<XF32, NT>(vdz, Cols<XF32>(tid, v, a.t_log2), o);
+        }
+      } else {  // (a loop of its own: dZ = dr, whatever Z is, which may be infinite)
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+          if constexpr (AHEAD) load_d(v);
+          store_bf<XF32, NT>(vdz, Cols<XF32>(tid, v, a.t_log2), G[v]);
+        }
       }
     }
   }

@@ -381,3 +381,25 @@ def test_on_a_stream_and_in_a_graph():
         for k, v in outs.items():
             assert torch.equal(v, want[k]), f"replay {rep}: {k}"
     N.ntp_destroy(h)
+
+
+@pytest.mark.parametrize("gate", ["channel", "token"])
+@pytest.mark.parametrize("fp32", [False, True])
+@pytest.mark.parametrize("H", [264, 1160, 16392])
+def test_the_gradient_of_a_gated_branch_without_a_norm_does_not_depend_on_it(gate, fp32, H):
+    """dZ = b G gate: an infinite or NaN Z reaches the gate's gradient alone."""
+    c = Case(9, H, B.RMS, False, True, gate, False, fp32, b=0.5)
+    torch = c.torch
+    dXo, dY, Xout, Z, Stats = _bwd_inputs(c)
+    dX, dZ, grads = run_bwd(c, dXo, dY, Xout, Z, Stats)
+    check_bwd(c, dXo, dY, Xout, Z, Stats, dX, dZ, grads)
+    Z[2, 17], Z[3, 5], Z[8, H - 1] = float("inf"), float("nan"), float("-inf")
+    dX2, dZ2, grads2 = run_bwd(c, dXo, dY, Xout, Z, Stats)
+    torch.cuda.synchronize()
+    assert torch.equal(dX, dX2) and torch.equal(dZ, dZ2)
+    same = grads["gate"] == grads2["gate"]
+    if gate == "channel":
+        assert [int(i) for i in (~same).nonzero()[:, 0]] == [5, 17, H - 1]
+    else:
+        assert (~same).nonzero().tolist() == [[2, 17], [3, 5], [8, H - 1]]
+    assert torch.equal(grads["pre_gamma"], grads2["pre_gamma"])
