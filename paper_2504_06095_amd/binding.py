@@ -481,7 +481,7 @@ def _rows(t, dtype, m, n, name):
         if tuple(t.size()) != (m, n):
             raise ValueError(f"{name}: expected {m} x {n}, got {tuple(t.size())}")
         _mat(t, dtype)
-    return t.data_ptr(), stride[0] if m > 1 else max(stride[0], n)  # (the stride of a single row does not count)
+    return t.data_ptr(), stride[0] if m > 1 else n  # (the stride of a single row does not count)
 
 
 def block_norm_shape(M, H, norm: int = NTP_NORM_RMS, gate: int = NTP_GATE_NONE, residual_fp32: bool = False, eps: float = 1e-5,

@@ -403,3 +403,18 @@ def test_the_gradient_of_a_gated_branch_without_a_norm_does_not_depend_on_it(gat
     else:
         assert (~same).nonzero().tolist() == [[2, 17], [3, 5], [8, H - 1]]
     assert torch.equal(grads["pre_gamma"], grads2["pre_gamma"])
+
+
+def test_the_stride_of_a_single_row_does_not_count():
+    """A row taken from a matrix whose leading dimension the calls would refuse, as one new token's rows may be."""
+    c = Case(1, 264, B.RMS, False, True, "token", False, False)
+    torch = c.torch
+    odd = lambda t: torch.nn.functional.pad(t, (0, 3))[:, :264]  # noqa: E731 (a stride of 267)
+    Xout, Y, Stats = c.new(), c.new(), torch.zeros(4, 1, device="cuda")
+    c.N.ntp_block_norm_fwd(c.shape, c.X, c.Z, Xout, Y, Stats, **c.w)
+    Xo, Yo = odd(Xout * 0), odd(Y * 0)
+    w = {**c.w, "gate": odd(c.w["gate"])}
+    assert Xo.stride(0) % 8 and w["gate"].stride(0) % 8
+    c.N.ntp_block_norm_fwd(c.shape, odd(c.X), odd(c.Z), Xo, Yo, Stats, **w)
+    torch.cuda.synchronize()
+    assert torch.equal(Xo, Xout) and torch.equal(Yo, Y)
