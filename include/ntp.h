@@ -442,8 +442,10 @@ int ntp_kv_append_shard(ntp_handle_t* h, const ntp_kv_append_shape_t* shape, con
  *   lengths      DEVICE int32 [n_seq]; 0 or less: no tokens.  max_len (host) bounds them, longer sequences are cut to it: it sizes the
  *                launch, and a captured graph serves every length up to it.  At most 2^30, and n_seq q_cnt < 2^24
  *                (UNSUPPORTED beyond)
- *   C            [n_seq x q_cnt head_dim] bf16; a sequence with no tokens gets zeros
- *   LSE          DEVICE fp32 [q_cnt x n_seq], may be NULL: natural logarithm of the sum of exp(score); -inf for no tokens
+ *   C            [n_seq x q_cnt head_dim] bf16; a sequence with no tokens gets zeros, and so does a query head all of whose scores are -inf
+ *                (weights of zero: not the quotient 0 / 0 of the definition)
+ *   LSE          DEVICE fp32 [q_cnt x n_seq], may be NULL: natural logarithm of the sum of exp(score); -inf in both of these cases
+ * No output may alias another buffer.
  * What lies in the cache behind a sequence's last token is not used (it may be NaN).  Where the handle's workspace has room for partial results
  * (ntp_workspace_bytes, NTP_CALL_ATTN_DECODE_SHARD), the tokens of all sequences and heads are shared out equally among the workgroups, by the lengths on the
  * device; how a sequence is cut, and with it the order of its fp32 sums, then depends on the lengths of the whole batch (the same lengths

@@ -237,3 +237,112 @@ def test_no_sequences_and_no_heads():
     c = Case([0, 0], 3, 1, 128, 16, group=4)
     C, LSE = c.run()
     assert bool((C == 0).all()) and bool((LSE == float("-inf")).all())
+
+
+def _cut(c, h):
+    """A workspace for the call, which the call cuts its work with."""
+    need = c.N.ntp_workspace_bytes(c.N.binding.NTP_CALL_ATTN_DECODE_SHARD, c.shape, handle=h)
+    assert need > 0
+    c.N.ntp_set_workspace(c.torch.full((need // 4,), float("nan"), device="cuda"), handle=h)
+
+
+@pytest.mark.parametrize("q,kv,d,q_off,group", [(5, 2, 128, 1, 4), (40, 2, 64, 0, 20)])
+def test_a_captured_cut_call_serves_every_length(q, kv, d, q_off, group):
+    """One capture at a max_len of many steps, replayed with lengths that cut the work differently; eager calls of other lengths and synchronizations between.
+    Every replay against the oracle and the eager bits."""
+    import torch
+    n, top = 70, 20000
+    lengths = [top] + [600] * (n - 1)
+    c = Case(lengths, q, kv, d, 64, q_off, 0, group, max_len=top, seed=q)
+    N = c.N
+    # every sequence may reach max_len: those behind the first share its pages
+    c.table[1:] = c.table[0]
+    h = N.ntp_create()
+    _cut(c, h)
+    cache = N.kv_cache(c.K, c.V)
+    C, LSE = torch.empty(n, q * d, dtype=torch.bfloat16, device="cuda"), torch.empty(q, n, device="cuda")
+    run = lambda: N.ntp_attn_decode_shard(c.shape, cache, c.Q, c.table, c.len_dev, C, LSE, handle=h)
+    graph, side = torch.cuda.CUDAGraph(), torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        with torch.cuda.graph(graph, stream=side):
+            run()
+    torch.cuda.synchronize()
+    rng = np.random.default_rng(3)
+    mixed = rng.integers(0, 3000, n)
+    mixed[[7, 64, 69]] = 9000, 0, 19999
+    one = np.zeros(n, dtype=np.int64)
+    one[65] = top
+    for what in (np.full(n, 1), mixed, one, np.full(n, 130), np.zeros(n, dtype=np.int64), mixed[::-1].copy()):
+        c.lengths = [int(x) for x in what]
+        c.len_dev.copy_(torch.from_numpy(what.astype(np.int32)))
+        run()
+        torch.cuda.synchronize()
+        eager, eager_lse = C.clone(), LSE.clone()
+        C.fill_(float("nan"))
+        LSE.fill_(float("nan"))
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(C, eager) and torch.equal(LSE, eager_lse)
+        c.check(C, LSE)
+    N.ntp_destroy(h)
+
+
+def test_two_captured_calls_share_a_workspace():
+    """Two graphs whose calls use one handle's workspace, replayed in turn on one stream."""
+    import torch
+    cases = [Case([3000, 17, 900], 8, 2, 128, 16, group=4, seed=1), Case([40, 5000, 2222], 6, 3, 64, 32, group=2, seed=2)]
+    N = cases[0].N
+    h, st = N.ntp_create(), torch.cuda.Stream()
+    need = max(N.ntp_workspace_bytes(N.binding.NTP_CALL_ATTN_DECODE_SHARD, c.shape, handle=h) for c in cases)
+    assert need > 0
+    N.ntp_set_workspace(torch.full((need // 4,), float("nan"), device="cuda"), handle=h)
+    st.wait_stream(torch.cuda.current_stream())
+    runs = []
+    for c in cases:
+        C, LSE = torch.empty(len(c.lengths), c.q * c.d, dtype=torch.bfloat16, device="cuda"), torch.empty(c.q, len(c.lengths), device="cuda")
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.stream(st):
+            with torch.cuda.graph(graph, stream=st):
+                N.ntp_attn_decode_shard(c.shape, N.kv_cache(c.K, c.V), c.Q, c.table, c.len_dev, C, LSE, handle=h)
+        runs.append((graph, C, LSE))
+    torch.cuda.synchronize()
+    with torch.cuda.stream(st):
+        for turn in range(3):
+            for graph, C, LSE in runs:
+                C.fill_(float("nan"))
+                LSE.fill_(float("nan"))
+            for graph, _, _ in (runs, runs[::-1], runs)[turn]:
+                graph.replay()
+            torch.cuda.synchronize()
+            for c, (_, C, LSE) in zip(cases, runs):
+                c.check(C, LSE)
+    N.ntp_destroy(h)
+
+
+@pytest.mark.parametrize("workspace", [False, True], ids=["whole", "cut"])
+@pytest.mark.parametrize("d", [64, 128])
+def test_lengths_behind_a_max_len_of_many_steps_are_cut(d, workspace):
+    c = Case([2900, 5000, 64, 2610], 4, 2, d, 32, 0, 0, 2, max_len=2610)
+    h = c.N.ntp_create()
+    assert c.N.ntp_workspace_bytes(c.N.binding.NTP_CALL_ATTN_DECODE_SHARD, c.shape, handle=h) > 0
+    c.N.ntp_destroy(h)
+    c.check(*c.run(workspace))
+
+
+@pytest.mark.parametrize("workspace", [False, True], ids=["whole", "cut"])
+@pytest.mark.parametrize("d", [64, 128])
+def test_scores_that_are_all_minus_infinity(d, workspace):
+    """A query head that no token counts for gives what a sequence without tokens gives; the heads and sequences beside it are not touched by it."""
+    c = Case([1700, 1700, 40], 4, 2, d, 32, 0, 0, 2, max_len=4000)
+    C0, LSE0 = c.run(workspace)
+    torch = c.torch
+    c.Q.view(3, 4, d)[0, :2] = 0.5  # the heads of sequence 0 over KV head 0
+    C1, LSE1 = c.run(workspace)
+    pages = c.table[0, :(1700 + 31) // 32].long()
+    c.K[pages, 0, :, 3] = float("-inf")
+    C, LSE = c.run(workspace)
+    v, was = C.view(3, 4, d), C1.view(3, 4, d)
+    assert bool((v[0, :2] == 0).all()) and bool((LSE[:2, 0] == float("-inf")).all())
+    assert torch.equal(v[0, 2:], was[0, 2:]) and torch.equal(v[1:], C0.view(3, 4, d)[1:]) and torch.equal(LSE[:, 1:], LSE0[:, 1:]) and torch.equal(LSE[2:, 0], LSE1[2:, 0])
