@@ -414,6 +414,8 @@ int ntp_block_norm_bwd(ntp_handle_t* h, const ntp_block_norm_shape_t* shape, con
  *              where two name the same one, that slot holds pieces of either.  slots and cache may both be NULL: nothing is appended
  *   Qout       [M x q_cnt head_dim] rotated queries, NULL: not wanted
  *   Kout       [M x kv_cnt head_dim] rotated keys beside the cache, NULL: not wanted
+ * The gradient goes back through the rotation by the same call with inv_freq negated (the transpose of a rotation is the rotation by the opposite angle), no
+ * cache, and the query and key columns of ntp_attn_core_shard_bwd's dQKV as QKV, Qout and Kout.
  * A prompt's rows go on to ntp_attn_core_shard_fwd, which reads packed QKV: Qout and Kout may be the query and key columns of QKV itself
  * (QKV with ldqkv, and QKV + q_cnt * head_dim with ldqkv); no other aliasing, of which what Qout, Kout and QKV share is refused (INVALID_ARG; columns of one matrix,
  * with one leading dimension, share nothing where they do not meet; views of different leading dimensions must not lie in each other's span).  head_dim 64 or 128 (UNSUPPORTED otherwise,

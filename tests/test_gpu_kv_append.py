@@ -135,3 +135,74 @@ def test_slots_behind_four_gigabytes():
     for m, s in enumerate(slots):
         assert torch.equal(K[s // page, :, s % page].reshape(-1), QKV[m, 2 * d:4 * d]) and torch.equal(V[s // page, :, s % page].reshape(-1), QKV[m, 4 * d:])
     assert int((K != 0).any(3).sum()) == kv * M and int((V != 0).any(3).sum()) == kv * M
+
+
+# a workgroup takes min(8, 384 / chunk pairs of a row, M / 512) tokens on 256 compute units: 8, 5, 2 and 4 of them here, and a last one with fewer
+MANY = [
+    (4099, 3, 1, 128, 128, False, 16, 8, 131072),
+    (8191, 11, 4, 64, 32, True, 32, 0, 1 << 20),
+    (1031, 3, 1, 128, 64, False, 64, 0, 2 ** 31 - 1),
+    (2053, 2, 2, 64, 16, True, 256, 40, 4096),
+]
+
+
+@pytest.mark.parametrize("M,q,kv,d,rd,inter,page,pad,far", MANY)
+def test_append_of_several_tokens_a_workgroup(M, q, kv, d, rd, inter, page, pad, far):
+    test_append(M, q, kv, d, rd, inter, page, pad, far)
+
+
+def test_outputs_beside_the_columns_of_one_matrix():
+    """Queries and keys written into columns of the matrix that holds QKV, which they do not meet: the same bits as elsewhere."""
+    import torch
+    import paper_2504_06095_amd as N
+    M, q, kv, d = 37, 3, 1, 64
+    g = torch.Generator(device="cuda").manual_seed(5)
+    w = (q + 2 * kv) * d
+    wide = _rand(torch, g, M, w + (q + kv) * d)
+    f = torch.tensor(10000.0 ** (-np.arange(d // 2) * 2.0 / d), device="cuda")
+    pos = torch.arange(M, dtype=torch.int32, device="cuda") * 11
+    shape = N.kv_append_shape(M, dict(q_cnt=q, kv_cnt=kv, head_dim=d))
+    QKV = wide[:, :w].clone()
+    Q, K = (torch.empty(M, n * d, dtype=torch.bfloat16, device="cuda") for n in (q, kv))
+    N.ntp_kv_append_shard(shape, None, QKV, pos, None, f, Q, K)
+    N.ntp_kv_append_shard(shape, None, wide[:, :w], pos, None, f, wide[:, w:w + q * d], wide[:, w + q * d:])
+    torch.cuda.synchronize()
+    assert torch.equal(wide[:, :w], QKV) and torch.equal(wide[:, w:w + q * d], Q) and torch.equal(wide[:, w + q * d:], K)
+
+
+@pytest.mark.parametrize("inter", [False, True])
+@pytest.mark.parametrize("d,rd", [(64, 32), (128, 128)])
+def test_the_gradient_of_the_rotation_is_the_rotation_back(d, rd, inter):
+    """With inv_freq negated, no cache, and the query and key columns of dQKV as outputs.  Against the transposed rotation in float64, and the
+    identity sum dY R x = sum (R^T dY) x for what the calls themselves made of x."""
+    import torch
+    import paper_2504_06095_amd as N
+    M, q, kv, far = 213, 5, 2, 100000
+    g = torch.Generator(device="cuda").manual_seed(d)
+    X, dQKV = _rand(torch, g, M, (q + 2 * kv) * d), _rand(torch, g, M, (q + 2 * kv) * d, 8)
+    pos = torch.randint(0, far, (M,), dtype=torch.int32, device="cuda", generator=g)
+    f = torch.tensor(500000.0 ** (-np.arange(rd // 2) * 2.0 / rd), device="cuda")
+    shape = N.kv_append_shape(M, dict(q_cnt=q, kv_cnt=kv, head_dim=d), rd, inter)
+    before, x = f64(dQKV), f64(X)
+    wq, wk = q * d, kv * d
+    N.ntp_kv_append_shard(shape, None, dQKV, pos, None, -f, dQKV[:, :wq], dQKV[:, wq:wq + wk])
+    N.ntp_kv_append_shard(shape, None, X, pos, None, f, X[:, :wq], X[:, wq:wq + wk])
+    torch.cuda.synchronize()
+    want = before.copy()
+    turned = before.reshape(M, -1, d)[:, :q + kv].copy()
+    n = rd // 2
+    first, second = (slice(0, rd, 2), slice(1, rd, 2)) if inter else (slice(0, n), slice(n, rd))
+    a = f64(pos)[:, None, None] * f64(f)
+    c, s = np.cos(a), np.sin(a)
+    y1, y2 = turned[..., first].copy(), turned[..., second].copy()
+    turned[..., first], turned[..., second] = c * y1 + s * y2, c * y2 - s * y1  # transpose of (x1 c - x2 s, x2 c + x1 s)
+    want[:, :wq + wk] = turned.reshape(M, -1)
+    tol = np.concatenate([_tol(before, want[:, :wq], q, kv, d, rd, inter, 0, q), _tol(before, want[:, wq:wq + wk], q, kv, d, rd, inter, q, kv), np.zeros((M, wk))], 1)
+    assert (np.abs(f64(dQKV) - want) <= tol).all()
+    # both sides of the identity, row by row: each rounded value is off by half a step of its own, and by 8 fp32 steps of the pair it came from
+    rows = slice(0, wq + wk)
+    left, right = before[:, rows] * f64(X)[:, rows], f64(dQKV)[:, rows] * x[:, rows]
+    slack = np.concatenate([_tol(x, f64(X)[:, :wq], q, kv, d, rd, inter, 0, q), _tol(x, f64(X)[:, wq:wq + wk], q, kv, d, rd, inter, q, kv)], 1)
+    # (a half step of the rounded value: (1 + 2^-8) of one of the value itself)
+    bound = (1 + BF) * ((np.abs(before[:, rows]) * slack).sum(1) + (tol[:, rows] * np.abs(x[:, rows])).sum(1)) + 1e-9
+    assert (np.abs(left.sum(1) - right.sum(1)) <= bound).all()
