@@ -204,3 +204,15 @@ def test_gradient_of_a_residual_block(norm, fp32):
     for k, v in sums.items():
         _close(grads[k], v, k)
     N.ntp_destroy(L.h)
+
+
+@pytest.mark.parametrize("H,ffn,n_q,n_kv,d,tp,rank,n_seq,S,page", [
+    (1024, 4096, 16, 4, 64, 3, 1, 2, 1300, 16),
+    (1024, 2816, 16, 16, 128, 7, 0, 1, 600, 64),
+])
+def test_steps_whose_attention_is_cut(H, ffn, n_q, n_kv, d, tp, rank, n_seq, S, page):
+    """The same at lengths that the call of one new token shares out among the workgroups and joins."""
+    import paper_2504_06095_amd as N
+    plan = N.ntp_attn_shard_plan(n_q, n_kv, d, tp, rank)
+    assert N.ntp_workspace_bytes(N.binding.NTP_CALL_ATTN_DECODE_SHARD, N.attn_decode_shape(n_seq, S, plan, n_q // n_kv)) > 0
+    test_a_prompt_and_then_token_by_token(H, ffn, n_q, n_kv, d, tp, rank, n_seq, S, page)
