@@ -350,7 +350,7 @@ int ntp_attn_core_shard_bwd(ntp_handle_t* h, const ntp_attn_core_shape_t* shape,
  * token) or NTP_GATE_TOKEN (gate = [M x H] with leading dimension ldgate).
  * Z, Y, the gate and the norm vectors are bf16; X and X' (and their gradients) are bf16, or fp32 where residual_fp32 != 0.  Sums are
  * fp32, each output is rounded once.  16-byte aligned base pointers; leading dimensions and H multiples of 8
- * (fp32 matrices: of 4); H <= 32768 (UNSUPPORTED beyond; forward also M T >= 2^32, T = H / 32 rounded up to a power of two in 64 .. 1024: threads of a
+ * (fp32 matrices: of 4); H <= 32768 (UNSUPPORTED beyond; the backward call is made for H <= 16384 and about four times slower per element above; forward also M T >= 2^32, T = H / 32 rounded up to a power of two in 64 .. 1024: threads of a
  * launch); eps > 0.
  * Matrices without rows (M = 0) may be NULL.  No buffer may alias another, with two exceptions: Xout may be X, and dX may be dXout (same pointer and leading dimension). */
 #define NTP_NORM_RMS 0
@@ -451,7 +451,7 @@ int ntp_kv_append_shard(ntp_handle_t* h, const ntp_kv_append_shape_t* shape, con
  * What lies in the cache behind a sequence's last token is not used (it may be NaN).  Where the handle's workspace has room for partial results
  * (ntp_workspace_bytes, NTP_CALL_ATTN_DECODE_SHARD), the tokens of all sequences and heads are shared out equally among the workgroups, by the lengths on the
  * device; how a sequence is cut, and with it the order of its fp32 sums, then depends on the lengths of the whole batch (the same lengths
- * give the same bits).  Without one, and at a max_len of a few hundred tokens (ntp_workspace_bytes gives 0), a workgroup takes one sequence and KV head whole. */
+ * give the same bits).  Without one, with one that is smaller (it is used whole or not at all), and at a max_len of a few hundred tokens (ntp_workspace_bytes gives 0), a workgroup takes one sequence and KV head whole. */
 typedef struct ntp_attn_decode_shape {
   int32_t n_seq, max_len;
   int32_t q_cnt, kv_cnt;

@@ -10,7 +10,9 @@
 //
 // The wavefronts of a workgroup have a running maximum and sum of their own and put their results together at the end of a unit.  Both products run on the
 // 16x16x32 bf16 matrix instruction with the query head on the lane axis (S^T = K Q^T, O^T += V^T P^T), the scores go from the one to the other in
-// registers.  With one query head 15 of 16 columns are idle: matrix work is far from the bound, 16 instructions a tile against 16 KB from HBM.
+// registers.  With one query head 15 of 16 columns are idle: matrix work is far from the bound, 24 instructions a tile (8 for the
+// scores, 8 each for the weights and their rest) against 16 KB from HBM.  A KV head with more than 16 query heads is several units, each of which reads its keys and values (64
+// sequences of up to 8192, one KV head of 128: 16 query heads 31 us, 32 52, 64 98).
 // Both matrices go through a part of the LDS that is the wavefront's own, by DMA, so that nothing but a unit's end needs a barrier.  The loads are non-temporal: a cache line is
 // used once (equal lengths of 4096, 14 heads, 64 sequences: 326 -> 292 us, 6.4 TB/s).
 //
@@ -390,8 +392,8 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2))) v
     const float m_new = fmaxf(m_run, mx), m_use = m_new == -INFINITY ? 0.f : m_new;  // (no score above -inf so far: weights of 0)
     const float alpha = fast_exp2(m_run - m_use);
     float ls = 0.f;
-    // weights as operand B of the second product, per 32 tokens: bf16, and what that leaves, in a product of its own (no rounding of the weights is left in
-    // the result, and the matrix pipe has the room)
+    // weights as operand B of the second product, per 32 tokens: bf16, and what that leaves, rounded to bf16 too, in a product of its own.  Together they are within 2^-17 of
+    // the fp32 weight; an output is a mean of values by these weights, rounded to 2^-8, and a weight has the error of its fp32 score anyway (about 2^-20 for scores of 10)
     bf16x8 pf[NB / 2], pr[NB / 2];
 #pragma unroll
     for (int b = 0; b < NB; ++b)

@@ -10,8 +10,10 @@
 // A row belongs to T threads (a power of two from 64 to 1024), which hold its 16-byte chunks tid, tid + T, ... in registers (V a thread), so that
 // every matrix is read and written once; a workgroup takes several rows side by side where T is small.  What bounds both directions is HBM: 8 to 18 bytes an
 // element against some 20 to 40 operations.  The backward kernel is persistent, one workgroup per compute unit that takes every gridDim-th set of rows, because the sums over
-// the rows stay in its registers until the end; the next row's loads are in flight while this one's sums go round.  Measured: forward 8192 x 16384, fp32 residual, 189 us
-// (5.7 TB/s), 2048 x 12288 bf16 36 us (5.6); backward 8192 x 16384 with both norms and a gate 292 us (5.5), 4099 x 6144, fp32, 93 us (4.9 with a last turn of 3 rows for 256 workgroups).
+// the rows stay in its registers until the end; the next row's loads are in flight while this one's sums go round.  Measured: forward 8192 x 16384 188 us with a bf16
+// residual stream (5.7 TB/s), 285 with an fp32 one (5.7), with a gate per token 234 and 347 (5.7, 5.4), 2048 x 12288 bf16 36 us (5.6); where a row leaves threads idle (T is a power
+// of two) 4096 x 9216 68 (4.5), 4096 x 8456 66 (4.2), 8192 x 5120 66 (5.1).  Backward 8192 x 16384 with both norms and a gate 288 us (5.6), 4099 x 6144, fp32, 93 us (4.9 with a last turn
+// of 3 rows for 256 workgroups); rows of more than 16384 columns are slow (block_norm_bwd_long_kernel).
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -75,8 +77,9 @@ __device__ __forceinline__ u32x4 pack8(const float (&v)[8]) {
 __device__ __forceinline__ __amdgpu_buffer_rsrc_t row_view(const void* base, int64_t at, int elem, int columns) {
   return __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(static_cast<const char*>(base) + at * elem), 0, columns * elem, 0x00020000);
 }
-// Rows go past the caches (NT: non-temporal) where a thread has more than one chunk: large launches, whose matrices no cache holds until they are used again
-// (8192 x 16384 forward 225 -> 202 us, backward 456 -> 376 us).
+// Rows go past the caches (NT: non-temporal) where a thread has more than one chunk: in the forward call many rows, or rows of more than 8192 columns however few; in the
+// backward call all rows of more than 512 columns.  In large launches, whose matrices no cache holds until they are used again, it pays (8192 x 16384 forward 225 -> 202 us, backward
+// 456 -> 376 us); what it costs the reader of a Y that the last-level cache would have kept was not measured.
 template <bool NT>
 __device__ __forceinline__ u32x4 load_16(__amdgpu_buffer_rsrc_t rs, uint32_t off) {
   return __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(rs, off, 0, NT ? 2 : 0));
@@ -320,7 +323,8 @@ __global__ __launch_bounds__(kMaxThreads) void block_norm_fwd_kernel(const NormA
 }
 
 // Which sums over the rows a backward kernel holds, by kind: 0 nothing behind the block (no norm, no gate: Z is not read), 1 no gate or one per channel, no
-// betas, 2 the same with betas, 3 a gate per token.  Numbers into NormArgs::sums.
+// betas, 2 the same with betas, 3 a gate per token.  Numbers into NormArgs::sums.  A kind holds all its sums, also those that a call has no vector for (3 both betas', 0 the one
+// before the next block, 2 both where there is one).  They are fp32: at most one addition a row of the workgroup's share, without a workspace one for every row.
 constexpr int kSums[4] = {2, 3, 5, 4};
 __device__ constexpr int kSumOf[4][kVectors] = {{3, 4, -1, -1, -1}, {0, 2, 3, -1, -1}, {0, 1, 2, 3, 4}, {0, 1, 3, 4, -1}};
 
@@ -582,7 +586,8 @@ template <int V, bool XF32, int KIND>
 __global__ __launch_bounds__(kBwdThreads) void block_norm_bwd_kernel(const NormArgs a) {
   bwd_body<V, XF32, KIND, false>(a);
 }
-// rows of more than kBwdThreads * kMaxV chunks
+// Rows of more than kBwdThreads * kMaxV chunks: 1024 threads leave 128 registers each, of which the sums alone would take 64 to 160, so that all of these kernels keep
+// part of them in memory (312 to 740 bytes a lane).  2048 x 20480 444 us (floor 83), with betas 570-690, in fp32 509 and 690 (floor 124); 2048 x 32768 505 (132), 649, 547 (198), 786.
 template <int V, bool XF32, int KIND>
 __global__ __launch_bounds__(kMaxThreads) void block_norm_bwd_long_kernel(const NormArgs a) {
   bwd_body<V, XF32, KIND, true>(a);
