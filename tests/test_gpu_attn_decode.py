@@ -346,3 +346,14 @@ def test_scores_that_are_all_minus_infinity(d, workspace):
     v, was = C.view(3, 4, d), C1.view(3, 4, d)
     assert bool((v[0, :2] == 0).all()) and bool((LSE[:2, 0] == float("-inf")).all())
     assert torch.equal(v[0, 2:], was[0, 2:]) and torch.equal(v[1:], C0.view(3, 4, d)[1:]) and torch.equal(LSE[:, 1:], LSE0[:, 1:]) and torch.equal(LSE[2:, 0], LSE1[2:, 0])
+
+
+@pytest.mark.parametrize("workspace", [False, True], ids=["whole", "cut"])
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("n", [3, 130])
+def test_local_kv_heads_that_no_query_head_reads(n, d, workspace):
+    """Query heads 12 .. 16 of groups of 4 read global KV heads 3 and 4: the third and fourth of the local ones, which begin at 1."""
+    lengths = ([2700, 33, 0, 1500] * n)[:n] if n < 65 else [2700, 33, 0, 1500] + [5, 70] * ((n - 4) // 2)
+    c = Case(lengths, 5, 5, d, 32, q_off=12, kv_off=1, group=4, seed=n)
+    C, LSE = c.run(workspace)
+    c.check(C, LSE)

@@ -206,3 +206,27 @@ def test_the_gradient_of_the_rotation_is_the_rotation_back(d, rd, inter):
     # (a half step of the rounded value: (1 + 2^-8) of one of the value itself)
     bound = (1 + BF) * ((np.abs(before[:, rows]) * slack).sum(1) + (tol[:, rows] * np.abs(x[:, rows])).sum(1)) + 1e-9
     assert (np.abs(left.sum(1) - right.sum(1)) <= bound).all()
+
+
+@pytest.mark.parametrize("q,kv", [(0, 3), (4, 0)])
+def test_queries_or_keys_alone(q, kv):
+    import torch
+    import paper_2504_06095_amd as N
+    M, d, page = 45, 64, 16
+    X = _rand(torch, torch.Generator(device="cuda").manual_seed(q), M, (q + 2 * kv) * d)
+    pos = torch.arange(M, dtype=torch.int32, device="cuda") * 7
+    f = torch.tensor(10000.0 ** (-np.arange(d // 2) * 2.0 / d), device="cuda")
+    shape = N.kv_append_shape(M, dict(q_cnt=q, kv_cnt=kv, head_dim=d))
+    out = torch.zeros(M, (q + kv) * d, dtype=torch.bfloat16, device="cuda")
+    K, V = (torch.zeros(3, kv, page, d, dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    if q:
+        N.ntp_kv_append_shard(shape, None, X, pos, None, f, out)
+    else:
+        N.ntp_kv_append_shard(shape, N.kv_cache(K, V), X, pos, torch.arange(M, device="cuda"), f, None, out)
+    torch.cuda.synchronize()
+    x = f64(X)
+    want = B.rotate(x.reshape(M, -1, d)[:, :q + kv], f64(pos), f64(f), False).reshape(M, -1)
+    assert (np.abs(f64(out) - want) <= _tol(x, want, q, kv, d, d, False, 0, q + kv)).all()
+    if kv:
+        rows = lambda t: t.transpose(1, 2).reshape(3 * page, kv * d)[:M]  # noqa: E731
+        assert torch.equal(rows(K), out) and torch.equal(rows(V), X[:, kv * d:])

@@ -118,3 +118,29 @@ def test_gradient_from_what_the_forward_call_kept(M, H, post, gate, bias, fp32, 
     else:
         e_z = e_z + 512 * U * z_size
     _close(dZ, want["dZ"], _step(want["dZ"], dZ) * (1 + BF) + (1 + BF) * e_z, "dZ")
+
+
+@pytest.mark.parametrize("fp32", [False, True], ids=["bf16 residual", "fp32 residual"])
+@pytest.mark.parametrize("M,H", [(37, 264), (300, 4104), (5, 16392)])
+@pytest.mark.parametrize("post,gate", [(False, "none"), (False, "channel"), (False, "token"), (True, "none")])
+def test_a_block_without_a_norm_before_the_next(post, gate, M, H, fp32):
+    """Residual addition alone, with a gate, or with the norm behind the block: no dY and no X' are read; the gradient without a residual's own is zero."""
+    c = Case(M, H, B.LAYER, post, False, gate, True, fp32, a=1.5, b=0.5, seed=H)
+    torch = c.torch
+    Xout, Stats = c.new(c.rt), torch.full((4, M), 7.0, device="cuda")
+    c.N.ntp_block_norm_fwd(c.shape, c.X, c.Z, Xout, None, Stats, **c.w)
+    dXo = c.rand(0.1, c.rt)
+    dX, dZ, grads = run_bwd(c, dXo, None, None, c.Z, Stats if post else None)
+    torch.cuda.synchronize()
+    st = check_fwd(c, c.X, c.Z, Xout, None, Stats)
+    check_bwd(c, dXo, None, None, c.Z, Stats, dX, dZ, grads)
+    assert post or not st.any()
+    dX0, dZ0, grads0 = run_bwd(c, None, None, None, c.Z, Stats if post else None)
+    torch.cuda.synchronize()
+    assert not any(bool(t.any()) for t in (dX0, dZ0, *grads0.values()))
+    if gate == "none" and not post:  # Z is not read
+        dX2 = c.new(c.rt)
+        dZ2 = c.new()
+        c.N.ntp_block_norm_bwd(c.shape, dXo, None, None, None, None, dX2, dZ2)
+        torch.cuda.synchronize()
+        assert torch.equal(dX2, dX) and torch.equal(dZ2, dZ)
