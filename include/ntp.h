@@ -463,6 +463,72 @@ int ntp_attn_decode_shard(ntp_handle_t* h, const ntp_attn_decode_shape_t* shape,
                           void* stream);
 
 /* ---------------------------------------------------------------------------
+ * The paged cache in either of two formats, norms of query and key heads, and attention of chunks of new tokens.
+ *
+ * ntp_kv_pages_t: the pages of ntp_kv_cache_t (NTP_KV_BF16: the same memory, so that the calls of both kinds may share a cache), or the same layout with 8-bit
+ * elements (NTP_KV_E4M3): element (page, g, t, c) is an e4m3 number (OCP, no infinities) at page * page_stride + (g * page_size + t) * head_dim + c,
+ * and the token's values of head g are those numbers times 2^(b - 127), b the byte at page * exp_stride + g * page_size + t of K_exp or V_exp (the E8M0
+ * code).  b is the smallest for which no finite value of the head is above 448 * 2^(b - 127), at least 16 (heads of values below 448 * 2^-111 lose precision), and
+ * 127 for a head of zeros; values are rounded once, to the nearest number (ties to even), NaN and infinities become NaN.  Bytes that a caller writes itself
+ * lie in 16 .. 246.
+ *   page_size as ntp_kv_cache_t; page_stride: elements, at least kv_cnt * page_size * head_dim and a multiple of 8 (E4M3: of 16); exp_stride:
+ *   bytes, at least kv_cnt * page_size and a multiple of 16 (K_exp, V_exp and exp_stride count with E4M3 only); all base pointers 16-byte aligned. */
+#define NTP_KV_BF16 0
+#define NTP_KV_E4M3 1
+typedef struct ntp_kv_pages { /* DEVICE */
+  void *K, *V, *K_exp, *V_exp;
+  int64_t n_pages, page_stride, exp_stride;
+  int32_t page_size, format; /* NTP_KV_* */
+} ntp_kv_pages_t;
+
+/* ntp_qk_norm_append_shard: ntp_kv_append_shard with a norm of every query and key head before its rotation, into pages of either format.  A head x of
+ * head_dim elements becomes, before it is rotated,
+ *   x / sqrt(sum x^2 / head_dim + eps) .* gamma       (sums and results fp32, rounded once behind the rotation: to bf16 in Qout, Kout and bf16 pages, to e4m3 in 8-bit ones)
+ * with gamma = q_gamma for query heads and k_gamma for key heads (DEVICE bf16 [head_dim], 16-byte aligned; NULL: those heads have no norm; norm itself may be
+ * NULL: neither has).  eps > 0 where there is a gamma.  Value heads are appended as they are.  Everything else as ntp_kv_append_shard: shape, positions, slots (NULL exactly where pages is), inv_freq,
+ * what may be NULL, what is refused, and Qout and Kout in place of QKV's own columns. */
+typedef struct ntp_qk_norm {
+  const void *q_gamma, *k_gamma;
+  float eps;
+} ntp_qk_norm_t;
+int ntp_qk_norm_append_shard(ntp_handle_t* h, const ntp_kv_append_shape_t* shape, const ntp_qk_norm_t* norm, const ntp_kv_pages_t* pages, const void* QKV,
+                             int64_t ldqkv, const int32_t* positions, const int64_t* slots, const double* inv_freq, void* Qout, int64_t ldq, void* Kout, int64_t ldk,
+                             void* stream);
+
+/* Gradient of the norms and the rotation.  QKV: what the forward call read (not overwritten in place); dQ [M x q_cnt head_dim], dK [M x kv_cnt head_dim]: gradients at
+ * Qout and Kout.  Writes the query and key columns of dQKV [M x (q_cnt + 2 kv_cnt) head_dim] (the value columns stay as they are) and the gradients of the gammas,
+ * fp32 [head_dim], 4-byte aligned, sums over the tokens and the heads that share them (either may be NULL: not wanted; a gradient of a gamma that is NULL is refused); accumulate != 0 adds into them.  dQ and dK may be the query and key
+ * columns of dQKV itself (ntp_attn_core_shard_bwd's dQKV, with its leading dimension); no other aliasing (of dQKV with QKV, dQ or dK: refused).  Deterministic: the order of the sums is fixed by the shape, the handle and
+ * whether its workspace has room for their partial sums (ntp_workspace_bytes, NTP_CALL_QK_NORM; without it one workgroup forms them in a pass of its own: slow). */
+int ntp_qk_norm_shard_bwd(ntp_handle_t* h, const ntp_kv_append_shape_t* shape, const ntp_qk_norm_t* norm, const void* QKV, int64_t ldqkv, const void* dQ, int64_t lddq,
+                          const void* dK, int64_t lddk, const int32_t* positions, const double* inv_freq, void* dQKV, int64_t lddqkv, float* d_q_gamma,
+                          float* d_k_gamma, int32_t accumulate, void* stream);
+
+/* Attention of the new tokens of a batch of sequences over their pages, the new tokens' own keys and values, appended before, included: one token a
+ * sequence, a few (proposed tokens checked at once), the chunk of a long prompt, whole packed prompts, or all of them in one call.  Sequence s has the rows
+ * row_starts[s] .. row_starts[s + 1] - 1 of Q and C; its n rows are the last n of its lengths[s] tokens, so that its row i sees the first lengths[s] - n + i + 1 of them:
+ *   C[row, j] = softmax(q_j K_g^T / sqrt(head_dim)) V_g     over those tokens, KV head g of query head j as in ntp_attn_core_shard_fwd.
+ *   Q           [M x q_cnt head_dim] bf16, rotated: Qout of the append
+ *   row_starts  DEVICE int32 [n_seq + 1], ascending, within 0 .. M (values outside are taken to the nearer end); NULL: M == n_seq (INVALID_ARG otherwise) and sequence s has row s alone.  A sequence may have no
+ *               rows.  max_new (host) bounds the rows of a sequence: rows behind its first max_new stay as they are
+ *   block_table, ldt, lengths, max_len   as ntp_attn_decode_shard (tokens of an entry outside [0, n_pages) are left out of the softmax; longer sequences are cut to max_len)
+ *   C           [M x q_cnt head_dim] bf16.  A row that sees no token (a length of 0, or shorter than its sequence's rows) gets zeros, and so does a query
+ *               head all of whose scores are -inf; rows of no sequence (the padding of a batch) stay as they are
+ *   LSE         DEVICE fp32 [q_cnt x M], may be NULL: natural logarithm of the sum of exp(score); -inf in both of these cases
+ * No output may alias another buffer.  What lies in the pages behind a sequence's last token is not used (it may be NaN).  M * q_cnt < 2^31, max_len <= 2^30 and
+ * n_seq (max_len + 1) (kv heads) < 2^31 in steps of 64 tokens (UNSUPPORTED beyond).  With a workspace of ntp_workspace_bytes (NTP_CALL_ATTN_CHUNK_SHARD) walks over many tokens
+ * are cut into parts where there are few rows, and their order of fp32 sums then depends on the lengths of the whole batch (the same lengths give the same bits); a smaller one is not used. */
+typedef struct ntp_attn_chunk_shape {
+  int64_t M;
+  int32_t n_seq, max_new, max_len;
+  int32_t q_cnt, kv_cnt;
+  int32_t q_off, kv_off, group;
+  int32_t head_dim;
+} ntp_attn_chunk_shape_t;
+int ntp_attn_chunk_shard(ntp_handle_t* h, const ntp_attn_chunk_shape_t* shape, const ntp_kv_pages_t* pages, const void* Q, int64_t ldq, const int32_t* row_starts,
+                         const int32_t* block_table, int64_t ldt, const int32_t* lengths, void* C, int64_t ldc, float* LSE, void* stream);
+
+/* ---------------------------------------------------------------------------
  * Weight gradients written straight into the destination layout of the
  * reshard (Sec. 3.1 "Shard-mapping algorithm"; Appendix, the pre-sync hook):
  * the gradient GEMMs of a backward call store each output row where the
@@ -643,12 +709,16 @@ int ntp_kernel_timing_read(ntp_handle_t* h, ntp_kernel_time_t* out, int64_t max_
  *   NTP_CALL_ATTN_CORE_SHARD  const ntp_attn_core_shape_t*  ntp_attn_core_shard_fwd, _bwd
  *   NTP_CALL_BLOCK_NORM       const ntp_block_norm_shape_t* ntp_block_norm_bwd (with every gradient wanted)
  *   NTP_CALL_ATTN_DECODE_SHARD const ntp_attn_decode_shape_t* ntp_attn_decode_shard
+ *   NTP_CALL_QK_NORM          const ntp_kv_append_shape_t*  ntp_qk_norm_shard_bwd (with both gradients wanted)
+ *   NTP_CALL_ATTN_CHUNK_SHARD const ntp_attn_chunk_shape_t* ntp_attn_chunk_shard
  * Errors: NTP_ERR_INVALID_ARG (NULL, unknown call, a shape the call itself would refuse). */
 #define NTP_CALL_MLP_SHARD 0
 #define NTP_CALL_ATTN_PROJ_SHARD 1
 #define NTP_CALL_ATTN_CORE_SHARD 2
 #define NTP_CALL_BLOCK_NORM 3
 #define NTP_CALL_ATTN_DECODE_SHARD 4
+#define NTP_CALL_QK_NORM 5
+#define NTP_CALL_ATTN_CHUNK_SHARD 6
 int ntp_workspace_bytes(const ntp_handle_t* h, int32_t call, const void* shape, int64_t* bytes);
 int ntp_set_workspace(ntp_handle_t* h, void* workspace, int64_t bytes);
 

@@ -128,3 +128,91 @@ def attn_decode(Q, K, V, table, lengths, max_len, q_off, kv_off, group):
             C[s, j], A[s, j] = w @ v / w.sum(), w @ np.abs(v) / w.sum()
             LSE[j, s] = top + np.log(w.sum())
     return C.reshape(n_seq, -1), LSE, A.reshape(n_seq, -1)
+
+
+def head_norm(x, gamma, eps):
+    """Heads x [..., d] divided by the root of their mean square, times gamma [d] (None: as they are)."""
+    return x if gamma is None else x / np.sqrt((x * x).mean(-1, keepdims=True) + eps) * gamma
+
+
+def qk_norm(QKV, q_cnt, kv_cnt, d, q_gamma, k_gamma, eps, positions, inv_freq, interleaved):
+    """Normed and rotated query heads [M, q_cnt, d] and key heads [M, kv_cnt, d] of QKV, and its value heads."""
+    x = QKV.reshape(QKV.shape[0], q_cnt + 2 * kv_cnt, d)
+    q, k = head_norm(x[:, :q_cnt], q_gamma, eps), head_norm(x[:, q_cnt:q_cnt + kv_cnt], k_gamma, eps)
+    return rotate(q, positions, inv_freq, interleaved), rotate(k, positions, inv_freq, interleaved), x[:, q_cnt + kv_cnt:]
+
+
+def qk_norm_bwd(QKV, q_cnt, kv_cnt, d, q_gamma, k_gamma, eps, positions, inv_freq, interleaved, dQ, dK):
+    """Gradients of qk_norm: at the query and key columns of QKV [M, (q_cnt + kv_cnt) d], and of the gammas (None where there is none)."""
+    M = QKV.shape[0]
+    x = QKV.reshape(M, q_cnt + 2 * kv_cnt, d)
+    out, dg = [], []
+    for t, gamma, up in ((x[:, :q_cnt], q_gamma, dQ.reshape(M, q_cnt, d)), (x[:, q_cnt:q_cnt + kv_cnt], k_gamma, dK.reshape(M, kv_cnt, d))):
+        u = rotate(up, positions, -np.asarray(inv_freq), interleaved)
+        if gamma is None:
+            out.append(u), dg.append(None)
+            continue
+        rstd = 1.0 / np.sqrt((t * t).mean(-1, keepdims=True) + eps)
+        hat = t * rstd
+        dg.append((u * hat).sum((0, 1)))
+        w = u * gamma
+        out.append((w - hat * (w * hat).mean(-1, keepdims=True)) * rstd)
+    return np.concatenate(out, 1).reshape(M, -1), dg[0], dg[1]
+
+
+def e4m3_code(top):
+    """Byte of the smallest power of two 2^(b - 127), b >= 16, whose 448-fold is not below `top`; 127 for 0."""
+    top = np.asarray(top, dtype=np.float64)
+    part, e = np.frexp(np.where(top > 0, top, 1.0))
+    return np.where(top > 0, np.maximum(e - 9 + (part > 0.875) + 127, 16), 127)
+
+
+def to_e4m3(u):
+    """Numbers of at most 448 to the nearest e4m3 number, ties to the even one: 3 bits behind the first, from 2^-6 down in steps of 2^-9."""
+    step = np.ldexp(1.0, np.maximum(np.frexp(u)[1] - 1, -6) - 3)
+    return np.rint(u / step) * step
+
+
+def heads_to_8_bits(x):
+    """e4m3 numbers and bytes of heads x [..., d]: values above the type's range of the head's largest finite one, NaN for what is not finite."""
+    fine = np.isfinite(x)
+    code = e4m3_code(np.where(fine, np.abs(x), 0.0).max(-1))
+    u = np.where(fine, x, 0.0) * np.ldexp(1.0, 127 - code)[..., None]
+    return np.where(fine, to_e4m3(u), np.nan), code
+
+
+def attn_chunk(Q, K, V, starts, table, lengths, max_new, max_len, q_off, kv_off, group):
+    """Attention of each sequence's newest rows over its pages (K, V [pages, kv_cnt, page, d] as numbers): C [M, q_cnt d], LSE [q_cnt, M], A [M, q_cnt d] =
+    sum p |V| / sum p, and which rows are written."""
+    M = Q.shape[0]
+    pages, _, page, d = K.shape
+    q_cnt = Q.shape[1] // d
+    C, A, LSE, written = np.zeros((M, q_cnt, d)), np.zeros((M, q_cnt, d)), np.full((q_cnt, M), -np.inf), np.zeros(M, dtype=bool)
+    if starts is None:
+        starts = list(range(M + 1))
+    for s in range(len(lengths)):
+        lo, hi = (min(max(int(x), 0), M) for x in starts[s:s + 2])
+        n = max(hi - lo, 0)
+        rows = min(n, max_new)
+        written[lo:lo + rows] = True
+        length = min(int(lengths[s]), max_len)
+        at = np.arange(max(length, 0))
+        p_of = np.asarray(table[s], dtype=np.int64)[at // page] if len(at) else at
+        there = (p_of >= 0) & (p_of < pages)
+        at, p_of = at[there], p_of[there]
+        if rows == 0 or len(at) == 0:
+            continue
+        seen = at[None, :] <= (length - n + np.arange(rows))[:, None]
+        for j in range(q_cnt):
+            g = (q_off + j) // group - kv_off
+            k, v = K[p_of, g, at % page].astype(np.float64), V[p_of, g, at % page].astype(np.float64)
+            score = np.where(seen, Q[lo:lo + rows, j * d:(j + 1) * d] @ k.T / np.sqrt(d), -np.inf)
+            top = score.max(1, keepdims=True)
+            top = np.where(np.isneginf(top), 0.0, top)
+            w = np.exp(score - top)
+            total = w.sum(1)
+            inv = np.where(total > 0, 1.0 / np.where(total > 0, total, 1.0), 0.0)[:, None]
+            C[lo:lo + rows, j], A[lo:lo + rows, j] = w @ v * inv, w @ np.abs(v) * inv
+            with np.errstate(divide="ignore"):
+                LSE[j, lo:lo + rows] = top[:, 0] + np.log(total)
+    return C.reshape(M, -1), LSE, A.reshape(M, -1), written

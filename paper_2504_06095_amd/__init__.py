@@ -13,4 +13,5 @@ from .binding import (  # noqa: F401
     ntp_mlp_shard_fwd, ntp_reshard_grad, ntp_reshard_segments, ntp_set_workspace, ntp_shard_plan, ntp_version, tensor_spec,
     Handle, default_handle, ntp_create, ntp_destroy, ntp_device_info, ntp_set_option, ntp_workspace_bytes, ntp_attn_proj_shard_fwd_static, ntp_replica_sum, ntp_probe_rates,
     block_norm_shape, ntp_block_norm_fwd, ntp_block_norm_bwd, kv_cache, kv_append_shape, ntp_kv_append_shard, attn_decode_shape, ntp_attn_decode_shard,
+    kv_pages, qk_norm, ntp_qk_norm_append_shard, ntp_qk_norm_shard_bwd, attn_chunk_shape, ntp_attn_chunk_shard,
 )

@@ -47,6 +47,8 @@ NTP_CALL_ATTN_PROJ_SHARD = 1
 NTP_CALL_ATTN_CORE_SHARD = 2
 NTP_CALL_BLOCK_NORM = 3
 NTP_CALL_ATTN_DECODE_SHARD = 4
+NTP_CALL_QK_NORM = 5
+NTP_CALL_ATTN_CHUNK_SHARD = 6
 # NTP_OPT_GEMM_TILE values by name
 GEMM_TILES = {"auto": 0, "generic": 1, "256x256": 2, "256x224": 3, "224x256": 4, "256x192": 5, "192x256": 6,
               "256x128": 7, "128x256": 8, "128x128": 9, "128x128w8": 10}
@@ -57,6 +59,8 @@ NTP_NORM_LAYER = 1
 NTP_GATE_NONE = 0
 NTP_GATE_CHANNEL = 1
 NTP_GATE_TOKEN = 2
+NTP_KV_BF16 = 0
+NTP_KV_E4M3 = 1
 NTP_KIND_PLAIN = 0
 NTP_KIND_QKV_GQA = 1
 
@@ -70,6 +74,7 @@ EXPORTS = (
     "ntp_set_workspace", "ntp_gemm_choice", "ntp_attn_core_choice", "ntp_create", "ntp_destroy", "ntp_device_info",
     "ntp_set_option", "ntp_workspace_bytes", "ntp_attn_proj_shard_fwd_static", "ntp_replica_sum", "ntp_probe_rates", "ntp_attn_core_bwd_rows",
     "ntp_block_norm_fwd", "ntp_block_norm_bwd", "ntp_kv_append_shard", "ntp_attn_decode_shard",
+    "ntp_qk_norm_append_shard", "ntp_qk_norm_shard_bwd", "ntp_attn_chunk_shard",
 )
 
 
@@ -139,6 +144,19 @@ class KvAppendShape(C.Structure):
 
 class AttnDecodeShape(C.Structure):
     _fields_ = [(n, C.c_int32) for n in ("n_seq", "max_len", "q_cnt", "kv_cnt", "q_off", "kv_off", "group", "head_dim")]
+
+
+class KvPages(C.Structure):
+    _fields_ = ([(n, C.c_void_p) for n in ("K", "V", "K_exp", "V_exp")] + [(n, C.c_int64) for n in ("n_pages", "page_stride", "exp_stride")]
+                + [(n, C.c_int32) for n in ("page_size", "format")])
+
+
+class QkNorm(C.Structure):
+    _fields_ = [("q_gamma", C.c_void_p), ("k_gamma", C.c_void_p), ("eps", C.c_float)]
+
+
+class AttnChunkShape(C.Structure):
+    _fields_ = [("M", C.c_int64)] + [(n, C.c_int32) for n in ("n_seq", "max_new", "max_len", "q_cnt", "kv_cnt", "q_off", "kv_off", "group", "head_dim")]
 
 
 class RowSegment(C.Structure):
@@ -217,6 +235,10 @@ def lib() -> C.CDLL:
         L.ntp_block_norm_bwd.argtypes = [vp, normp, weightp] + [vp, i64] * 4 + [vp] + [vp, i64] * 2 + [C.POINTER(BlockNormGrads), C.c_int32, vp]
         L.ntp_kv_append_shard.argtypes = [vp, C.POINTER(KvAppendShape), cachep, vp, i64, vp, vp, vp, vp, i64, vp, i64, vp]
         L.ntp_attn_decode_shard.argtypes = [vp, C.POINTER(AttnDecodeShape), cachep, vp, i64, vp, i64, vp, vp, i64, vp, vp]
+        pagesp, normqp, appendp = C.POINTER(KvPages), C.POINTER(QkNorm), C.POINTER(KvAppendShape)
+        L.ntp_qk_norm_append_shard.argtypes = [vp, appendp, normqp, pagesp, vp, i64, vp, vp, vp, vp, i64, vp, i64, vp]
+        L.ntp_qk_norm_shard_bwd.argtypes = [vp, appendp, normqp] + [vp, i64] * 3 + [vp, vp, vp, i64, vp, vp, C.c_int32, vp]
+        L.ntp_attn_chunk_shard.argtypes = [vp, C.POINTER(AttnChunkShape), pagesp, vp, i64, vp, vp, i64, vp, vp, i64, vp, vp]
         L.ntp_kernel_timing_enable.argtypes = [vp, C.c_int32]
         L.ntp_kernel_timing_read.argtypes = [vp, C.POINTER(KernelTime), i64, C.POINTER(i64)]
         L.ntp_calibration_copy.argtypes = [vp, vp, vp, i64, vp]
@@ -578,6 +600,95 @@ def ntp_attn_decode_shard(shape: AttnDecodeShape, cache: KvCache, Q, block_table
     t, ldt = _rows(block_table, torch.int32, n, block_table.size(1), "block_table")
     _check(lib().ntp_attn_decode_shard(_h(handle), C.byref(shape), C.byref(cache), *_rows(Q, bf, n, w, "Q"), t, ldt, _vec(lengths, torch.int32, n),
                                        *_rows(C_, bf, n, w, "C_"), _vec(LSE, torch.float32, n * shape.q_cnt), _stream()), "ntp_attn_decode_shard")
+
+
+def kv_pages(K, V, K_exp=None, V_exp=None) -> KvPages:
+    """The paged cache in either format: K, V [n_pages, kv_cnt, page_size, head_dim] device tensors as for kv_cache, bf16, or float8_e4m3fn with the
+    tokens' powers of two K_exp, V_exp [n_pages, kv_cnt, page_size] (float8_e8m0fnu or uint8).  The tensors must outlive it."""
+    torch = _torch or _bind_torch()
+    fp8 = K.dtype is torch.float8_e4m3fn
+    for t in (K, V):
+        if t.dtype is not (torch.float8_e4m3fn if fp8 else torch.bfloat16):
+            raise TypeError(f"expected {torch.bfloat16}, or {torch.float8_e4m3fn} for both, got {t.dtype}")
+    if fp8 != (K_exp is not None) or fp8 != (V_exp is not None):
+        raise ValueError("8-bit keys and values, and only they, have powers of two")
+    for t, dims in ((K, 4), (V, 4), (K_exp, 3), (V_exp, 3)):
+        if t is not None and (not t.is_cuda or t.dim() != dims or (t.shape[0] > 0 and not t[0].is_contiguous())):
+            raise ValueError("expected device tensors [n_pages, kv_cnt, page_size, head_dim] (powers of two: without head_dim), contiguous inside a page")
+    if K.shape != V.shape or (K.shape[0] > 1 and K.stride(0) != V.stride(0)):
+        raise ValueError("K and V must have the same shape and the same distance between pages")
+    n, g, p, d = K.shape
+    c = KvPages(K.data_ptr() if n else None, V.data_ptr() if n else None, None, None, n, K.stride(0) if n > 1 else g * p * d, 0, p, NTP_KV_E4M3 if fp8 else NTP_KV_BF16)
+    if fp8:
+        for t in (K_exp, V_exp):
+            if t.dtype not in (torch.uint8, torch.float8_e8m0fnu):
+                raise TypeError(f"expected {torch.float8_e8m0fnu} or {torch.uint8}, got {t.dtype}")
+            if t.shape != K.shape[:3] or (n > 1 and t.stride(0) != K_exp.stride(0)):
+                raise ValueError("the powers of two must have K's shape without head_dim and the same distance between pages")
+        c.K_exp, c.V_exp, c.exp_stride = K_exp.data_ptr() if n else None, V_exp.data_ptr() if n else None, K_exp.stride(0) if n > 1 else g * p
+    c.kv_cnt, c.head_dim, c.tensors = g, d, (K, V, K_exp, V_exp)
+    return c
+
+
+def qk_norm(q_gamma=None, k_gamma=None, eps: float = 1e-6) -> QkNorm:
+    """Norms of the query and key heads: bf16 device tensors [head_dim], None: no norm on those heads.  The tensors must outlive it."""
+    torch = _torch or _bind_torch()
+    n = QkNorm(*(None if t is None else _vec(t, torch.bfloat16, t.numel()) for t in (q_gamma, k_gamma)), eps)
+    n.sizes, n.tensors = {t.numel() for t in (q_gamma, k_gamma) if t is not None}, (q_gamma, k_gamma)
+    return n
+
+
+def _fits_norm(norm, shape):
+    if norm is not None and norm.sizes - {shape.head_dim}:
+        raise ValueError(f"norm: expected weights of {shape.head_dim} elements")
+    return C.byref(norm) if norm is not None else None
+
+
+def ntp_qk_norm_append_shard(shape: KvAppendShape, norm: QkNorm | None, pages: KvPages | None, QKV, positions, slots, inv_freq, Qout=None, Kout=None,
+                             handle=None) -> None:
+    """ntp_kv_append_shard with a norm of every query and key head before its rotation, into pages of either format."""
+    torch = _torch or _bind_torch()
+    bf, M, d = torch.bfloat16, shape.M, shape.head_dim
+    if pages is not None:
+        _fits_cache(pages, shape)
+    wq, wk = shape.q_cnt * d, shape.kv_cnt * d
+    _check(lib().ntp_qk_norm_append_shard(_h(handle), C.byref(shape), _fits_norm(norm, shape), C.byref(pages) if pages is not None else None,
+                                          *_rows(QKV, bf, M, wq + 2 * wk, "QKV"), _vec(positions, torch.int32, M), _vec(slots, torch.int64, M),
+                                          _vec(inv_freq, torch.float64, shape.rotary_dim // 2), *_rows(Qout, bf, M, wq, "Qout"), *_rows(Kout, bf, M, wk, "Kout"),
+                                          _stream()), "ntp_qk_norm_append_shard")
+
+
+def ntp_qk_norm_shard_bwd(shape: KvAppendShape, norm: QkNorm | None, QKV, dQ, dK, positions, inv_freq, dQKV, d_q_gamma=None, d_k_gamma=None,
+                          accumulate: bool = False, handle=None) -> None:
+    """Gradient of the norms and the rotation: dQ [M, q_cnt d] and dK [M, kv_cnt d] at their outputs -> the query and key columns of dQKV, in QKV's layout, and
+    the fp32 [d] gradients of the norms' weights that are given."""
+    torch = _torch or _bind_torch()
+    bf, f32, M, d = torch.bfloat16, torch.float32, shape.M, shape.head_dim
+    wq, wk = shape.q_cnt * d, shape.kv_cnt * d
+    _check(lib().ntp_qk_norm_shard_bwd(_h(handle), C.byref(shape), _fits_norm(norm, shape), *_rows(QKV, bf, M, wq + 2 * wk, "QKV"), *_rows(dQ, bf, M, wq, "dQ"),
+                                       *_rows(dK, bf, M, wk, "dK"), _vec(positions, torch.int32, M), _vec(inv_freq, torch.float64, shape.rotary_dim // 2),
+                                       *_rows(dQKV, bf, M, wq + 2 * wk, "dQKV"), _vec(d_q_gamma, f32, d), _vec(d_k_gamma, f32, d), int(bool(accumulate)), _stream()),
+           "ntp_qk_norm_shard_bwd")
+
+
+def attn_chunk_shape(M, n_seq, max_new, max_len, plan: dict, group: int) -> AttnChunkShape:
+    """Shape of the attention call of chunks of new tokens (M rows in all, at most max_new of a sequence), from a rank's ntp_attn_shard_plan and the query heads per
+    KV head."""
+    return AttnChunkShape(M, n_seq, max_new, max_len, plan["q_cnt"], plan["kv_cnt"], plan["q_off"], plan["kv_off"], group, plan["head_dim"])
+
+
+def ntp_attn_chunk_shard(shape: AttnChunkShape, pages: KvPages, Q, row_starts, block_table, lengths, C_, LSE=None, handle=None) -> None:
+    """Rows row_starts[s] .. row_starts[s + 1] - 1 (int32 [n_seq + 1]; None: row s alone) of Q [M, q_cnt d] bf16 are sequence s's newest tokens, of lengths[s] (int32 [n_seq])
+    in the pages that block_table (int32 [n_seq, >= pages of max_len]) names -> C_ [M, q_cnt d] bf16 and LSE [q_cnt, M] fp32 (optional)."""
+    torch = _torch or _bind_torch()
+    bf, n, M, w = torch.bfloat16, shape.n_seq, shape.M, shape.q_cnt * shape.head_dim
+    _fits_cache(pages, shape)
+    if block_table.size(0) != n or block_table.size(1) * pages.page_size < shape.max_len:
+        raise ValueError(f"block_table: expected {n} rows of at least {-(-shape.max_len // pages.page_size)} pages, got {tuple(block_table.size())}")
+    t, ldt = _rows(block_table, torch.int32, n, block_table.size(1), "block_table")
+    _check(lib().ntp_attn_chunk_shard(_h(handle), C.byref(shape), C.byref(pages), *_rows(Q, bf, M, w, "Q"), _vec(row_starts, torch.int32, n + 1), t, ldt,
+                                      _vec(lengths, torch.int32, n), *_rows(C_, bf, M, w, "C_"), _vec(LSE, torch.float32, M * shape.q_cnt), _stream()),
+           "ntp_attn_chunk_shard")
 
 
 def ntp_reshard_row_segments(spec: TensorSpec, src_tp: int, src_rank: int, dst_tp: int, dst_shards):

@@ -119,6 +119,9 @@ int attn_core_workspace_wish(const ntp_handle* h, const ntp_attn_core_shape_t* s
 // Largest workspace that a backward call of the block norms, or an attention call of one new token, of this shape could use.
 int block_norm_workspace_wish(const ntp_handle* h, const ntp_block_norm_shape_t* s, int64_t* bytes);
 int attn_decode_workspace_wish(const ntp_handle* h, const ntp_attn_decode_shape_t* s, int64_t* bytes);
+// The same for the gradient of the norms of query and key heads, and the attention of chunks of new tokens.
+int qk_norm_workspace_wish(const ntp_handle* h, const ntp_kv_append_shape_t* s, int64_t* bytes);
+int attn_chunk_workspace_wish(const ntp_handle* h, const ntp_attn_chunk_shape_t* s, int64_t* bytes);
 // deep: false for the choice without the deep-pipelined kernel.
 int64_t gemm_workspace_wish(const ntp_handle* h, int layout, int64_t M, int64_t N, int64_t n_store, int64_t K, bool deep = true);
 

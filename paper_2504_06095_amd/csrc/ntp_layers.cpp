@@ -290,6 +290,12 @@ extern "C" int ntp_workspace_bytes(const ntp_handle_t* h, int32_t call, const vo
   } else if (call == NTP_CALL_ATTN_DECODE_SHARD) {
     const int st = ntp::attn_decode_workspace_wish(h, static_cast<const ntp_attn_decode_shape_t*>(shape), &need);
     if (st != NTP_OK) return st;
+  } else if (call == NTP_CALL_QK_NORM) {
+    const int st = ntp::qk_norm_workspace_wish(h, static_cast<const ntp_kv_append_shape_t*>(shape), &need);
+    if (st != NTP_OK) return st;
+  } else if (call == NTP_CALL_ATTN_CHUNK_SHARD) {
+    const int st = ntp::attn_chunk_workspace_wish(h, static_cast<const ntp_attn_chunk_shape_t*>(shape), &need);
+    if (st != NTP_OK) return st;
   } else {
     return NTP_ERR_INVALID_ARG;
   }
