@@ -1,77 +1,63 @@
-// Attention of chunks of new tokens over the paged cache (ntp_attn_chunk_shard).
+// Attention of chunks of new tokens over the paged cache (ntp_attn_chunk_shard): row i of a sequence's n new ones sees its first len - n + i + 1 tokens,
+//   C[row, j] = sum_t p_t V[t] / sum_t p_t,   p_t = exp(q_j . K[t] / sqrt(d) - max).
+// One pass over the tokens with a running maximum and sum.  Sequences of up to 32 rows (new tokens x query heads of a KV head) are bound by HBM and go by
+// ntp_attn_chunk_rows.h, the others by the matrix instructions and by ntp_attn_chunk_tiles.h; one launch holds workgroups of both kinds, since which sequences are which only the device
+// knows, and one more joins what was cut.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
 #include <cmath>
 #include <cstdint>
 
-#include "ntp_gemm_kernels.h"
+#include "ntp_attn_chunk_rows.h"
+#include "ntp_attn_chunk_tiles.h"
 #include "ntp_internal.h"
 #include "ntp_kv_cache.h"
 
 namespace {
 
+using namespace ntp_chunk;
 using ntp::off16;
 
-struct ChunkArgs {
-  const uint16_t* Q;
-  const unsigned char *K, *V;
-  const uint8_t *K_exp, *V_exp;
-  const int32_t *starts, *table, *lengths;
-  uint16_t* C;
-  float* LSE;
-  int64_t M, ldq, ldc, ldt, page_stride, exp_stride;
-  int32_t n_pages, n_seq, max_new, max_len, q_cnt, q_off, kv_off, group, page_size, page_log2;
-  float scale_log2;
-};
+template <int D, bool FP8, int QB>
+__global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2))) void chunk_rows_kernel(const ChunkArgs a) {
+  __shared__ __attribute__((aligned(1024))) unsigned char lds[kRowLds<D, QB>];
+  chunk_rows<D, FP8, QB>(a, int(blockIdx.x), lds);
+}
 
 template <int D, bool FP8>
-__global__ __launch_bounds__(256) void attn_chunk_plain_kernel(const ChunkArgs a) {
-  constexpr int N = D / 64;
-  const int lane = threadIdx.x & 63;
-  const int64_t id = int64_t(blockIdx.x) * 4 + (threadIdx.x >> 6);
-  if (id >= a.M * a.q_cnt) return;
-  const int64_t row = id / a.q_cnt;
-  const int head = int(id % a.q_cnt), g = (a.q_off + head) / a.group - a.kv_off;
-  int s = -1, start = 0, n = 0;
-  if (!a.starts) s = int(row), start = int(row), n = 1;
-  else
-    for (int i = 0; i < a.n_seq; ++i) {
-      const int64_t lo = std::min<int64_t>(std::max(a.starts[i], 0), a.M), hi = std::min<int64_t>(std::max(a.starts[i + 1], 0), a.M);
-      if (row >= lo && row < hi) s = i, start = int(lo), n = int(hi - lo);
+__global__ __attribute__((amdgpu_flat_work_group_size(kThreads, kThreads), amdgpu_waves_per_eu(2, 2))) void chunk_both_kernel(const ChunkArgs a) {
+  __shared__ __attribute__((aligned(1024))) unsigned char lds[std::max(kRowLds<D, 2>, kTileLds<D>)];
+  if (int(blockIdx.x) < a.row_wgs) chunk_rows<D, FP8, 2>(a, int(blockIdx.x), lds);
+  else chunk_tiles<D, FP8>(a, int(blockIdx.x) - a.row_wgs, lds);
+}
+
+template <int D, bool FP8>
+__global__ __attribute__((amdgpu_flat_work_group_size(kThreads, kThreads), amdgpu_waves_per_eu(2, 2))) void chunk_tiles_kernel(const ChunkArgs a) {
+  __shared__ __attribute__((aligned(1024))) unsigned char lds[kTileLds<D>];
+  chunk_tiles<D, FP8>(a, int(blockIdx.x), lds);
+}
+
+// Workgroups: first those of the line's units, then those of the row tiles.
+struct Joins {
+  int32_t rows, row_jobs, lengthy;  // rows of a unit; workgroups for the units; few units of many parts
+};
+template <int D, bool FP8, int QB>
+__global__ __launch_bounds__(kThreads) void chunk_join_kernel(const ChunkArgs a, const Joins j) {
+  constexpr int STEP = RowFormat<D, FP8, QB>::STEP, R = 16 * QB;
+  const int wg = int(blockIdx.x);
+  if (wg < j.row_jobs) {
+    constexpr int SPLIT = D / kFewColumns, AT_ONCE = kThreads / (D / 4);
+    if (j.lengthy) {
+      chunk_rows_join_long<D, STEP, R>(a, wg / SPLIT / j.rows, wg / SPLIT % j.rows, wg % SPLIT * kFewColumns);
+    } else {
+      const int per = (j.rows + AT_ONCE - 1) / AT_ONCE;
+      chunk_rows_join_short<D, STEP, R>(a, wg / per, wg % per * AT_ONCE);
     }
-  if (s < 0 || row - start >= a.max_new) return;
-  const int seen = std::min(a.lengths[s], a.max_len) - n + int(row - start) + 1;
-  float q[N], acc[N];
-  for (int i = 0; i < N; ++i) q[i] = __builtin_bit_cast(float, uint32_t(a.Q[row * a.ldq + int64_t(head) * D + lane * N + i]) << 16), acc[i] = 0.f;
-  float m = -INFINITY, l = 0.f;
-  for (int t = 0; t < seen; ++t) {
-    const int page = a.table[int64_t(s) * a.ldt + (t >> a.page_log2)];
-    if (page < 0 || page >= a.n_pages) continue;
-    const int64_t in = int64_t(g) * a.page_size + (t & (a.page_size - 1)), at = int64_t(page) * a.page_stride + in * D + lane * N;
-    float k[N], v[N];
-    for (int i = 0; i < N; ++i) {
-      if constexpr (FP8) {
-        const uint32_t e = a.K_exp[int64_t(page) * a.exp_stride + in], f = a.V_exp[int64_t(page) * a.exp_stride + in];
-        k[i] = __builtin_amdgcn_cvt_f32_fp8(a.K[at + i], 0) * __builtin_bit_cast(float, e << 23);
-        v[i] = __builtin_amdgcn_cvt_f32_fp8(a.V[at + i], 0) * __builtin_bit_cast(float, f << 23);
-      } else {
-        k[i] = __builtin_bit_cast(float, uint32_t(reinterpret_cast<const uint16_t*>(a.K)[at + i]) << 16);
-        v[i] = __builtin_bit_cast(float, uint32_t(reinterpret_cast<const uint16_t*>(a.V)[at + i]) << 16);
-      }
-    }
-    float x = 0.f;
-    for (int i = 0; i < N; ++i) x = fmaf(q[i], k[i], x);
-    for (int d = 1; d < 64; d *= 2) x += __shfl_xor(x, d);
-    x *= a.scale_log2;
-    const float mn = fmaxf(m, x), use = mn == -INFINITY ? 0.f : mn, al = exp2f(m - use), p = exp2f(x - use);
-    l = l * al + p;
-    for (int i = 0; i < N; ++i) acc[i] = acc[i] * al + p * v[i];
-    m = mn;
+  } else {
+    constexpr int PER = kTileRows / (kThreads / (D / 8));
+    chunk_tiles_join<D>(a, (wg - j.row_jobs) / PER, (wg - j.row_jobs) % PER);
   }
-  const float inv = l == 0.f ? 0.f : 1.0f / l;
-  for (int i = 0; i < N; ++i) a.C[row * a.ldc + int64_t(head) * D + lane * N + i] = ntp_gemm::f32_to_bf16(acc[i] * inv);
-  if (lane == 0 && a.LSE) a.LSE[int64_t(head) * a.M + row] = (m == -INFINITY ? -INFINITY : m + log2f(l)) * 0.6931471805599453f;
 }
 
 int check_chunk_shape(const ntp_attn_chunk_shape_t* s) {
@@ -88,13 +74,79 @@ int check_chunk_shape(const ntp_attn_chunk_shape_t* s) {
   return NTP_OK;
 }
 
+struct ChunkChoice {
+  int32_t kv_first, kv_used, gmax, cap, qb;
+  int32_t row_wgs, shares, rows;    // workgroups that take sequences of few rows; shares of their line (0: workgroup = unit); most rows of a unit
+  int64_t units;                    // such units at most
+  int64_t tiles;                    // (sequence, KV head, row tile)s of the others at most
+  int32_t slots;                    // pieces that these are cut into where they are fewer (0: never)
+  int64_t ws_rows, ws_bytes;        // bytes of the line's partial results, and of all
+};
+
+ChunkChoice choose_chunk(const ntp_handle* h, int64_t ws_bytes, const ntp_attn_chunk_shape_t* s) {
+  ChunkChoice c{};
+  const int64_t most = std::min<int64_t>(s->max_new, s->M);  // rows of a sequence
+  if (s->q_cnt == 0 || s->n_seq == 0 || most == 0) return c;
+  c.kv_first = s->q_off / s->group - s->kv_off;
+  c.kv_used = (s->q_off + s->q_cnt - 1) / s->group - s->kv_off - c.kv_first + 1;
+  c.gmax = std::min(s->group, s->q_cnt);
+  c.qb = most * c.gmax <= 16 ? 1 : 2;
+  const bool tiles = most * c.gmax > 32;
+  c.cap = tiles && (s->n_seq == 1 || c.gmax > 32) ? 0 : 16 * c.qb;
+  if (c.cap > 0) {
+    c.units = int64_t(s->n_seq) * c.kv_used;
+    c.rows = int32_t(std::min<int64_t>(c.cap, most * c.gmax));
+  }
+  if (tiles) {
+    const int64_t all = s->M * c.gmax;
+    c.tiles = c.kv_used * std::min<int64_t>(s->n_seq * ((most * c.gmax + kTileRows - 1) / kTileRows), all / kTileRows + std::min<int64_t>(s->n_seq, all / (c.cap + 1)));
+  }
+  const int64_t step = (s->head_dim == 128 ? 128 : 256), steps = std::max<int64_t>((s->max_len + step - 1) / step, 1);  // (8-bit steps of up to 16 rows are twice as long)
+  if (c.units > 0 && steps > 4 && (steps > 8 || c.units < h->compute_units / 2)) {
+    c.shares = int32_t(std::min<int64_t>(std::min(2 * int64_t(h->compute_units), steps * c.units), kMaxShares));
+    c.ws_rows = (int64_t(c.shares) * 2 * c.cap * (s->head_dim + 2) * 4 + 255) / 256 * 256;
+  }
+  if (c.tiles > 0 && s->max_len > kMinPiece * kTileKeys) c.slots = 2 * h->compute_units;
+  c.ws_bytes = c.ws_rows + int64_t(c.slots > 0 ? c.slots + 8 : 0) * kTileRows * (s->head_dim + kPartPad) * 4;
+  if (c.ws_bytes > ws_bytes) c.shares = c.slots = 0, c.ws_rows = c.ws_bytes = 0;
+  c.row_wgs = int32_t(c.shares > 0 ? c.shares : c.units);
+  if (tiles) c.row_wgs = (c.row_wgs + 7) / 8 * 8;  // (the row tiles' workgroups keep their XCDs)
+  return c;
+}
+
 }  // namespace
 
 int ntp::attn_chunk_workspace_wish(const ntp_handle* h, const ntp_attn_chunk_shape_t* s, int64_t* bytes) {
   if (check_chunk_shape(s) != NTP_OK) return NTP_ERR_INVALID_ARG;
-  *bytes = 0;
+  *bytes = choose_chunk(h, INT64_MAX, s).ws_bytes;
   return NTP_OK;
 }
+
+namespace {
+
+template <int D, bool FP8>
+bool launch_chunk(const ChunkArgs& a, const ChunkChoice& c, hipStream_t hs) {
+  const int64_t tile_wgs = c.tiles > 0 ? std::max<int64_t>(c.tiles, c.slots > 0 ? c.slots + 8 : 0) : 0;
+  const dim3 grid{uint32_t(c.row_wgs + tile_wgs)}, block{kThreads};
+  if (c.tiles > 0 && c.cap > 0) hipLaunchKernelGGL((chunk_both_kernel<D, FP8>), grid, block, 0, hs, a);
+  else if (c.tiles > 0) hipLaunchKernelGGL((chunk_tiles_kernel<D, FP8>), grid, block, 0, hs, a);
+  else if (c.qb == 1) hipLaunchKernelGGL((chunk_rows_kernel<D, FP8, 1>), grid, block, 0, hs, a);
+  else hipLaunchKernelGGL((chunk_rows_kernel<D, FP8, 2>), grid, block, 0, hs, a);
+  if (hipGetLastError() != hipSuccess) return false;
+  if (c.shares <= 1 && c.slots == 0) return true;
+  Joins j{c.rows, 0, c.shares >= 32 * c.units};
+  if (c.shares > 1) {
+    constexpr int AT_ONCE = kThreads / (D / 4);
+    j.row_jobs = int32_t(j.lengthy ? c.units * c.rows * (D / kFewColumns) : int64_t(c.shares - 1) * ((c.rows + AT_ONCE - 1) / AT_ONCE));
+  }
+  const int64_t tile_jobs = c.slots > 0 ? std::min<int64_t>(c.slots, c.tiles) * (kTileRows / (kThreads / (D / 8))) : 0;
+  const dim3 jobs{uint32_t(j.row_jobs + tile_jobs)};
+  if (c.qb == 1) hipLaunchKernelGGL((chunk_join_kernel<D, FP8, 1>), jobs, block, 0, hs, a, j);
+  else hipLaunchKernelGGL((chunk_join_kernel<D, FP8, 2>), jobs, block, 0, hs, a, j);
+  return hipGetLastError() == hipSuccess;
+}
+
+}  // namespace
 
 extern "C" int ntp_attn_chunk_shard(ntp_handle_t* h, const ntp_attn_chunk_shape_t* s, const ntp_kv_pages_t* pages, const void* Q, int64_t ldq, const int32_t* row_starts,
                                     const int32_t* block_table, int64_t ldt, const int32_t* lengths, void* C, int64_t ldc, float* LSE, void* stream) {
@@ -108,23 +160,26 @@ extern "C" int ntp_attn_chunk_shard(ntp_handle_t* h, const ntp_attn_chunk_shape_
   auto off4 = [](const void* p) { return (reinterpret_cast<uintptr_t>(p) & 3) != 0; };
   if (off16(Q) || off16(C) || ldq % 8 || ldc % 8 || off4(row_starts) || off4(block_table) || off4(lengths) || off4(LSE)) return NTP_ERR_ALIGNMENT;
   if (h->device < 0) return NTP_ERR_NO_DEVICE;
+  const ChunkChoice c = choose_chunk(h, h->workspace ? h->workspace_bytes : 0, s);
   ChunkArgs a{};
   a.Q = static_cast<const uint16_t*>(Q), a.K = static_cast<const unsigned char*>(pages->K), a.V = static_cast<const unsigned char*>(pages->V);
   a.K_exp = static_cast<const uint8_t*>(pages->K_exp), a.V_exp = static_cast<const uint8_t*>(pages->V_exp);
   a.starts = row_starts, a.table = block_table, a.lengths = lengths, a.C = static_cast<uint16_t*>(C), a.LSE = LSE;
-  a.M = s->M, a.ldq = ldq, a.ldc = ldc, a.ldt = ldt, a.page_stride = pages->page_stride, a.exp_stride = pages->exp_stride, a.n_pages = int32_t(pages->n_pages);
-  a.n_seq = s->n_seq, a.max_new = s->max_new, a.max_len = s->max_len, a.q_cnt = s->q_cnt, a.q_off = s->q_off, a.kv_off = s->kv_off, a.group = s->group;
-  a.page_size = pages->page_size, a.page_log2 = ntp::log2_of(pages->page_size);
+  if (c.shares > 0) {
+    a.part_rows = static_cast<float*>(h->workspace);
+    a.part_sums = reinterpret_cast<float2*>(a.part_rows + int64_t(c.shares) * 2 * c.cap * s->head_dim);
+  }
+  if (c.slots > 0) a.tile_parts = reinterpret_cast<float*>(static_cast<char*>(h->workspace) + c.ws_rows);
+  a.ldq = ldq, a.ldc = ldc, a.ldt = ldt, a.page_stride = pages->page_stride, a.exp_stride = pages->exp_stride;
+  a.M = int32_t(s->M), a.n_pages = int32_t(pages->n_pages), a.n_seq = s->n_seq, a.max_new = s->max_new, a.max_len = s->max_len;
+  a.q_cnt = s->q_cnt, a.q_off = s->q_off, a.kv_off = s->kv_off, a.group = s->group, a.page_size = pages->page_size, a.page_log2 = ntp::log2_of(pages->page_size);
+  a.kv_first = c.kv_first, a.kv_used = c.kv_used, a.gmax = c.gmax, a.cap = c.cap, a.shares = c.shares, a.row_wgs = c.row_wgs, a.slots = c.slots;
   a.scale_log2 = float(1.4426950408889634 / std::sqrt(double(s->head_dim)));
   hipStream_t hs = static_cast<hipStream_t>(stream);
   const bool fp8 = pages->format == NTP_KV_E4M3;
-  const dim3 grid{uint32_t((s->M * s->q_cnt + 3) / 4)};
   if (ntp::timing_on(h)) ntp::timing_begin(h, stream, fp8 ? "attn_chunk8" : "attn_chunk", 4.0 * double(s->M) * double(s->max_len) * s->head_dim * s->q_cnt, 0.0);
-  if (s->head_dim == 128 && fp8) hipLaunchKernelGGL((attn_chunk_plain_kernel<128, true>), grid, dim3(256), 0, hs, a);
-  else if (s->head_dim == 128) hipLaunchKernelGGL((attn_chunk_plain_kernel<128, false>), grid, dim3(256), 0, hs, a);
-  else if (fp8) hipLaunchKernelGGL((attn_chunk_plain_kernel<64, true>), grid, dim3(256), 0, hs, a);
-  else hipLaunchKernelGGL((attn_chunk_plain_kernel<64, false>), grid, dim3(256), 0, hs, a);
-  const bool ok = hipGetLastError() == hipSuccess;
+  const bool ok = s->head_dim == 128 ? (fp8 ? launch_chunk<128, true>(a, c, hs) : launch_chunk<128, false>(a, c, hs))
+                                     : (fp8 ? launch_chunk<64, true>(a, c, hs) : launch_chunk<64, false>(a, c, hs));
   ntp::timing_end(h, stream);
   return ok ? NTP_OK : NTP_ERR_LAUNCH;
 }

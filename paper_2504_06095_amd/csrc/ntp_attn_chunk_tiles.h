@@ -1,0 +1,500 @@
+// Chunk attention, sequences of many rows: the matrix instructions bound it.
+//
+// A workgroup takes 128 rows (token i, head h of a KV head's G: number i G + h) of a sequence and KV head, a wavefront 32 of them in two blocks of 16, and walks over the
+// tokens that they see in tiles of 64, which all wavefronts share: two buffers a matrix, one barrier a tile, two workgroups a compute unit.  Grouped heads stand in one tile,
+// so that 16 query heads on one KV head read its tokens once and not 16 times.  bf16 tiles come by DMA, wavefront w the tile's block w of 16 tokens (a page holds at least
+// 16); 8-bit ones through registers, where they become bf16 (exact: e4m3 times a power of two) before the LDS, once for all wavefronts: converted where fragments
+// are read it would be four times the work, on the vector unit that the softmax needs.
+//
+// Where a batch has fewer tiles than the GPU has room for, walks are cut into pieces, by the lengths on the device, whose partial results a second kernel joins.
+#ifndef NTP_ATTN_CHUNK_TILES_H_
+#define NTP_ATTN_CHUNK_TILES_H_
+
+#include "ntp_attn_chunk.h"
+
+namespace ntp_chunk {
+
+constexpr int kMinPiece = 4;    // tiles of a piece at least
+constexpr int kPartPad = 4;     // floats behind a partial row's outputs: maximum, sum
+
+// Row tiles and key tiles (of its last row) of a sequence; no row tiles where it is one of few rows.
+__device__ __forceinline__ void tiles_of(const ChunkArgs& a, int n, int len, int& tiles, int& walk) {
+  const int used = min(n, a.max_new);
+  tiles = used > a.cap / a.gmax ? int((int64_t(used) * a.gmax + kTileRows - 1) / kTileRows) : 0;
+  walk = max(1, (max(len - n + used, 0) + kTileKeys - 1) / kTileKeys);
+}
+
+// How the batch's walks are cut, and the piece with number x of them.  Pieces are numbered sequence by sequence, in it KV head by KV head, row tile by row tile from the last
+// (the longest walk) on; all tiles of a sequence are cut into the same number.
+struct TilePlan {
+  int units, total, piece_tiles;  // (sequence, KV head, row tile)s; pieces; key tiles of a piece at most
+  // this lane's sequence of 64
+  int start, n, len, tiles, walk;
+  __device__ __forceinline__ void load(const ChunkArgs& a, int i) {
+    start = n = len = tiles = 0, walk = 1;
+    if (i < a.n_seq) {
+      extent(a, i, start, n, len);
+      tiles_of(a, n, len, tiles, walk);
+    }
+  }
+  __device__ __forceinline__ int cut() const { return piece_tiles == 0 ? 1 : (walk + piece_tiles - 1) / piece_tiles; }
+  __device__ __forceinline__ static float sum_all(float v) {
+#pragma unroll
+    for (int d = 1; d < 64; d *= 2) v += __shfl_xor(v, d);
+    return v;
+  }
+  __device__ __forceinline__ int pieces(const ChunkArgs& a) {  // of the whole batch
+    int sum = 0;
+    for (int from = 0; from < a.n_seq; from += 64) {
+      if (a.n_seq > 64) load(a, from + int(threadIdx.x & 63));
+      sum += a.kv_used * tiles * cut();
+    }
+    return __builtin_amdgcn_readlane(sum_upto(sum), 63);
+  }
+  __device__ __forceinline__ void make(const ChunkArgs& a) {
+    piece_tiles = 0;
+    int count = 0;
+    float work = 0.f;  // (exact enough: below 2^24 pieces' worth of error)
+    load(a, threadIdx.x & 63);
+    for (int from = 0; from < a.n_seq; from += 64) {
+      if (a.n_seq > 64) load(a, from + int(threadIdx.x & 63));
+      count += a.kv_used * tiles;
+      work += float(a.kv_used * tiles) * float(walk);
+    }
+    units = total = __builtin_amdgcn_readlane(sum_upto(count), 63);
+    if (units == 0 || units >= a.slots) return;
+    work = sum_all(work);
+    piece_tiles = max(kMinPiece, int(ceilf(work / float(a.slots))));
+    total = pieces(a);
+    if (total > a.slots) {  // sum of ceil(walk / piece) <= work / piece + units
+      piece_tiles = max(kMinPiece, int(ceilf(work / float(a.slots - units))));
+      total = pieces(a);
+    }
+  }
+  // x < total: its sequence, KV head, row tile (from the last on), and piece
+  int seq, head, tile, piece, n_pieces, seq_start, seq_n, seq_len;
+  __device__ __forceinline__ void find(const ChunkArgs& a, int x) {
+    int from = 0, before = 0;
+    for (;; from += 64) {
+      if (from > 0 || a.n_seq > 64) load(a, from + int(threadIdx.x & 63));
+      const int mine = a.kv_used * tiles * cut(), upto = sum_upto(mine);
+      const uint64_t behind = __ballot(before + upto > x);
+      if (behind) {
+        const int at = __builtin_ctzll(behind);
+        auto of = [&](int v) { return __builtin_amdgcn_readlane(v, at); };
+        const int t = of(tiles);
+        n_pieces = of(cut());
+        int rest = x - before - (of(upto) - of(mine));
+        piece = rest % n_pieces;
+        rest /= n_pieces;
+        head = rest / t;
+        tile = t - 1 - rest % t;
+        seq = from + at, seq_start = of(start), seq_n = of(n), seq_len = of(len);
+        return;
+      }
+      before += __builtin_amdgcn_readlane(upto, 63);
+    }
+  }
+};
+
+template <int D>
+constexpr int kTileLds = 4 * kTileKeys * D * 2;
+
+template <int D>
+__device__ __forceinline__ uint32_t tile_swz(int r) {
+  return D == 128 ? uint32_t((r & 7) << 1) : uint32_t(((r >> 1) & 3) << 1);
+}
+
+template <int D, bool FP8>
+__device__ __forceinline__ void chunk_tiles(const ChunkArgs& a, const int wg, unsigned char* const lds) {
+  constexpr int KS = D / 32, DB = D / 16, QB = 2;
+  constexpr int TILE = kTileKeys * D * 2, BLOCK = kBlock * D * 2;  // bytes in the LDS
+  constexpr int NI = BLOCK / 1024;                                 // DMA instructions per wavefront, matrix and tile
+  constexpr int NL = FP8 ? kBlock * D / 1024 : 1;                  // or loads of 16 8-bit elements a lane
+  const int lane = threadIdx.x & 63, lq = lane & 15, lh = lane >> 4;
+  const int wave = uniform(threadIdx.x >> 6);
+
+  TilePlan plan;
+  plan.make(a);
+  if (wg >= plan.total) return;
+  // neighbouring pieces, which read the same tokens, on one XCD (workgroup b runs on XCD b % 8)
+  const int per_xcd = plan.total / 8, odd = plan.total % 8, xcd = wg % 8;
+  const int id = uniform(xcd * per_xcd + min(xcd, odd) + wg / 8);
+  plan.find(a, id);
+  const int seq = uniform(plan.seq), start = uniform(plan.seq_start), n = uniform(plan.seq_n), len = uniform(plan.seq_len), used = min(n, a.max_new);
+  const int g = a.kv_first + uniform(plan.head), n_pieces = uniform(plan.n_pieces), piece = uniform(plan.piece);
+  const Heads hd(a, g);
+  const int G = uniform(hd.j1 - hd.j0), j0 = uniform(hd.j0), rows = used * G, row0 = uniform(plan.tile) * kTileRows;
+  if (row0 >= rows) return;  // (a KV head that only a part of its group reads)
+  const int end = max(len - n + (min(rows, row0 + kTileRows) - 1) / G + 1, 0);  // tokens that the tile's last row sees
+  const int walk = (end + kTileKeys - 1) / kTileKeys;
+  const int t_lo = int(int64_t(piece) * walk / n_pieces), t_hi = int(int64_t(piece + 1) * walk / n_pieces);
+
+  // this wavefront's rows: their queries, and how many tokens they see
+  const int w0 = row0 + wave * 16 * QB;
+  const int all_see = len - n + w0 / G + 1, most = w0 < rows ? len - n + (min(rows, w0 + 16 * QB) - 1) / G + 1 : 0;
+  bf16x8 qf[QB][KS];
+  int sees[QB];
+#pragma unroll
+  for (int qb = 0; qb < QB; ++qb) {
+    const int rr = w0 + qb * 16 + lq, i = rr / G, j = j0 + rr - i * G;
+    sees[qb] = rr < rows ? len - n + i + 1 : 0;
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) qf[qb][ks] = bf16x8{};
+    if (rr < rows) {
+#pragma unroll
+      for (int ks = 0; ks < KS; ++ks) qf[qb][ks] = *reinterpret_cast<const bf16x8*>(a.Q + int64_t(start + i) * a.ldq + int64_t(j) * D + ks * 32 + lh * 8);
+    }
+  }
+  f32x4 acc[QB][DB];
+  float m_run[QB], l_run[QB];
+#pragma unroll
+  for (int qb = 0; qb < QB; ++qb) {
+#pragma unroll
+    for (int db = 0; db < DB; ++db) acc[qb][db] = f32x4{0.f, 0.f, 0.f, 0.f};
+    m_run[qb] = -INFINITY, l_run[qb] = 0.f;
+  }
+
+  // Page numbers of 16 tiles' four blocks, one a lane, and which of them there are not; the next 16 tiles' are on their way.
+  const int32_t* const row_of_table = a.table + int64_t(seq) * a.ldt;
+  auto pages_from = [&](int t) {
+    const int key = (t + lane / 4) * kTileKeys + (lane & 3) * kBlock;
+    return key < end ? row_of_table[key >> a.page_log2] : 0;
+  };
+  auto missing = [&](int pg) { return __ballot(pg < 0 || pg >= a.n_pages); };
+  int32_t pages = pages_from(t_lo), pages_next = pages_from(t_lo + 16);
+  uint64_t bad = missing(pages), bad_now = bad;  // (bad_now: of the tiles that are multiplied, which follow those that are requested)
+#pragma unroll
+  for (int qb = 0; qb < QB; ++qb)
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) arrived(qf[qb][ks]);
+
+  // this wavefront's block of tile t: where it is, and how many of its tokens count
+  auto place = [&](int t, int& valid, int64_t& page, int64_t& in) {
+    const int key = t * kTileKeys + wave * kBlock;
+    const int pg = __builtin_amdgcn_readlane(pages, (((t - t_lo) & 15) << 2) + wave);
+    const bool there = pg >= 0 && pg < a.n_pages;
+    valid = uniform(there ? min(max(end - key, 0), kBlock) : 0);
+    page = there ? pg : 0;
+    in = there ? int64_t(g) * a.page_size + (key & (a.page_size - 1)) : 0;
+  };
+  auto turn_pages = [&](int t) {  // before tile t is requested
+    if (((t - t_lo) & 15) == 0 && t > t_lo) {
+      pages = pages_next;
+      arrived(pages);
+      bad = missing(pages);
+      pages_next = pages_from(t + 16);
+    }
+  };
+  unsigned char* const sK = lds;
+  unsigned char* const sV = lds + 2 * TILE;
+  uint32_t voff[NI];
+#pragma unroll
+  for (int j = 0; j < NI; ++j) {
+    const int p = j * 64 + lane, row = p / (D / 8), slot = p % (D / 8);
+    voff[j] = uint32_t(row * D * 2) + ((uint32_t(slot) ^ tile_swz<D>(row)) * 16u);
+  }
+  auto request = [&](int t, int buf) {  // bf16: by DMA
+    int valid;
+    int64_t page, in;
+    place(t, valid, page, in);
+    const int64_t at = (page * a.page_stride + in * D) * 2;
+    const __amdgpu_buffer_rsrc_t rk = view(a.K + at, valid * D * 2), rv = view(a.V + at, valid * D * 2);
+#pragma unroll
+    for (int j = 0; j < NI; ++j) {
+      dma_16_shared(rk, sK + buf * TILE + wave * BLOCK + j * 1024, voff[j]);
+      dma_16_shared(rv, sV + buf * TILE + wave * BLOCK + j * 1024, voff[j]);
+    }
+  };
+  u32x4 k8[NL], v8[NL];  // 8 bits: 16 elements of a token, and its powers of two
+  uint32_t ke[NL], ve[NL];
+  auto fetch = [&](int t) {
+    int valid;
+    int64_t page, in;
+    place(t, valid, page, in);
+    const int64_t at = page * a.page_stride + in * D, ex = page * a.exp_stride + in;
+    const __amdgpu_buffer_rsrc_t rk = view(a.K + at, valid * D), rv = view(a.V + at, valid * D), rke = view(a.K_exp + ex, valid), rve = view(a.V_exp + ex, valid);
+#pragma unroll
+    for (int j = 0; j < NL; ++j) {
+      const int p = j * 64 + lane, row = p / (D / 16);
+      k8[j] = __builtin_amdgcn_raw_buffer_load_b128(rk, p * 16, 0, 0);
+      v8[j] = __builtin_amdgcn_raw_buffer_load_b128(rv, p * 16, 0, 0);
+      ke[j] = __builtin_amdgcn_raw_buffer_load_b8(rke, row, 0, 0);
+      ve[j] = __builtin_amdgcn_raw_buffer_load_b8(rve, row, 0, 0);
+    }
+  };
+  auto convert = [&](int buf) {
+#pragma unroll
+    for (int j = 0; j < NL; ++j) {
+      const int p = j * 64 + lane, row = p / (D / 16), c = p % (D / 16);
+      const uint32_t to = uint32_t(buf * TILE + wave * BLOCK + row * D * 2) + ((uint32_t(2 * c) ^ tile_swz<D>(row)) * 16u);
+      const float pk = power_of(ke[j]), pv = power_of(ve[j]);
+      bf16x8* const dk = reinterpret_cast<bf16x8*>(sK + to);
+      bf16x8* const dv = reinterpret_cast<bf16x8*>(sV + to);
+      dk[0] = from_e4m3(u32x2{k8[j][0], k8[j][1]}, pk);
+      dk[1] = from_e4m3(u32x2{k8[j][2], k8[j][3]}, pk);
+      dv[0] = from_e4m3(u32x2{v8[j][0], v8[j][1]}, pv);
+      dv[1] = from_e4m3(u32x2{v8[j][2], v8[j][3]}, pv);
+    }
+  };
+
+  uint32_t ak[KS], av[DB];
+  {
+    const uint32_t kbase = uint32_t(reinterpret_cast<uintptr_t>(sK)) + uint32_t(lq * D * 2), xk = tile_swz<D>(lq);
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) ak[ks] = kbase + ((uint32_t(ks * 4 + lh) ^ xk) * 16u);
+    const int rv = lh * 4 + (lq >> 2);
+    const uint32_t vbase = uint32_t(reinterpret_cast<uintptr_t>(sV)) + uint32_t(rv * D * 2) + uint32_t(lq & 1) * 8u, xv = tile_swz<D>(rv);
+#pragma unroll
+    for (int db = 0; db < DB; ++db) av[db] = vbase + ((uint32_t(db * 2 + ((lq & 3) >> 1)) ^ xv) * 16u);
+  }
+
+  // one key tile out of buffer BUF (a compile-time constant, so that every LDS offset is an immediate)
+  auto tile_step = [&](auto bufc, int t) {
+    constexpr int BUF = decltype(bufc)::value;
+    constexpr int BO = BUF * TILE;
+    if constexpr (!FP8) dma_left<0>();  // this wavefront's share of tile t has landed ...
+    __syncthreads();                    // ... and everyone's; everyone has finished reading tile t - 1 in the other buffer
+    if (((t - t_lo) & 15) == 0) bad_now = bad;
+    if (t + 1 < t_hi) {
+      if constexpr (FP8) {
+        convert(BUF ^ 1);
+        if (t + 2 < t_hi) {
+          turn_pages(t + 2);
+          fetch(t + 2);
+        }
+      } else {
+        turn_pages(t + 1);
+        request(t + 1, BUF ^ 1);
+      }
+    }
+    const int kv0 = t * kTileKeys;
+    if (kv0 >= most) return;  // every token of the tile lies behind what this wavefront's last row sees
+    // scores, transposed: st[kb][qb][r] = score of row qb * 16 + lane % 16 with token kv0 + kb * 16 + lane / 16 * 4 + r; eight key fragments at a time, the next ones read under
+    // the matrix instructions of the ones before
+    constexpr int KG = KS / 2, PER = 4 / KG;  // groups of reads, blocks of 16 tokens in one
+    u32x4 kf[KG][8];
+    auto k_reads = [&](auto grp) {
+      unrolled(std::make_integer_sequence<int, 8>{}, [&](auto c) {
+        constexpr int q = decltype(grp)::value, kb = q * PER + decltype(c)::value / KS, ks = decltype(c)::value % KS;
+        kf[q][decltype(c)::value] = lds_b128<BO + kb * BLOCK>(ak[ks]);
+      });
+    };
+    f32x4 st[4][QB];
+    auto k_products = [&](auto grp) {
+      constexpr int q = decltype(grp)::value;
+#pragma unroll
+      for (int k = 0; k < PER; ++k)
+#pragma unroll
+        for (int qb = 0; qb < QB; ++qb) {
+          st[q * PER + k][qb] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+          for (int ks = 0; ks < KS; ++ks)
+            st[q * PER + k][qb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, kf[q][k * KS + ks]), qf[qb][ks], st[q * PER + k][qb], 0, 0, 0);
+        }
+      __builtin_amdgcn_sched_barrier(0);
+    };
+    // value fragments, eight reads (two 16-column blocks) a group: [group][(db % 2) * 4 + kb], tokens kb * 16 ..
+    constexpr int VG = DB / 2;
+    u32x2 vf[VG][8];
+    auto v_reads = [&](auto grp) {
+      unrolled(std::make_integer_sequence<int, 8>{}, [&](auto c) {
+        constexpr int q = decltype(grp)::value, db = q * 2 + decltype(c)::value / 4, kb = decltype(c)::value % 4;
+        vf[q][decltype(c)::value] = lds_tr_b64<BO + kb * BLOCK>(av[db]);
+      });
+    };
+    using I0 = std::integral_constant<int, 0>;
+    using I1 = std::integral_constant<int, 1>;
+    k_reads(I0{});
+    lds_reads_done(kf[0]);
+    if constexpr (KG == 2) {
+      k_reads(I1{});
+      k_products(I0{});
+      lds_reads_done(kf[1]);
+    }
+    v_reads(I0{});
+    v_reads(I1{});
+    k_products(std::integral_constant<int, KG - 1>{});
+
+    const uint32_t gone = uint32_t(bad_now >> (((t - t_lo) & 15) << 2)) & 15u;  // blocks whose pages there are not
+    const bool edge = kv0 + kTileKeys > all_see || gone != 0 || w0 + 16 * QB > rows;
+    bf16x8 pf[QB][2];
+#pragma unroll
+    for (int qb = 0; qb < QB; ++qb) {
+      if (edge) {
+#pragma unroll
+        for (int kb = 0; kb < 4; ++kb)
+#pragma unroll
+          for (int r = 0; r < 4; ++r)
+            if (kv0 + kb * 16 + lh * 4 + r >= sees[qb] || ((gone >> kb) & 1u)) st[kb][qb][r] = -INFINITY;
+      }
+      float mx = -INFINITY;
+#pragma unroll
+      for (int kb = 0; kb < 4; ++kb)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) mx = fmaxf(mx, st[kb][qb][r]);
+      mx = over_rows(mx, larger) * a.scale_log2;
+      const float m_new = fmaxf(m_run[qb], mx);
+      const float m_use = m_new == -INFINITY ? 0.f : m_new;
+      const float alpha = fast_exp2(m_run[qb] - m_use);
+      float ls = 0.f;
+      float pr[4][4];
+#pragma unroll
+      for (int kb = 0; kb < 4; ++kb)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          pr[kb][r] = fast_exp2(fmaf(st[kb][qb][r], a.scale_log2, -m_use));
+          ls += pr[kb][r];
+        }
+      l_run[qb] = l_run[qb] * alpha + ls;
+      m_run[qb] = m_new;
+      if (__any(alpha != 1.0f)) {
+#pragma unroll
+        for (int db = 0; db < DB; ++db) acc[qb][db] *= alpha;
+      }
+      // weights as bf16: half a step of 2^-8 each, of a mean of values that is rounded to the same
+#pragma unroll
+      for (int s2 = 0; s2 < 2; ++s2)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          pf[qb][s2][r] = static_cast<__bf16>(pr[2 * s2][r]);
+          pf[qb][s2][4 + r] = static_cast<__bf16>(pr[2 * s2 + 1][r]);
+        }
+    }
+    // O^T += V^T P^T (token slots of a 32-token step in the order the scores sit in the registers); every group of reads lands under the matrix instructions of the group before it
+    auto v_products = [&](auto grp) {
+      constexpr int q = decltype(grp)::value;
+#pragma unroll
+      for (int d2 = 0; d2 < 2; ++d2)
+#pragma unroll
+        for (int s2 = 0; s2 < 2; ++s2) {
+          const u32x2 lo = vf[q][d2 * 4 + s2 * 2], hi = vf[q][d2 * 4 + s2 * 2 + 1];
+          const u32x4 both = {lo[0], lo[1], hi[0], hi[1]};
+#pragma unroll
+          for (int qb = 0; qb < QB; ++qb)
+            acc[qb][q * 2 + d2] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, both), pf[qb][s2], acc[qb][q * 2 + d2], 0, 0, 0);
+        }
+      __builtin_amdgcn_sched_barrier(0);
+    };
+    lds_reads_done(vf[0]);
+    lds_reads_tied(vf[1]);
+    __builtin_amdgcn_sched_barrier(0);
+    if constexpr (VG == 4) {
+      using I2 = std::integral_constant<int, 2>;
+      using I3 = std::integral_constant<int, 3>;
+      v_reads(I2{});
+      v_products(I0{});
+      v_reads(I3{});
+      v_products(I1{});
+      lds_reads_left<8>(vf[2]);
+      v_products(I2{});
+      lds_reads_done(vf[3]);
+      v_products(I3{});
+    } else {
+      v_products(I0{});
+      v_products(I1{});
+    }
+  };
+
+  if (t_lo < t_hi) {
+    if constexpr (FP8) {
+      fetch(t_lo);
+      convert(0);
+      if (t_lo + 1 < t_hi) fetch(t_lo + 1);
+    } else {
+      request(t_lo, 0);
+    }
+  }
+  for (int t = t_lo; t < t_hi; t += 2) {
+    tile_step(std::integral_constant<int, 0>{}, t);
+    if (t + 1 < t_hi) tile_step(std::integral_constant<int, 1>{}, t + 1);
+  }
+
+#pragma unroll
+  for (int qb = 0; qb < QB; ++qb) {
+    const int rr = w0 + qb * 16 + lq, i = rr / G, j = j0 + rr - i * G;
+    const float l = over_rows(l_run[qb], added);
+    if (n_pieces > 1) {
+      float* const to = a.tile_parts + (int64_t(id) * kTileRows + (rr - row0)) * (D + kPartPad);
+#pragma unroll
+      for (int db = 0; db < DB; ++db) *reinterpret_cast<f32x4*>(to + db * 16 + lh * 4) = acc[qb][db];
+      if (lh == 0) to[D] = m_run[qb], to[D + 1] = l;
+      continue;
+    }
+    if (rr >= rows) continue;
+    const float inv = l == 0.f ? 0.f : 1.0f / l;
+    uint16_t* const cp = a.C + int64_t(start + i) * a.ldc + int64_t(j) * D + lh * 4;
+#pragma unroll
+    for (int db = 0; db < DB; ++db) {
+      ntp_gemm::u16x4 o;
+#pragma unroll
+      for (int r = 0; r < 4; ++r) o[r] = ntp_gemm::f32_to_bf16(acc[qb][db][r] * inv);
+      *reinterpret_cast<ntp_gemm::u16x4*>(cp + db * 16) = o;
+    }
+    if (lh == 0 && a.LSE) a.LSE[int64_t(j) * a.M + start + i] = ((l == 0.f ? 0.f : m_run[qb]) + log2f(l)) * 0.6931471805599453f;
+  }
+}
+
+// The pieces of a row tile put together: workgroup = (unit, 16 or 32 of its rows).
+template <int D>
+__device__ __forceinline__ void chunk_tiles_join(const ChunkArgs& a, const int unit, const int part) {
+  constexpr int L = D / 8, R = kThreads / L;  // lanes of a row, 8 columns each; rows
+  TilePlan plan;
+  plan.make(a);
+  if (plan.total == plan.units || unit >= plan.units) return;
+  // the unit's first piece: units and pieces are numbered in the same order, so the unit is looked for with walks that are not cut
+  const int piece_tiles = plan.piece_tiles;
+  int from = 0, units = 0, pieces = 0;
+  int seq_start = 0, seq_n = 0, np = 1, head = 0, tile = 0, first = 0;
+  for (;; from += 64) {
+    if (from > 0 || a.n_seq > 64) plan.load(a, from + int(threadIdx.x & 63));
+    plan.piece_tiles = piece_tiles;
+    const int mine = a.kv_used * plan.tiles, upto = sum_upto(mine), cut = plan.cut(), p_upto = sum_upto(mine * cut);
+    const uint64_t behind = __ballot(units + upto > unit);
+    if (behind) {
+      const int at = __builtin_ctzll(behind);
+      auto of = [&](int v) { return __builtin_amdgcn_readlane(v, at); };
+      const int t = of(plan.tiles), rest = unit - units - (of(upto) - of(mine));
+      np = of(cut);
+      head = rest / t, tile = t - 1 - rest % t;
+      first = pieces + of(p_upto) - of(mine * cut) + rest * np;
+      seq_start = of(plan.start), seq_n = of(plan.n);
+      break;
+    }
+    units += __builtin_amdgcn_readlane(upto, 63);
+    pieces += __builtin_amdgcn_readlane(p_upto, 63);
+  }
+  if (np == 1) return;
+  const Heads hd(a, a.kv_first + head);
+  const int G = hd.j1 - hd.j0, in_tile = part * R + int(threadIdx.x) / L, rr = tile * kTileRows + in_tile, c = int(threadIdx.x) % L * 8;
+  if (rr >= min(seq_n, a.max_new) * G) return;
+  const int i = rr / G, j = hd.j0 + rr - i * G;
+  const float* const p0 = a.tile_parts + (int64_t(first) * kTileRows + in_tile) * (D + kPartPad);
+  constexpr int64_t kNext = int64_t(kTileRows) * (D + kPartPad);
+  float top = -INFINITY;
+  for (int p = 0; p < np; ++p) top = fmaxf(top, p0[p * kNext + D]);
+  const float base = top == -INFINITY ? 0.f : top;
+  f32x4 lo = {0.f, 0.f, 0.f, 0.f}, hi = lo;
+  float sum = 0.f;
+#pragma unroll 4
+  for (int p = 0; p < np; ++p) {
+    const float* const q = p0 + p * kNext;
+    const float w = fast_exp2(q[D] - base);
+    sum = fmaf(w, q[D + 1], sum);
+    lo += w * *reinterpret_cast<const f32x4*>(q + c);
+    hi += w * *reinterpret_cast<const f32x4*>(q + c + 4);
+  }
+  const float inv = sum == 0.f ? 0.f : 1.0f / sum;
+  u32x4 out;
+#pragma unroll
+  for (int k = 0; k < 2; ++k) {
+    out[k] = uint32_t(ntp_gemm::f32_to_bf16(lo[2 * k] * inv)) | uint32_t(ntp_gemm::f32_to_bf16(lo[2 * k + 1] * inv)) << 16;
+    out[2 + k] = uint32_t(ntp_gemm::f32_to_bf16(hi[2 * k] * inv)) | uint32_t(ntp_gemm::f32_to_bf16(hi[2 * k + 1] * inv)) << 16;
+  }
+  *reinterpret_cast<u32x4*>(a.C + int64_t(seq_start + i) * a.ldc + int64_t(j) * D + c) = out;
+  if (c == 0 && a.LSE) a.LSE[int64_t(j) * a.M + seq_start + i] = (base + log2f(sum)) * 0.6931471805599453f;
+}
+
+}  // namespace ntp_chunk
+
+#endif  // NTP_ATTN_CHUNK_TILES_H_
