@@ -25,13 +25,14 @@ struct ChunkArgs {
   // sum, and the D unnormalised outputs
   float2* part_sums;
   float* part_rows;
+  int32_t* plan;      // how the row tiles' walks are cut: units, pieces, key tiles of a piece
   float* tile_parts;  // per piece of a tile's walk its rows: D unnormalised outputs, maximum and sum, two unused
   int64_t ldq, ldc, ldt, page_stride, exp_stride;
   int32_t M, n_pages, n_seq, max_new, max_len, q_cnt, q_off, kv_off, group, page_size, page_log2;
   int32_t kv_first, kv_used, gmax;  // local KV heads that are read; the most local query heads of one
   int32_t cap;                      // sequences of up to so many rows (tokens x gmax) go by ntp_attn_chunk_rows.h, the others by ntp_attn_chunk_tiles.h
   int32_t shares, row_wgs;          // shares that the line is cut into at most; workgroups of the launch that take them (the first ones)
-  int32_t slots;                    // pieces that tiles are cut into where they are fewer; 0: never
+  int32_t slots;                    // workgroups that the device has room for, which walks are cut for (into up to twice as many pieces); 0: never
   float scale_log2;                 // log2(e) / sqrt(d)
 };
 

@@ -33,14 +33,15 @@ __global__ __attribute__((amdgpu_flat_work_group_size(kThreads, kThreads), amdgp
 }
 
 template <int D, bool FP8>
-__global__ __attribute__((amdgpu_flat_work_group_size(kThreads, kThreads), amdgpu_waves_per_eu(2, 2))) void chunk_tiles_kernel(const ChunkArgs a) {
+__global__ __attribute__((amdgpu_flat_work_group_size(kThreads, kThreads), amdgpu_waves_per_eu(kPlaces<D>, kPlaces<D>))) void chunk_tiles_kernel(const ChunkArgs a) {
   __shared__ __attribute__((aligned(1024))) unsigned char lds[kTileLds<D>];
   chunk_tiles<D, FP8>(a, int(blockIdx.x), lds);
 }
 
 // Workgroups: first those of the line's units, then those of the row tiles.
+enum { kByBorder, kByUnit, kLengthy };  // border between shares and some rows; unit and some rows; unit, row and some columns
 struct Joins {
-  int32_t rows, row_jobs, lengthy;  // rows of a unit; workgroups for the units; few units of many parts
+  int32_t kind, rows, row_jobs;  // rows of a unit; workgroups for the units
 };
 template <int D, bool FP8, int QB>
 __global__ __launch_bounds__(kThreads) void chunk_join_kernel(const ChunkArgs a, const Joins j) {
@@ -48,15 +49,15 @@ __global__ __launch_bounds__(kThreads) void chunk_join_kernel(const ChunkArgs a,
   const int wg = int(blockIdx.x);
   if (wg < j.row_jobs) {
     constexpr int SPLIT = D / kFewColumns, AT_ONCE = kThreads / (D / 4);
-    if (j.lengthy) {
+    if (j.kind == kLengthy) {
       chunk_rows_join_long<D, STEP, R>(a, wg / SPLIT / j.rows, wg / SPLIT % j.rows, wg % SPLIT * kFewColumns);
     } else {
       const int per = (j.rows + AT_ONCE - 1) / AT_ONCE;
-      chunk_rows_join_short<D, STEP, R>(a, wg / per, wg % per * AT_ONCE);
+      CutUnit u;
+      if (j.kind == kByUnit ? u.by_number<STEP>(a, wg / per) : u.by_border<STEP>(a, wg / per + 1)) chunk_rows_join_short<D, R>(a, u, wg % per * AT_ONCE);
     }
   } else {
-    constexpr int PER = kTileRows / (kThreads / (D / 8));
-    chunk_tiles_join<D>(a, (wg - j.row_jobs) / PER, (wg - j.row_jobs) % PER);
+    chunk_tiles_join<D>(a, wg - j.row_jobs, int(gridDim.x) - j.row_jobs);
   }
 }
 
@@ -79,7 +80,7 @@ struct ChunkChoice {
   int32_t row_wgs, shares, rows;    // workgroups that take sequences of few rows; shares of their line (0: workgroup = unit); most rows of a unit
   int64_t units;                    // such units at most
   int64_t tiles;                    // (sequence, KV head, row tile)s of the others at most
-  int32_t slots;                    // pieces that these are cut into where they are fewer (0: never)
+  int32_t slots;                    // workgroups that the device has room for: walks are cut for these (0: never), into twice as many at most
   int64_t ws_rows, ws_bytes;        // bytes of the line's partial results, and of all
 };
 
@@ -106,8 +107,8 @@ ChunkChoice choose_chunk(const ntp_handle* h, int64_t ws_bytes, const ntp_attn_c
     c.shares = int32_t(std::min<int64_t>(std::min(2 * int64_t(h->compute_units), steps * c.units), kMaxShares));
     c.ws_rows = (int64_t(c.shares) * 2 * c.cap * (s->head_dim + 2) * 4 + 255) / 256 * 256;
   }
-  if (c.tiles > 0 && s->max_len > kMinPiece * kTileKeys) c.slots = 2 * h->compute_units;
-  c.ws_bytes = c.ws_rows + int64_t(c.slots > 0 ? c.slots + 8 : 0) * kTileRows * (s->head_dim + kPartPad) * 4;
+  if (tiles && s->max_len > kMinPiece * kTileKeys) c.slots = (s->head_dim == 64 && c.cap == 0 ? kPlaces<64> : kPlaces<128>) * h->compute_units;
+  c.ws_bytes = c.ws_rows + (c.slots > 0 ? 256 + int64_t(2 * c.slots) * kTileRows * (s->head_dim + kPartPad) * 4 : 0);
   if (c.ws_bytes > ws_bytes) c.shares = c.slots = 0, c.ws_rows = c.ws_bytes = 0;
   c.row_wgs = int32_t(c.shares > 0 ? c.shares : c.units);
   if (tiles) c.row_wgs = (c.row_wgs + 7) / 8 * 8;  // (the row tiles' workgroups keep their XCDs)
@@ -124,9 +125,11 @@ int ntp::attn_chunk_workspace_wish(const ntp_handle* h, const ntp_attn_chunk_sha
 
 namespace {
 
+constexpr int kJoinWgs = 1024;  // that join row tiles
+
 template <int D, bool FP8>
 bool launch_chunk(const ChunkArgs& a, const ChunkChoice& c, hipStream_t hs) {
-  const int64_t tile_wgs = c.tiles > 0 ? std::max<int64_t>(c.tiles, c.slots > 0 ? c.slots + 8 : 0) : 0;
+  const int64_t tile_wgs = c.tiles > 0 ? (std::max<int64_t>(c.tiles, 2 * c.slots) + 8 * kRun - 1) / (8 * kRun) * (8 * kRun) : 0;
   const dim3 grid{uint32_t(c.row_wgs + tile_wgs)}, block{kThreads};
   if (c.tiles > 0 && c.cap > 0) hipLaunchKernelGGL((chunk_both_kernel<D, FP8>), grid, block, 0, hs, a);
   else if (c.tiles > 0) hipLaunchKernelGGL((chunk_tiles_kernel<D, FP8>), grid, block, 0, hs, a);
@@ -134,12 +137,11 @@ bool launch_chunk(const ChunkArgs& a, const ChunkChoice& c, hipStream_t hs) {
   else hipLaunchKernelGGL((chunk_rows_kernel<D, FP8, 2>), grid, block, 0, hs, a);
   if (hipGetLastError() != hipSuccess) return false;
   if (c.shares <= 1 && c.slots == 0) return true;
-  Joins j{c.rows, 0, c.shares >= 32 * c.units};
-  if (c.shares > 1) {
-    constexpr int AT_ONCE = kThreads / (D / 4);
-    j.row_jobs = int32_t(j.lengthy ? c.units * c.rows * (D / kFewColumns) : int64_t(c.shares - 1) * ((c.rows + AT_ONCE - 1) / AT_ONCE));
-  }
-  const int64_t tile_jobs = c.slots > 0 ? std::min<int64_t>(c.slots, c.tiles) * (kTileRows / (kThreads / (D / 8))) : 0;
+  constexpr int AT_ONCE = kThreads / (D / 4);
+  const int64_t per = (c.rows + AT_ONCE - 1) / AT_ONCE;
+  Joins j{c.shares >= 32 * c.units ? kLengthy : c.units < c.shares ? kByUnit : kByBorder, c.rows, 0};
+  if (c.shares > 1) j.row_jobs = int32_t(j.kind == kLengthy ? c.units * c.rows * (D / kFewColumns) : (j.kind == kByUnit ? c.units : c.shares - 1) * per);
+  const int64_t tile_jobs = c.slots > 0 ? std::min<int64_t>(kJoinWgs, c.tiles * (kTileRows / 2)) : 0;
   const dim3 jobs{uint32_t(j.row_jobs + tile_jobs)};
   if (c.qb == 1) hipLaunchKernelGGL((chunk_join_kernel<D, FP8, 1>), jobs, block, 0, hs, a, j);
   else hipLaunchKernelGGL((chunk_join_kernel<D, FP8, 2>), jobs, block, 0, hs, a, j);
@@ -169,7 +171,10 @@ extern "C" int ntp_attn_chunk_shard(ntp_handle_t* h, const ntp_attn_chunk_shape_
     a.part_rows = static_cast<float*>(h->workspace);
     a.part_sums = reinterpret_cast<float2*>(a.part_rows + int64_t(c.shares) * 2 * c.cap * s->head_dim);
   }
-  if (c.slots > 0) a.tile_parts = reinterpret_cast<float*>(static_cast<char*>(h->workspace) + c.ws_rows);
+  if (c.slots > 0) {
+    a.plan = reinterpret_cast<int32_t*>(static_cast<char*>(h->workspace) + c.ws_rows);
+    a.tile_parts = reinterpret_cast<float*>(a.plan + 64);
+  }
   a.ldq = ldq, a.ldc = ldc, a.ldt = ldt, a.page_stride = pages->page_stride, a.exp_stride = pages->exp_stride;
   a.M = int32_t(s->M), a.n_pages = int32_t(pages->n_pages), a.n_seq = s->n_seq, a.max_new = s->max_new, a.max_len = s->max_len;
   a.q_cnt = s->q_cnt, a.q_off = s->q_off, a.kv_off = s->kv_off, a.group = s->group, a.page_size = pages->page_size, a.page_log2 = ntp::log2_of(pages->page_size);

@@ -483,6 +483,31 @@ struct CutUnit {
     late = line.begin(w0) < begin;
     parts = line.share_of(begin + steps - 1) - w0 + 1;
   }
+  // unit `number` of the batch (sequence by sequence, KV head by KV head); whether it is cut
+  template <int STEP>
+  __device__ __forceinline__ bool by_number(const ChunkArgs& a, int number) {
+    RowLine<STEP> line;
+    line.measure(a);
+    const int seq = number / line.per_seq, unit = number % line.per_seq;
+    while (seq >= line.base + 64) line.next64(a);
+    const int steps = line.of(line.mine, seq);
+    if (steps == 0) return false;
+    set(a, line, seq, unit, (line.before + line.of(line.upto, seq) - steps) * line.per_seq + unit * steps);
+    return parts > 1;
+  }
+  // the unit with the border between shares w - 1 and w in it, if that is the unit's first
+  template <int STEP>
+  __device__ __forceinline__ bool by_border(const ChunkArgs& a, int w) {
+    RowLine<STEP> line;
+    line.measure(a);
+    if (w >= line.shares || line.total == 0) return false;
+    const int x = line.begin(w);
+    int seq, unit, step;
+    line.seek(a, x, seq, unit, step);
+    if (step == 0 || line.begin(w - 1) > x - step) return false;
+    set(a, line, seq, unit, x - step);
+    return true;
+  }
   __device__ __forceinline__ int64_t slot(int p, int R) const { return (int64_t(w0 + p) * 2 + (p == 0 ? late : 0)) * R; }
 };
 __device__ __forceinline__ void store_row(const ChunkArgs& a, const CutUnit& u, int rr, int col, int D, f32x4 o, float base, float sum) {
@@ -502,15 +527,8 @@ __device__ __forceinline__ void chunk_rows_join_long(const ChunkArgs& a, const i
   constexpr int L = kFewColumns / 4, GR = kThreads / L, N = kMaxShares / kThreads;
   __shared__ float weight[kMaxShares], wave_max[kWaves], wave_sum[kWaves];
   __shared__ f32x4 sums[GR][L];
-  RowLine<STEP> line;
-  line.measure(a);
-  const int seq = number / line.per_seq, unit = number % line.per_seq;
-  while (seq >= line.base + 64) line.next64(a);
-  const int steps = line.of(line.mine, seq);
-  if (steps == 0) return;
   CutUnit u;
-  u.set(a, line, seq, unit, (line.before + line.of(line.upto, seq) - steps) * line.per_seq + unit * steps);
-  if (u.parts == 1 || rr >= u.rows) return;
+  if (!u.by_number<STEP>(a, number) || rr >= u.rows) return;
   const int grp = threadIdx.x / L, c = col0 + int(threadIdx.x) % L * 4;
   auto part_row = [&](int p) { return *reinterpret_cast<const f32x4*>(a.part_rows + (u.slot(p, R) + rr) * D + c); };
   f32x4 o = {0.f, 0.f, 0.f, 0.f};
@@ -557,36 +575,39 @@ __device__ __forceinline__ void chunk_rows_join_long(const ChunkArgs& a, const i
   store_row(a, u, rr, c, D, o, base, sum);
 }
 
-// Many units: workgroup = (border between two shares, 8 or 16 rows), the first border inside a unit has it; D / 4 lanes a row.
-template <int D, int STEP, int R>
-__device__ __forceinline__ void chunk_rows_join_short(const ChunkArgs& a, const int border, const int row0) {
+// Some rows of a unit of few parts, D / 4 lanes a row.
+template <int D, int R>
+__device__ __forceinline__ void chunk_rows_join_short(const ChunkArgs& a, const CutUnit& u, const int row0) {
   constexpr int L = D / 4;
-  RowLine<STEP> line;
-  line.measure(a);
-  const int w = border + 1;
-  if (w >= line.shares || line.total == 0) return;
-  const int x = line.begin(w);
-  int seq, unit, step;
-  line.seek(a, x, seq, unit, step);
-  const int begin = x - step;
-  if (step == 0 || line.begin(w - 1) > begin) return;
-  CutUnit u;
-  u.set(a, line, seq, unit, begin);
   const int rr = row0 + int(threadIdx.x) / L, c = int(threadIdx.x) % L * 4;
   if (rr >= u.rows) return;
+  constexpr int AT_ONCE = 16;  // parts whose loads go out together
   float top = -INFINITY, sum = 0.f;
-#pragma unroll 4
-  for (int p = 0; p < u.parts; ++p) top = fmaxf(top, a.part_sums[u.slot(p, R) + rr].x);
-  const float base = top == -INFINITY ? 0.f : top;
   f32x4 o = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll 4
-  for (int p = 0; p < u.parts; ++p) {
-    const float2 ms = a.part_sums[u.slot(p, R) + rr];
-    const float wt = fast_exp2(ms.x - base);
-    sum = fmaf(wt, ms.y, sum);
-    o += wt * *reinterpret_cast<const f32x4*>(a.part_rows + (u.slot(p, R) + rr) * D + c);
+  for (int p = 0; p < u.parts; p += AT_ONCE) {
+    float2 ms[AT_ONCE];
+    f32x4 x[AT_ONCE];
+#pragma unroll
+    for (int k = 0; k < AT_ONCE; ++k) {
+      ms[k] = float2{-INFINITY, 0.f}, x[k] = f32x4{0.f, 0.f, 0.f, 0.f};
+      if (p + k < u.parts) {
+        const int64_t at = u.slot(p + k, R) + rr;
+        ms[k] = a.part_sums[at];
+        x[k] = *reinterpret_cast<const f32x4*>(a.part_rows + at * D + c);
+      }
+    }
+    float more = top;
+#pragma unroll
+    for (int k = 0; k < AT_ONCE; ++k) more = fmaxf(more, ms[k].x);
+    const float base = more == -INFINITY ? 0.f : more, old = fast_exp2(top - base);
+    sum *= old, o *= old, top = more;
+#pragma unroll
+    for (int k = 0; k < AT_ONCE; ++k) {
+      const float wt = fast_exp2(ms[k].x - base);
+      sum = fmaf(wt, ms[k].y, sum), o += wt * x[k];
+    }
   }
-  store_row(a, u, rr, c, D, o, base, sum);
+  store_row(a, u, rr, c, D, o, top == -INFINITY ? 0.f : top, sum);
 }
 
 }  // namespace ntp_chunk

@@ -14,8 +14,11 @@
 
 namespace ntp_chunk {
 
-constexpr int kMinPiece = 4;    // tiles of a piece at least
-constexpr int kPartPad = 4;     // floats behind a partial row's outputs: maximum, sum
+constexpr int kMinPiece = 4;  // key tiles of a piece at least
+constexpr int kPartPad = 4;   // floats behind a partial row's outputs: maximum, sum
+constexpr int kRun = 4;       // neighbouring pieces, which read the same tokens, that stay on one XCD
+template <int D>
+constexpr int kPlaces = D == 128 ? 2 : 3;  // workgroups that a compute unit has room for
 
 // Row tiles and key tiles (of its last row) of a sequence; no row tiles where it is one of few rows.
 __device__ __forceinline__ void tiles_of(const ChunkArgs& a, int n, int len, int& tiles, int& walk) {
@@ -24,12 +27,11 @@ __device__ __forceinline__ void tiles_of(const ChunkArgs& a, int n, int len, int
   walk = max(1, (max(len - n + used, 0) + kTileKeys - 1) / kTileKeys);
 }
 
-// How the batch's walks are cut, and the piece with number x of them.  Pieces are numbered sequence by sequence, in it KV head by KV head, row tile by row tile from the last
-// (the longest walk) on; all tiles of a sequence are cut into the same number.
+// How the batch's walks are cut, and the piece with number x of them.  Pieces are numbered sequence by sequence, in it KV head by KV head, piece by piece, row tile by row tile from the
+// last (the longest walk) on; all tiles of a sequence are cut into the same number.
 struct TilePlan {
-  int units, total, piece_tiles;  // (sequence, KV head, row tile)s; pieces; key tiles of a piece at most
-  // this lane's sequence of 64
-  int start, n, len, tiles, walk;
+  int units, total, piece_tiles;  // (sequence, KV head, row tile)s; pieces; key tiles of a piece at most (0: whole)
+  int start, n, len, tiles, walk;  // this lane's sequence of 64
   __device__ __forceinline__ void load(const ChunkArgs& a, int i) {
     start = n = len = tiles = 0, walk = 1;
     if (i < a.n_seq) {
@@ -38,45 +40,127 @@ struct TilePlan {
     }
   }
   __device__ __forceinline__ int cut() const { return piece_tiles == 0 ? 1 : (walk + piece_tiles - 1) / piece_tiles; }
-  __device__ __forceinline__ static float sum_all(float v) {
+  static constexpr int kAtOnce = 256;  // sequences whose loads go out together
+  // of the sequences from .. from + kAtOnce - 1: units and pieces of this lane's
+  __device__ __forceinline__ void sums(const ChunkArgs& a, int from, int& count, int& pieces) {
+    count = pieces = 0;
 #pragma unroll
-    for (int d = 1; d < 64; d *= 2) v += __shfl_xor(v, d);
-    return v;
-  }
-  __device__ __forceinline__ int pieces(const ChunkArgs& a) {  // of the whole batch
-    int sum = 0;
-    for (int from = 0; from < a.n_seq; from += 64) {
-      if (a.n_seq > 64) load(a, from + int(threadIdx.x & 63));
-      sum += a.kv_used * tiles * cut();
+    for (int k = 0; k < kAtOnce / 64; ++k) {
+      TilePlan p;
+      p.load(a, from + k * 64 + int(threadIdx.x & 63));
+      p.piece_tiles = piece_tiles;
+      count += a.kv_used * p.tiles;
+      pieces += a.kv_used * p.tiles * p.cut();
     }
-    return __builtin_amdgcn_readlane(sum_upto(sum), 63);
   }
+  __device__ __forceinline__ static int all(int v) { return __builtin_amdgcn_readlane(sum_upto(v), 63); }
+  template <typename F>
+  __device__ __forceinline__ static float all(float v, F&& f) {
+#pragma unroll
+    for (int d = 1; d < 16; d *= 2) v = f(v, __shfl_xor(v, d));
+    return over_rows(v, f);
+  }
+  // A call's time by an estimate in key tiles, for walks cut into pieces of at most S: rounds of whole pieces, or what list scheduling takes at most, and per piece its way in and out and its
+  // partial results.  Taken is the best of whole walks and of one to four rounds.
+  template <int D>
   __device__ __forceinline__ void make(const ChunkArgs& a) {
     piece_tiles = 0;
     int count = 0;
-    float work = 0.f;  // (exact enough: below 2^24 pieces' worth of error)
+    float work = 0.f, most = 0.f;
     load(a, threadIdx.x & 63);
-    for (int from = 0; from < a.n_seq; from += 64) {
-      if (a.n_seq > 64) load(a, from + int(threadIdx.x & 63));
-      count += a.kv_used * tiles;
-      work += float(a.kv_used * tiles) * float(walk);
+    auto add = [&](const TilePlan& p) {
+      const int c = a.kv_used * p.tiles;
+      count += c;
+      work += float(c) * (float(p.walk) - float(min(p.n, a.max_new)) * (0.5f / kTileKeys));  // (half a triangle less)
+      if (c > 0) most = fmaxf(most, float(p.walk));
+    };
+    if (a.n_seq <= 64) {
+      add(*this);
+    } else {
+      for (int from = 0; from < a.n_seq; from += kAtOnce) {
+#pragma unroll
+        for (int k = 0; k < kAtOnce / 64; ++k) {
+          TilePlan p;
+          p.load(a, from + k * 64 + int(threadIdx.x & 63));
+          add(p);
+        }
+      }
     }
-    units = total = __builtin_amdgcn_readlane(sum_upto(count), 63);
-    if (units == 0 || units >= a.slots) return;
-    work = sum_all(work);
-    piece_tiles = max(kMinPiece, int(ceilf(work / float(a.slots))));
-    total = pieces(a);
-    if (total > a.slots) {  // sum of ceil(walk / piece) <= work / piece + units
-      piece_tiles = max(kMinPiece, int(ceilf(work / float(a.slots - units))));
-      total = pieces(a);
+    units = total = all(count);
+    if (a.slots == 0 || units == 0) return;
+    work = all(work, added), most = all(most, larger);
+    const float slots = float(a.slots), share = work / slots;
+    if (a.n_seq > 64) {  // (not looked at piece by piece)
+      if (units >= a.slots || most <= 1.5f * share) return;
+      piece_tiles = max(kMinPiece, int(ceilf(share)));
+      int pieces = 0, c, p;
+      for (int from = 0; from < a.n_seq; from += kAtOnce) {
+        sums(a, from, c, p);
+        pieces += p;
+      }
+      total = all(pieces);
+      if (total <= 2 * a.slots) return;
+      piece_tiles = 0, total = units;
+      return;
     }
+    auto estimate = [&](int S, int pieces) {
+      const float longest = fminf(float(S), most), rounds = ceilf(float(pieces) / slots);
+      return fminf(rounds * longest, share + 0.5f * longest) + 3.0f * rounds + (pieces > units ? float(pieces) * (1.0f / 85) : 0.0f);
+    };
+    float best = estimate(1 << 30, units);
+    int best_tiles = 0;
+    for (int j = 1; j <= 8; ++j) {
+      const float room = j <= 4 ? slots * float(j) : slots * float(j - 4) - float(units);
+      if (room <= 0.f) continue;
+      piece_tiles = max(kMinPiece, int(ceilf(work / room)));
+      const int pieces = all(a.kv_used * tiles * cut());
+      const float t = estimate(piece_tiles, pieces);
+      if (pieces <= 2 * a.slots && t < best) best = t, best_tiles = piece_tiles, total = pieces;
+    }
+    piece_tiles = best_tiles;
   }
-  // x < total: its sequence, KV head, row tile (from the last on), and piece
+  // Row tiles of this lane's sequence whose walks have `least` key tiles or more: row tile t's last row is min(rows, 128 (t + 1)) - 1, of token len - n + row / gmax.
+  __device__ __forceinline__ int tiles_from(const ChunkArgs& a, int least) const {
+    const int used = min(n, a.max_new), m = (least - 1) * kTileKeys - (len - n);  // (tokens of the chunk behind which the walk is so long)
+    if (least <= 0 || m <= 0) return tiles;
+    if (m >= used) return 0;
+    return tiles - (m * a.gmax + kTileRows) / kTileRows + 1;
+  }
+  static constexpr int kLevel = 8;  // key tiles
+  // x < total: its sequence, KV head, row tile, and piece.  Where there are more whole walks than places, the longest come first, whosever they are, by levels of their lengths: tiles of a
+  // level are numbered sequence by sequence, head by head.
   int seq, head, tile, piece, n_pieces, seq_start, seq_n, seq_len;
   __device__ __forceinline__ void find(const ChunkArgs& a, int x) {
+    if (piece_tiles == 0 && a.n_seq <= 64) {
+      auto upto = [&](int level) { return all(a.kv_used * tiles_from(a, level * kLevel)); };
+      int lo = 0, hi = a.max_len / (kTileKeys * kLevel) + 1, longer = 0;  // the level: the highest with more than x tiles in it and above it
+      while (hi - lo > 1) {
+        const int mid = (lo + hi) / 2, count = upto(mid);
+        if (count > x) lo = mid;
+        else hi = mid, longer = count;
+      }
+      const int above = tiles_from(a, (lo + 1) * kLevel), here = tiles_from(a, lo * kLevel) - above, sum = sum_upto(a.kv_used * here);
+      const int at = __builtin_ctzll(__ballot(longer + sum > x));
+      auto of = [&](int v) { return __builtin_amdgcn_readlane(v, at); };
+      const int rest = x - longer - (of(sum) - a.kv_used * of(here));
+      n_pieces = 1, piece = 0;
+      head = rest / of(here);
+      tile = of(tiles) - 1 - of(above) - rest % of(here);
+      seq = at, seq_start = of(start), seq_n = of(n), seq_len = of(len);
+      return;
+    }
     int from = 0, before = 0;
-    for (;; from += 64) {
-      if (from > 0 || a.n_seq > 64) load(a, from + int(threadIdx.x & 63));
+    if (a.n_seq > 64) {
+      for (; from < a.n_seq - kAtOnce; from += kAtOnce) {
+        int c, p;
+        sums(a, from, c, p);
+        p = all(p);
+        if (before + p > x) break;
+        before += p;
+      }
+      load(a, from + int(threadIdx.x & 63));
+    }
+    for (;;) {
       const int mine = a.kv_used * tiles * cut(), upto = sum_upto(mine);
       const uint64_t behind = __ballot(before + upto > x);
       if (behind) {
@@ -85,14 +169,50 @@ struct TilePlan {
         const int t = of(tiles);
         n_pieces = of(cut());
         int rest = x - before - (of(upto) - of(mine));
-        piece = rest % n_pieces;
-        rest /= n_pieces;
-        head = rest / t;
         tile = t - 1 - rest % t;
+        rest /= t;
+        piece = rest % n_pieces;
+        head = rest / n_pieces;
         seq = from + at, seq_start = of(start), seq_n = of(n), seq_len = of(len);
         return;
       }
       before += __builtin_amdgcn_readlane(upto, 63);
+      from += 64;
+      load(a, from + int(threadIdx.x & 63));
+    }
+  }
+  // unit < units: the same of it, and the number of its first piece; the unit's pieces lie `tiles_there` apart
+  int tiles_there;
+  __device__ __forceinline__ int find_unit(const ChunkArgs& a, int unit) {
+    int from = 0, before = 0, pieces = 0;
+    if (a.n_seq > 64) {
+      for (; from < a.n_seq - kAtOnce; from += kAtOnce) {
+        int c, p;
+        sums(a, from, c, p);
+        c = all(c);
+        if (before + c > unit) break;
+        before += c;
+        pieces += all(p);
+      }
+      load(a, from + int(threadIdx.x & 63));
+    }
+    for (;;) {
+      const int mine = a.kv_used * tiles, upto = sum_upto(mine), pieces_upto = sum_upto(mine * cut());
+      const uint64_t behind = __ballot(before + upto > unit);
+      if (behind) {
+        const int at = __builtin_ctzll(behind);
+        auto of = [&](int v) { return __builtin_amdgcn_readlane(v, at); };
+        tiles_there = of(tiles);
+        n_pieces = of(cut());
+        const int rest = unit - before - (of(upto) - of(mine)), place = rest % tiles_there;
+        head = rest / tiles_there, tile = tiles_there - 1 - place;
+        seq_start = of(start), seq_n = of(n);
+        return pieces + of(pieces_upto) - of(mine * cut()) + head * n_pieces * tiles_there + place;
+      }
+      before += __builtin_amdgcn_readlane(upto, 63);
+      pieces += __builtin_amdgcn_readlane(pieces_upto, 63);
+      from += 64;
+      load(a, from + int(threadIdx.x & 63));
     }
   }
 };
@@ -115,11 +235,12 @@ __device__ __forceinline__ void chunk_tiles(const ChunkArgs& a, const int wg, un
   const int wave = uniform(threadIdx.x >> 6);
 
   TilePlan plan;
-  plan.make(a);
-  if (wg >= plan.total) return;
-  // neighbouring pieces, which read the same tokens, on one XCD (workgroup b runs on XCD b % 8)
-  const int per_xcd = plan.total / 8, odd = plan.total % 8, xcd = wg % 8;
-  const int id = uniform(xcd * per_xcd + min(xcd, odd) + wg / 8);
+  plan.make<D>(a);
+  if (wg == 0 && threadIdx.x == 0 && a.plan) a.plan[0] = plan.units, a.plan[1] = plan.total, a.plan[2] = plan.piece_tiles;  // for the kernel that joins
+  // runs of pieces on one XCD (workgroup b runs on XCD b % 8), turned by one with every eight of them, so that no XCD has all the long ones
+  const int in_xcd = wg / 8, round = in_xcd / kRun;
+  const int id = uniform((round * 8 + ((wg - round) & 7)) * kRun + in_xcd % kRun);
+  if (id >= plan.total) return;
   plan.find(a, id);
   const int seq = uniform(plan.seq), start = uniform(plan.seq_start), n = uniform(plan.seq_n), len = uniform(plan.seq_len), used = min(n, a.max_new);
   const int g = a.kv_first + uniform(plan.head), n_pieces = uniform(plan.n_pieces), piece = uniform(plan.piece);
@@ -435,64 +556,81 @@ __device__ __forceinline__ void chunk_tiles(const ChunkArgs& a, const int wg, un
   }
 }
 
-// The pieces of a row tile put together: workgroup = (unit, 16 or 32 of its rows).
+// The pieces of row tiles put together: workgroup number wg of n takes every n-th of (unit, some of its rows).  D / 8 lanes a row, eight pieces' loads at a time; where there are
+// many pieces, all groups of lanes take one row's pieces in turn.
 template <int D>
-__device__ __forceinline__ void chunk_tiles_join(const ChunkArgs& a, const int unit, const int part) {
-  constexpr int L = D / 8, R = kThreads / L;  // lanes of a row, 8 columns each; rows
+__device__ __forceinline__ void chunk_tiles_join(const ChunkArgs& a, const int wg, const int n_wgs) {
+  constexpr int L = D / 8, G = kThreads / L, W = D + kPartPad, AT_ONCE = 8;  // lanes of a row, groups of lanes, floats of a partial row
+  __shared__ f32x4 rows_of[G][L][2];
+  __shared__ float2 sums_of[G];
   TilePlan plan;
-  plan.make(a);
-  if (plan.total == plan.units || unit >= plan.units) return;
-  // the unit's first piece: units and pieces are numbered in the same order, so the unit is looked for with walks that are not cut
-  const int piece_tiles = plan.piece_tiles;
-  int from = 0, units = 0, pieces = 0;
-  int seq_start = 0, seq_n = 0, np = 1, head = 0, tile = 0, first = 0;
-  for (;; from += 64) {
-    if (from > 0 || a.n_seq > 64) plan.load(a, from + int(threadIdx.x & 63));
-    plan.piece_tiles = piece_tiles;
-    const int mine = a.kv_used * plan.tiles, upto = sum_upto(mine), cut = plan.cut(), p_upto = sum_upto(mine * cut);
-    const uint64_t behind = __ballot(units + upto > unit);
-    if (behind) {
-      const int at = __builtin_ctzll(behind);
-      auto of = [&](int v) { return __builtin_amdgcn_readlane(v, at); };
-      const int t = of(plan.tiles), rest = unit - units - (of(upto) - of(mine));
-      np = of(cut);
-      head = rest / t, tile = t - 1 - rest % t;
-      first = pieces + of(p_upto) - of(mine * cut) + rest * np;
-      seq_start = of(plan.start), seq_n = of(plan.n);
-      break;
-    }
-    units += __builtin_amdgcn_readlane(upto, 63);
-    pieces += __builtin_amdgcn_readlane(p_upto, 63);
-  }
-  if (np == 1) return;
-  const Heads hd(a, a.kv_first + head);
-  const int G = hd.j1 - hd.j0, in_tile = part * R + int(threadIdx.x) / L, rr = tile * kTileRows + in_tile, c = int(threadIdx.x) % L * 8;
-  if (rr >= min(seq_n, a.max_new) * G) return;
-  const int i = rr / G, j = hd.j0 + rr - i * G;
-  const float* const p0 = a.tile_parts + (int64_t(first) * kTileRows + in_tile) * (D + kPartPad);
-  constexpr int64_t kNext = int64_t(kTileRows) * (D + kPartPad);
-  float top = -INFINITY;
-  for (int p = 0; p < np; ++p) top = fmaxf(top, p0[p * kNext + D]);
-  const float base = top == -INFINITY ? 0.f : top;
-  f32x4 lo = {0.f, 0.f, 0.f, 0.f}, hi = lo;
-  float sum = 0.f;
-#pragma unroll 4
-  for (int p = 0; p < np; ++p) {
-    const float* const q = p0 + p * kNext;
-    const float w = fast_exp2(q[D] - base);
-    sum = fmaf(w, q[D + 1], sum);
-    lo += w * *reinterpret_cast<const f32x4*>(q + c);
-    hi += w * *reinterpret_cast<const f32x4*>(q + c + 4);
-  }
-  const float inv = sum == 0.f ? 0.f : 1.0f / sum;
-  u32x4 out;
+  plan.units = a.plan[0], plan.total = a.plan[1], plan.piece_tiles = a.plan[2];
+  if (plan.total == plan.units) return;
+  plan.load(a, threadIdx.x & 63);
+  const int grp = threadIdx.x / L, c = int(threadIdx.x) % L * 8;
+  const bool lengthy = plan.total >= 16 * plan.units;
+  const int per_unit = lengthy ? kTileRows : kTileRows / G;
+  for (int job = wg; job < plan.units * per_unit; job += n_wgs) {
+    const int first = plan.find_unit(a, job / per_unit), np = plan.n_pieces;
+    if (np == 1) continue;
+    const Heads hd(a, a.kv_first + plan.head);
+    const int heads = hd.j1 - hd.j0, in_tile = lengthy ? job % per_unit : job % per_unit * G + grp, rr = plan.tile * kTileRows + in_tile;
+    const bool there = rr < min(plan.seq_n, a.max_new) * heads;
+    const float* const p0 = a.tile_parts + (int64_t(first) * kTileRows + in_tile) * W;
+    const int64_t next = int64_t(plan.tiles_there) * kTileRows * W;
+    float top = -INFINITY, sum = 0.f;
+    f32x4 lo = {0.f, 0.f, 0.f, 0.f}, hi = lo;
+    const int by = lengthy ? G : 1;
+    for (int p = lengthy ? grp : 0; there && p < np; p += by * AT_ONCE) {
+      float m[AT_ONCE], l[AT_ONCE];
+      f32x4 x[AT_ONCE], y[AT_ONCE];
 #pragma unroll
-  for (int k = 0; k < 2; ++k) {
-    out[k] = uint32_t(ntp_gemm::f32_to_bf16(lo[2 * k] * inv)) | uint32_t(ntp_gemm::f32_to_bf16(lo[2 * k + 1] * inv)) << 16;
-    out[2 + k] = uint32_t(ntp_gemm::f32_to_bf16(hi[2 * k] * inv)) | uint32_t(ntp_gemm::f32_to_bf16(hi[2 * k + 1] * inv)) << 16;
+      for (int k = 0; k < AT_ONCE; ++k) {
+        m[k] = -INFINITY, l[k] = 0.f, x[k] = y[k] = f32x4{0.f, 0.f, 0.f, 0.f};
+        if (p + k * by < np) {
+          const float* const q = p0 + (p + k * by) * next;
+          m[k] = q[D], l[k] = q[D + 1], x[k] = *reinterpret_cast<const f32x4*>(q + c), y[k] = *reinterpret_cast<const f32x4*>(q + c + 4);
+        }
+      }
+      float more = top;
+#pragma unroll
+      for (int k = 0; k < AT_ONCE; ++k) more = fmaxf(more, m[k]);
+      const float base = more == -INFINITY ? 0.f : more, old = fast_exp2(top - base);
+      sum *= old, lo *= old, hi *= old, top = more;
+#pragma unroll
+      for (int k = 0; k < AT_ONCE; ++k) {
+        const float w = fast_exp2(m[k] - base);
+        sum = fmaf(w, l[k], sum), lo += w * x[k], hi += w * y[k];
+      }
+    }
+    if (lengthy) {  // (the same in the whole workgroup)
+      rows_of[grp][c / 8][0] = lo, rows_of[grp][c / 8][1] = hi;
+      if (c == 0) sums_of[grp] = float2{top, sum};
+      __syncthreads();
+      if (grp == 0) {
+        for (int k = 1; k < G; ++k) top = fmaxf(top, sums_of[k].x);
+        const float base = top == -INFINITY ? 0.f : top;
+        sum = 0.f, lo = hi = f32x4{0.f, 0.f, 0.f, 0.f};
+        for (int k = 0; k < G; ++k) {
+          const float w = fast_exp2(sums_of[k].x - base);
+          sum = fmaf(w, sums_of[k].y, sum), lo += w * rows_of[k][c / 8][0], hi += w * rows_of[k][c / 8][1];
+        }
+      }
+      __syncthreads();
+      if (grp > 0) continue;
+    }
+    if (!there) continue;
+    const float inv = sum == 0.f ? 0.f : 1.0f / sum;
+    u32x4 out;
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+      out[k] = uint32_t(ntp_gemm::f32_to_bf16(lo[2 * k] * inv)) | uint32_t(ntp_gemm::f32_to_bf16(lo[2 * k + 1] * inv)) << 16;
+      out[2 + k] = uint32_t(ntp_gemm::f32_to_bf16(hi[2 * k] * inv)) | uint32_t(ntp_gemm::f32_to_bf16(hi[2 * k + 1] * inv)) << 16;
+    }
+    const int i = rr / heads, j = hd.j0 + rr - i * heads;
+    *reinterpret_cast<u32x4*>(a.C + int64_t(plan.seq_start + i) * a.ldc + int64_t(j) * D + c) = out;
+    if (c == 0 && a.LSE) a.LSE[int64_t(j) * a.M + plan.seq_start + i] = ((top == -INFINITY ? 0.f : top) + log2f(sum)) * 0.6931471805599453f;
   }
-  *reinterpret_cast<u32x4*>(a.C + int64_t(seq_start + i) * a.ldc + int64_t(j) * D + c) = out;
-  if (c == 0 && a.LSE) a.LSE[int64_t(j) * a.M + seq_start + i] = (base + log2f(sum)) * 0.6931471805599453f;
 }
 
 }  // namespace ntp_chunk

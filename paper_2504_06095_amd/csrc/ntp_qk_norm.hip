@@ -135,26 +135,18 @@ __global__ __launch_bounds__(kThreads) void qk_norm_append_kernel(const AppendAr
   __shared__ int64_t slot_of[kMaxTokens];
   const int64_t row0 = int64_t(blockIdx.x) * a.tokens;
   const int rows = int(std::min<int64_t>(a.tokens, a.M - row0));
-  if (int(threadIdx.x) < rows) slot_of[threadIdx.x] = a.slots ? a.slots[row0 + threadIdx.x] : -1;
-  angles(cs, a.positions, a.inv_freq, row0, rows, a.rotary_dim / 2);
-
   const int j = int(threadIdx.x) & (kHead - 1), rot = a.rotary_dim / 16;
   const bool turned = j < rot;
   // this lane's 8 + 8 elements of a query or key head: pairs number 8 j .. 8 j + 7, or two chunks behind the rotated part; of a value head
   const int c0 = (turned ? (a.interleaved ? 2 * j : j) : 2 * j) * 8, c1 = (turned ? (a.interleaved ? 2 * j + 1 : j + rot) : 2 * j + 1) * 8;
   const int v0 = j * 8, v1 = (j + kHead) * 8;
-  u32x4 gq0{}, gq1{}, gk0{}, gk1{};
-  if (a.q_gamma) gq0 = load_16(a.q_gamma + c0), gq1 = load_16(a.q_gamma + c1);
-  if (a.k_gamma) gk0 = load_16(a.k_gamma + c0), gk1 = load_16(a.k_gamma + c1);
-  __syncthreads();
-
   const int heads = a.q_cnt + 2 * a.kv_cnt, per_row = heads << kLog2;
   int t = int(threadIdx.x) / per_row, at = int(threadIdx.x) % per_row;
   const int dt = kThreads / per_row, dat = kThreads % per_row;
-  constexpr int kItems = 2;  // of a thread, whose loads go out together
-  while (t < rows) {
-    int tn[kItems], hn[kItems];
-    u32x4 xw[kItems], yw[kItems];
+  constexpr int kItems = 2;  // of a thread, whose loads go out together; the first ones before the angles are formed
+  int tn[kItems], hn[kItems];
+  u32x4 xw[kItems], yw[kItems];
+  auto fetch = [&] {
 #pragma unroll
     for (int n = 0; n < kItems; ++n) {
       tn[n] = t, hn[n] = at >> kLog2;
@@ -168,6 +160,16 @@ __global__ __launch_bounds__(kThreads) void qk_norm_append_kernel(const AppendAr
       at += dat;
       if (at >= per_row) at -= per_row, ++t;
     }
+  };
+  fetch();
+  if (int(threadIdx.x) < rows) slot_of[threadIdx.x] = a.slots ? a.slots[row0 + threadIdx.x] : -1;
+  u32x4 gq0{}, gq1{}, gk0{}, gk1{};
+  if (a.q_gamma) gq0 = load_16(a.q_gamma + c0), gq1 = load_16(a.q_gamma + c1);
+  if (a.k_gamma) gk0 = load_16(a.k_gamma + c0), gk1 = load_16(a.k_gamma + c1);
+  angles(cs, a.positions, a.inv_freq, row0, rows, a.rotary_dim / 2);
+  __syncthreads();
+
+  while (tn[0] < rows) {
 #pragma unroll
     for (int n = 0; n < kItems; ++n) {
       if (tn[n] >= rows) continue;  // (all lanes of a head together)
@@ -227,19 +229,26 @@ __global__ __launch_bounds__(kThreads) void qk_norm_append_kernel(const AppendAr
         if (j == 0) (is_v ? a.V_exp : a.K_exp)[page * a.exp_stride + in_head] = uint8_t(code);
       }
     }
+    fetch();
   }
 }
 
 // ---- gradient ---------------------------------------------------------------------------------------
+// The query heads' part and the key heads' have workgroups of their own (fewer registers than sums of both gammas in one: 4 wavefronts a SIMD more).
+struct BwdSide {
+  const uint16_t *x, *up, *gamma;  // the first head's columns of QKV, its gradient, and the weights of its norm (NULL: none)
+  uint16_t* out;                   // the first head's columns of dQKV
+  float* d_gamma;                  // where parts is NULL: one workgroup of the side writes it itself; NULL: not wanted
+  int64_t ldup;
+  int32_t heads, tokens, wgs, wanted;  // heads; tokens of a workgroup at a time; workgroups; whether the gamma's gradient is formed
+};
 struct BwdArgs {
-  const uint16_t *QKV, *dQ, *dK, *q_gamma, *k_gamma;
-  uint16_t* dQKV;           // NULL: the gammas' gradients alone
-  float* parts;             // [workgroup][2][D] partial sums of the gammas' gradients
-  float *d_q, *d_k;         // where parts is NULL: one workgroup writes what is wanted of them itself
+  BwdSide q, k;
+  float* parts;  // [workgroup][D] partial sums of the gammas' gradients
   const int32_t* positions;
   const double* inv_freq;
-  int64_t M, ldqkv, lddq, lddk, lddqkv;
-  int32_t q_cnt, kv_cnt, rotary_dim, interleaved, tokens, accumulate;
+  int64_t M, ldx, ldout;
+  int32_t rotary_dim, interleaved, accumulate, store;
   float eps;
 };
 
@@ -247,39 +256,49 @@ template <int D>
 __global__ __launch_bounds__(kThreads) void qk_norm_bwd_kernel(const BwdArgs a) {
   constexpr int kHead = D / 16, kLog2 = D == 128 ? 3 : 2;
   __shared__ float2 cs[kMaxTokens][kMaxPairs];
-  __shared__ float sums[kThreads / 64][2][D];
+  __shared__ float sums[kThreads / 64][D];
+  const bool is_q = int(blockIdx.x) < a.q.wgs;
+  const BwdSide& s = is_q ? a.q : a.k;
+  const int wg = int(blockIdx.x) - (is_q ? 0 : a.q.wgs);
   const int j = int(threadIdx.x) & (kHead - 1), rot = a.rotary_dim / 16;
   const bool turned = j < rot;
   const int c0 = (turned ? (a.interleaved ? 2 * j : j) : 2 * j) * 8, c1 = (turned ? (a.interleaved ? 2 * j + 1 : j + rot) : 2 * j + 1) * 8;
-  u32x4 gq0{}, gq1{}, gk0{}, gk1{};
-  if (a.q_gamma) gq0 = load_16(a.q_gamma + c0), gq1 = load_16(a.q_gamma + c1);
-  if (a.k_gamma) gk0 = load_16(a.k_gamma + c0), gk1 = load_16(a.k_gamma + c1);
-  float dgq[16] = {}, dgk[16] = {};
-  const int per_row = (a.q_cnt + a.kv_cnt) << kLog2;
+  u32x4 gw0{}, gw1{};
+  if (s.gamma) gw0 = load_16(s.gamma + c0), gw1 = load_16(s.gamma + c1);
+  float dg[16] = {};
+  const int per_row = s.heads << kLog2;
   const int dt = kThreads / per_row, dat = kThreads % per_row;
-  for (int64_t row0 = int64_t(blockIdx.x) * a.tokens; row0 < a.M; row0 += int64_t(gridDim.x) * a.tokens) {
-    const int rows = int(std::min<int64_t>(a.tokens, a.M - row0));
+  for (int64_t row0 = int64_t(wg) * s.tokens; row0 < a.M; row0 += int64_t(s.wgs) * s.tokens) {
+    const int rows = int(std::min<int64_t>(s.tokens, a.M - row0));
+    int t = int(threadIdx.x) / per_row, at = int(threadIdx.x) % per_row;
+    u32x4 xw[4];
+    auto fetch = [&] {
+      if (t >= rows) return;
+      const int64_t row = row0 + t, col = int64_t(at >> kLog2) * D;
+      const uint16_t *const src = s.x + row * a.ldx + col, *const up = s.up + row * s.ldup + col;
+      xw[0] = load_16(src + c0), xw[1] = load_16(src + c1), xw[2] = load_16(up + c0), xw[3] = load_16(up + c1);
+    };
+    fetch();  // (on its way while the angles are formed)
     __syncthreads();  // the angles of the rows before have been used
     angles(cs, a.positions, a.inv_freq, row0, rows, a.rotary_dim / 2);
     __syncthreads();
-    int t = int(threadIdx.x) / per_row, at = int(threadIdx.x) % per_row;
     while (t < rows) {
-      const int head = at >> kLog2;
-      const int64_t row = row0 + t;
-      const bool is_q = head < a.q_cnt;
-      const uint16_t* const src = a.QKV + row * a.ldqkv + int64_t(head) * D;
-      const uint16_t* const up = is_q ? a.dQ + row * a.lddq + int64_t(head) * D : a.dK + row * a.lddk + int64_t(head - a.q_cnt) * D;
-      const bool norm = is_q ? a.q_gamma != nullptr : a.k_gamma != nullptr;
       float x[8], y[8], u[8], w[8];
-      unpack(load_16(src + c0), x);
-      unpack(load_16(src + c1), y);
-      unpack(load_16(up + c0), u);
-      unpack(load_16(up + c1), w);
-      if (turned) turn(u, w, &cs[t][8 * j], a.interleaved, -1.0f);
-      if (norm) {
+      unpack(xw[0], x);
+      unpack(xw[1], y);
+      unpack(xw[2], u);
+      unpack(xw[3], w);
+      uint16_t* const out = s.out + (row0 + t) * a.ldout + int64_t(at >> kLog2) * D;
+      const float2* const angle = &cs[t][8 * j];
+      t += dt;
+      at += dat;
+      if (at >= per_row) at -= per_row, ++t;
+      fetch();
+      if (turned) turn(u, w, angle, a.interleaved, -1.0f);
+      if (s.gamma) {
         float g0[8], g1[8], ss = 0.f, dot = 0.f;
-        unpack(is_q ? gq0 : gk0, g0);
-        unpack(is_q ? gq1 : gk1, g1);
+        unpack(gw0, g0);
+        unpack(gw1, g1);
 #pragma unroll
         for (int k = 0; k < 8; ++k) {
           ss = fmaf(x[k], x[k], fmaf(y[k], y[k], ss));
@@ -291,58 +310,52 @@ __global__ __launch_bounds__(kThreads) void qk_norm_bwd_kernel(const BwdArgs a) 
 #pragma unroll
         for (int k = 0; k < 8; ++k) {
           const float xh = x[k] * rstd, yh = y[k] * rstd;
-          if (is_q) dgq[k] = fmaf(u[k], xh, dgq[k]), dgq[8 + k] = fmaf(w[k], yh, dgq[8 + k]);
-          else dgk[k] = fmaf(u[k], xh, dgk[k]), dgk[8 + k] = fmaf(w[k], yh, dgk[8 + k]);
+          dg[k] = fmaf(u[k], xh, dg[k]), dg[8 + k] = fmaf(w[k], yh, dg[8 + k]);
           u[k] = (u[k] * g0[k] - xh * mean) * rstd;
           w[k] = (w[k] * g1[k] - yh * mean) * rstd;
         }
       }
-      if (a.dQKV) {
-        uint16_t* const out = a.dQKV + row * a.lddqkv + int64_t(head) * D;
+      if (a.store) {
         store_16(out + c0, pack(u));
         store_16(out + c1, pack(w));
       }
-      t += dt;
-      at += dat;
-      if (at >= per_row) at -= per_row, ++t;
     }
   }
-  if (!a.parts && !a.d_q && !a.d_k) return;
+  if (!s.wanted) return;
   const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
 #pragma unroll
-  for (int k = 0; k < 16; ++k) dgq[k] = over_same<D>(dgq[k]), dgk[k] = over_same<D>(dgk[k]);
+  for (int k = 0; k < 16; ++k) dg[k] = over_same<D>(dg[k]);
   if (lane < kHead) {
 #pragma unroll
-    for (int k = 0; k < 8; ++k) {
-      sums[wave][0][c0 + k] = dgq[k], sums[wave][0][c1 + k] = dgq[8 + k];
-      sums[wave][1][c0 + k] = dgk[k], sums[wave][1][c1 + k] = dgk[8 + k];
-    }
+    for (int k = 0; k < 8; ++k) sums[wave][c0 + k] = dg[k], sums[wave][c1 + k] = dg[8 + k];
   }
   __syncthreads();
-  for (int i = threadIdx.x; i < 2 * D; i += kThreads) {
-    const int which = i / D, c = i % D;
-    const float v = (sums[0][which][c] + sums[1][which][c]) + (sums[2][which][c] + sums[3][which][c]);
-    float* const out = which ? a.d_k : a.d_q;
-    if (a.parts) a.parts[int64_t(blockIdx.x) * 2 * D + i] = v;
-    else if (out) out[c] = a.accumulate ? out[c] + v : v;
-  }
+  const int c = threadIdx.x;
+  if (c >= D) return;
+  const float v = (sums[0][c] + sums[1][c]) + (sums[2][c] + sums[3][c]);
+  if (a.parts) a.parts[int64_t(blockIdx.x) * D + c] = v;
+  else s.d_gamma[c] = a.accumulate ? s.d_gamma[c] + v : v;
 }
 
-// Adds up n partial sums of one gamma's gradient (blockIdx.y), 16 columns a workgroup.
+// Adds up the partial sums of one gamma's gradient (blockIdx.y; the first n_q are the query heads'), 16 columns a workgroup, 64 of them side by side.
+constexpr int kSumThreads = 1024;
 template <int D>
-__global__ __launch_bounds__(kThreads) void qk_norm_sum_kernel(const float* parts, int n, float* d_q, float* d_k, int accumulate) {
-  __shared__ float rows[16][17];
+__global__ __launch_bounds__(kSumThreads) void qk_norm_sum_kernel(const float* parts, int n_q, int n_k, float* d_q, float* d_k, int accumulate) {
+  __shared__ float rows[64][17];
   float* const out = blockIdx.y == 0 ? d_q : d_k;
   if (!out) return;
-  const int c = threadIdx.x & 15, r = threadIdx.x >> 4, col = int(blockIdx.x) * 16 + c;
+  const int n = blockIdx.y == 0 ? n_q : n_k, c = threadIdx.x & 15, r = threadIdx.x >> 4, col = int(blockIdx.x) * 16 + c;
+  parts += blockIdx.y == 0 ? 0 : int64_t(n_q) * D;
   float sum = 0.f;
 #pragma unroll 8
-  for (int i = r; i < n; i += 16) sum += parts[int64_t(i) * 2 * D + blockIdx.y * D + col];
+  for (int i = r; i < n; i += 64) sum += parts[int64_t(i) * D + col];
   rows[r][c] = sum;
   __syncthreads();
-  if (r > 0) return;
-  for (int i = 1; i < 16; ++i) sum += rows[i][c];
-  out[col] = accumulate ? out[col] + sum : sum;
+  for (int half = 32; half > 0; half /= 2) {
+    if (r < half) rows[r][c] += rows[r + half][c];
+    __syncthreads();
+  }
+  if (r == 0) out[col] = accumulate ? out[col] + rows[0][c] : rows[0][c];
 }
 
 int check_shape(const ntp_kv_append_shape_t* s) {
@@ -364,9 +377,17 @@ int32_t tokens_of(int64_t M, int64_t items_per_row, int64_t wgs) {
   return int32_t(std::max<int64_t>(1, std::min(most, M / wgs)));
 }
 
-int32_t bwd_workgroups(const ntp_handle* h, const ntp_kv_append_shape_t* s, int32_t* tokens) {
-  *tokens = tokens_of(s->M, int64_t(s->q_cnt + s->kv_cnt) * (s->head_dim / 16), 2 * int64_t(h->compute_units));
-  return int32_t(std::min<int64_t>((s->M + *tokens - 1) / *tokens, 4 * int64_t(h->compute_units)));
+// Workgroups of both sides of the gradient, in proportion to their heads: up to four on every compute unit.
+void bwd_sides(const ntp_handle* h, const ntp_kv_append_shape_t* s, BwdSide* q, BwdSide* k) {
+  const int64_t all = 4 * int64_t(h->compute_units), heads = std::max(s->q_cnt + s->kv_cnt, 1);
+  auto side = [&](BwdSide* d, int32_t n) {
+    const int64_t room = std::max<int64_t>(1, all * n / heads);
+    d->heads = n;
+    d->tokens = tokens_of(s->M, int64_t(n) * (s->head_dim / 16), std::max<int64_t>(1, room / 2));
+    d->wgs = n == 0 ? 0 : int32_t(std::min<int64_t>((s->M + d->tokens - 1) / d->tokens, room));
+  };
+  side(q, s->q_cnt);
+  side(k, s->kv_cnt);
 }
 
 }  // namespace
@@ -374,8 +395,9 @@ int32_t bwd_workgroups(const ntp_handle* h, const ntp_kv_append_shape_t* s, int3
 int ntp::qk_norm_workspace_wish(const ntp_handle* h, const ntp_kv_append_shape_t* s, int64_t* bytes) {
   const int st = check_shape(s);
   if (st != NTP_OK) return NTP_ERR_INVALID_ARG;
-  int32_t tokens;
-  *bytes = s->M == 0 || s->q_cnt + s->kv_cnt == 0 ? 0 : int64_t(bwd_workgroups(h, s, &tokens)) * 2 * s->head_dim * 4;
+  BwdSide q{}, k{};
+  bwd_sides(h, s, &q, &k);
+  *bytes = s->M == 0 || q.wgs + k.wgs <= 2 ? 0 : int64_t(q.wgs + k.wgs) * s->head_dim * 4;
   return NTP_OK;
 }
 
@@ -454,39 +476,48 @@ extern "C" int ntp_qk_norm_shard_bwd(ntp_handle_t* h, const ntp_kv_append_shape_
   }
   if (h->device < 0) return NTP_ERR_NO_DEVICE;
   BwdArgs a{};
-  a.QKV = static_cast<const uint16_t*>(QKV), a.dQ = static_cast<const uint16_t*>(dQ), a.dK = static_cast<const uint16_t*>(dK), a.dQKV = static_cast<uint16_t*>(dQKV);
-  if (norm) a.q_gamma = static_cast<const uint16_t*>(norm->q_gamma), a.k_gamma = static_cast<const uint16_t*>(norm->k_gamma), a.eps = norm->eps;
-  a.positions = positions, a.inv_freq = inv_freq, a.M = rows ? s->M : 0, a.ldqkv = ldqkv, a.lddq = lddq, a.lddk = lddk, a.lddqkv = lddqkv;
-  a.q_cnt = s->q_cnt, a.kv_cnt = s->kv_cnt, a.rotary_dim = s->rotary_dim, a.interleaved = s->interleaved != 0;
-  const int32_t n = rows ? bwd_workgroups(h, s, &a.tokens) : 0;
+  bwd_sides(h, s, &a.q, &a.k);
+  a.q.x = static_cast<const uint16_t*>(QKV), a.k.x = a.q.x + wq, a.q.up = static_cast<const uint16_t*>(dQ), a.k.up = static_cast<const uint16_t*>(dK);
+  a.q.out = static_cast<uint16_t*>(dQKV), a.k.out = a.q.out + wq, a.q.ldup = lddq, a.k.ldup = lddk;
+  if (norm) a.q.gamma = static_cast<const uint16_t*>(norm->q_gamma), a.k.gamma = static_cast<const uint16_t*>(norm->k_gamma), a.eps = norm->eps;
+  a.positions = positions, a.inv_freq = inv_freq, a.M = rows ? s->M : 0, a.ldx = ldqkv, a.ldout = lddqkv;
+  a.rotary_dim = s->rotary_dim, a.interleaved = s->interleaved != 0, a.accumulate = accumulate;
+  if (!rows) a.q.wgs = a.k.wgs = 0;
   hipStream_t hs = static_cast<hipStream_t>(stream);
-  const bool sums = d_q_gamma || d_k_gamma, room = h->workspace && h->workspace_bytes >= int64_t(n) * 2 * d * 4;
-  auto launch = [&](int grid) {
-    if (d == 128) hipLaunchKernelGGL(qk_norm_bwd_kernel<128>, dim3(uint32_t(grid)), dim3(kThreads), 0, hs, a);
-    else hipLaunchKernelGGL(qk_norm_bwd_kernel<64>, dim3(uint32_t(grid)), dim3(kThreads), 0, hs, a);
+  const bool sums = d_q_gamma || d_k_gamma, few = a.q.wgs <= 1 && a.k.wgs <= 1, room = h->workspace && h->workspace_bytes >= int64_t(a.q.wgs + a.k.wgs) * d * 4;
+  auto launch = [&] {
+    const dim3 grid{uint32_t(a.q.wgs + a.k.wgs)};
+    if (d == 128) hipLaunchKernelGGL(qk_norm_bwd_kernel<128>, grid, dim3(kThreads), 0, hs, a);
+    else hipLaunchKernelGGL(qk_norm_bwd_kernel<64>, grid, dim3(kThreads), 0, hs, a);
     return hipGetLastError() == hipSuccess;
   };
-  auto add_up = [&](const float* parts, int count) {
+  auto add_up = [&](float* d_q, float* d_k) {
     const dim3 grid{uint32_t(d / 16), 2};
-    if (d == 128) hipLaunchKernelGGL(qk_norm_sum_kernel<128>, grid, dim3(kThreads), 0, hs, parts, count, d_q_gamma, d_k_gamma, accumulate);
-    else hipLaunchKernelGGL(qk_norm_sum_kernel<64>, grid, dim3(kThreads), 0, hs, parts, count, d_q_gamma, d_k_gamma, accumulate);
+    if (d == 128) hipLaunchKernelGGL(qk_norm_sum_kernel<128>, grid, dim3(kSumThreads), 0, hs, a.parts, a.q.wgs, a.k.wgs, d_q, d_k, accumulate);
+    else hipLaunchKernelGGL(qk_norm_sum_kernel<64>, grid, dim3(kSumThreads), 0, hs, a.parts, a.q.wgs, a.k.wgs, d_q, d_k, accumulate);
     return hipGetLastError() == hipSuccess;
   };
   if (ntp::timing_on(h)) ntp::timing_begin(h, stream, "qk_norm_bwd", 0.0, 6.0 * double(a.M) * double(wq + wk));
   bool ok = true;
-  if (sums && n == 0) {
-    ok = add_up(nullptr, 0);
-  } else if (sums && n > 1 && room) {
+  a.store = 1;
+  a.q.wanted = d_q_gamma != nullptr, a.k.wanted = d_k_gamma != nullptr;
+  if (sums && room && !few) {
     a.parts = static_cast<float*>(h->workspace);
-    ok = launch(n) && add_up(a.parts, n);
+    ok = launch() && add_up(d_q_gamma, d_k_gamma);
   } else {
-    if (sums) {  // one workgroup forms them, before dQKV may take the place of dQ and dK
-      a.d_q = d_q_gamma, a.d_k = d_k_gamma, a.accumulate = accumulate;
-      if (n > 1) a.dQKV = nullptr;
-      ok = launch(1);
-      a.d_q = a.d_k = nullptr, a.dQKV = static_cast<uint16_t*>(dQKV);
+    if (sums) {
+      float* const none_q = a.q.wgs == 0 ? d_q_gamma : nullptr;  // a sum over no heads or no tokens
+      float* const none_k = a.k.wgs == 0 ? d_k_gamma : nullptr;
+      if (none_q || none_k) ok = add_up(none_q, none_k);
+      a.q.d_gamma = d_q_gamma, a.k.d_gamma = d_k_gamma;
+      if (!few) {  // one workgroup of each side forms them, before dQKV may take the place of dQ and dK
+        const int32_t n_q = a.q.wgs, n_k = a.k.wgs;
+        a.q.wgs = std::min(n_q, 1), a.k.wgs = std::min(n_k, 1), a.store = 0;
+        ok = ok && launch();
+        a.q.wgs = n_q, a.k.wgs = n_k, a.store = 1, a.q.wanted = a.k.wanted = 0;
+      }
     }
-    if (!sums || n > 1) ok = ok && launch(n);
+    if (a.q.wgs + a.k.wgs > 0) ok = ok && launch();
   }
   ntp::timing_end(h, stream);
   return ok ? NTP_OK : NTP_ERR_LAUNCH;
