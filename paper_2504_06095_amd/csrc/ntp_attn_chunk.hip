@@ -33,7 +33,7 @@ __global__ __attribute__((amdgpu_flat_work_group_size(kThreads, kThreads), amdgp
 }
 
 template <int D, bool FP8>
-__global__ __attribute__((amdgpu_flat_work_group_size(kThreads, kThreads), amdgpu_waves_per_eu(kPlaces<D>, kPlaces<D>))) void chunk_tiles_kernel(const ChunkArgs a) {
+__global__ __attribute__((amdgpu_flat_work_group_size(kThreads, kThreads), amdgpu_waves_per_eu(kPlaces<D, FP8>, kPlaces<D, FP8>))) void chunk_tiles_kernel(const ChunkArgs a) {
   __shared__ __attribute__((aligned(1024))) unsigned char lds[kTileLds<D>];
   chunk_tiles<D, FP8>(a, int(blockIdx.x), lds);
 }
@@ -84,7 +84,7 @@ struct ChunkChoice {
   int64_t ws_rows, ws_bytes;        // bytes of the line's partial results, and of all
 };
 
-ChunkChoice choose_chunk(const ntp_handle* h, int64_t ws_bytes, const ntp_attn_chunk_shape_t* s) {
+ChunkChoice choose_chunk(const ntp_handle* h, int64_t ws_bytes, const ntp_attn_chunk_shape_t* s, bool fp8) {
   ChunkChoice c{};
   const int64_t most = std::min<int64_t>(s->max_new, s->M);  // rows of a sequence
   if (s->q_cnt == 0 || s->n_seq == 0 || most == 0) return c;
@@ -102,12 +102,12 @@ ChunkChoice choose_chunk(const ntp_handle* h, int64_t ws_bytes, const ntp_attn_c
     const int64_t all = s->M * c.gmax;
     c.tiles = c.kv_used * std::min<int64_t>(s->n_seq * ((most * c.gmax + kTileRows - 1) / kTileRows), all / kTileRows + std::min<int64_t>(s->n_seq, all / (c.cap + 1)));
   }
-  const int64_t step = (s->head_dim == 128 ? 128 : 256), steps = std::max<int64_t>((s->max_len + step - 1) / step, 1);  // (8-bit steps of up to 16 rows are twice as long)
+  const int64_t step = s->head_dim == 128 ? 128 : 256, steps = std::max<int64_t>((s->max_len + step - 1) / step, 1);  // (8-bit steps of up to 16 rows are twice as long)
   if (c.units > 0 && steps > 4 && (steps > 8 || c.units < h->compute_units / 2)) {
     c.shares = int32_t(std::min<int64_t>(std::min(2 * int64_t(h->compute_units), steps * c.units), kMaxShares));
     c.ws_rows = (int64_t(c.shares) * 2 * c.cap * (s->head_dim + 2) * 4 + 255) / 256 * 256;
   }
-  if (tiles && s->max_len > kMinPiece * kTileKeys) c.slots = (s->head_dim == 64 && c.cap == 0 ? kPlaces<64> : kPlaces<128>) * h->compute_units;
+  if (tiles && s->max_len > kMinPiece * kTileKeys) c.slots = (s->head_dim == 64 && c.cap == 0 && !fp8 ? kPlaces<64, false> : kPlaces<128, false>) * h->compute_units;
   c.ws_bytes = c.ws_rows + (c.slots > 0 ? 256 + int64_t(2 * c.slots) * kTileRows * (s->head_dim + kPartPad) * 4 : 0);
   if (c.ws_bytes > ws_bytes) c.shares = c.slots = 0, c.ws_rows = c.ws_bytes = 0;
   c.row_wgs = int32_t(c.shares > 0 ? c.shares : c.units);
@@ -119,7 +119,7 @@ ChunkChoice choose_chunk(const ntp_handle* h, int64_t ws_bytes, const ntp_attn_c
 
 int ntp::attn_chunk_workspace_wish(const ntp_handle* h, const ntp_attn_chunk_shape_t* s, int64_t* bytes) {
   if (check_chunk_shape(s) != NTP_OK) return NTP_ERR_INVALID_ARG;
-  *bytes = choose_chunk(h, INT64_MAX, s).ws_bytes;
+  *bytes = std::max(choose_chunk(h, INT64_MAX, s, false).ws_bytes, choose_chunk(h, INT64_MAX, s, true).ws_bytes);
   return NTP_OK;
 }
 
@@ -162,7 +162,8 @@ extern "C" int ntp_attn_chunk_shard(ntp_handle_t* h, const ntp_attn_chunk_shape_
   auto off4 = [](const void* p) { return (reinterpret_cast<uintptr_t>(p) & 3) != 0; };
   if (off16(Q) || off16(C) || ldq % 8 || ldc % 8 || off4(row_starts) || off4(block_table) || off4(lengths) || off4(LSE)) return NTP_ERR_ALIGNMENT;
   if (h->device < 0) return NTP_ERR_NO_DEVICE;
-  const ChunkChoice c = choose_chunk(h, h->workspace ? h->workspace_bytes : 0, s);
+  const bool fp8 = pages->format == NTP_KV_E4M3;
+  const ChunkChoice c = choose_chunk(h, h->workspace ? h->workspace_bytes : 0, s, fp8);
   ChunkArgs a{};
   a.Q = static_cast<const uint16_t*>(Q), a.K = static_cast<const unsigned char*>(pages->K), a.V = static_cast<const unsigned char*>(pages->V);
   a.K_exp = static_cast<const uint8_t*>(pages->K_exp), a.V_exp = static_cast<const uint8_t*>(pages->V_exp);
@@ -178,10 +179,9 @@ extern "C" int ntp_attn_chunk_shard(ntp_handle_t* h, const ntp_attn_chunk_shape_
   a.ldq = ldq, a.ldc = ldc, a.ldt = ldt, a.page_stride = pages->page_stride, a.exp_stride = pages->exp_stride;
   a.M = int32_t(s->M), a.n_pages = int32_t(pages->n_pages), a.n_seq = s->n_seq, a.max_new = s->max_new, a.max_len = s->max_len;
   a.q_cnt = s->q_cnt, a.q_off = s->q_off, a.kv_off = s->kv_off, a.group = s->group, a.page_size = pages->page_size, a.page_log2 = ntp::log2_of(pages->page_size);
-  a.kv_first = c.kv_first, a.kv_used = c.kv_used, a.gmax = c.gmax, a.cap = c.cap, a.shares = c.shares, a.row_wgs = c.row_wgs, a.slots = c.slots;
+  a.kv_first = c.kv_first, a.kv_used = c.kv_used, a.gmax = c.gmax, a.cap = c.cap, a.shares = c.shares, a.row_wgs = c.row_wgs, a.slots = c.slots, a.parts = int32_t(h->opt[NTP_OPT_ATTN_PARTS]);
   a.scale_log2 = float(1.4426950408889634 / std::sqrt(double(s->head_dim)));
   hipStream_t hs = static_cast<hipStream_t>(stream);
-  const bool fp8 = pages->format == NTP_KV_E4M3;
   if (ntp::timing_on(h)) ntp::timing_begin(h, stream, fp8 ? "attn_chunk8" : "attn_chunk", 4.0 * double(s->M) * double(s->max_len) * s->head_dim * s->q_cnt, 0.0);
   const bool ok = s->head_dim == 128 ? (fp8 ? launch_chunk<128, true>(a, c, hs) : launch_chunk<128, false>(a, c, hs))
                                      : (fp8 ? launch_chunk<64, true>(a, c, hs) : launch_chunk<64, false>(a, c, hs));

@@ -84,7 +84,7 @@ struct RowLine {
       for (int from = 0; from < a.n_seq; from += kAtOnce) steps += all_steps(a, from);
     }
     total = steps * per_seq;
-    shares = max(min(a.shares, total), 1);  // (one step at least for each)
+    shares = max(min(a.shares, max(total / 2, min(total, a.shares / 2))), 1);  // (of one step only where compute units would be left over)
     q = total / shares;
     r = total % shares;
   }

@@ -17,8 +17,8 @@ namespace ntp_chunk {
 constexpr int kMinPiece = 4;  // key tiles of a piece at least
 constexpr int kPartPad = 4;   // floats behind a partial row's outputs: maximum, sum
 constexpr int kRun = 4;       // neighbouring pieces, which read the same tokens, that stay on one XCD
-template <int D>
-constexpr int kPlaces = D == 128 ? 2 : 3;  // workgroups that a compute unit has room for
+template <int D, bool FP8>
+constexpr int kPlaces = D == 64 && !FP8 ? 3 : 2;  // workgroups that a compute unit has room for (8-bit tiles of 64 columns: a third takes registers that a walk needs)
 
 // Row tiles and key tiles (of its last row) of a sequence; no row tiles where it is one of few rows.
 __device__ __forceinline__ void tiles_of(const ChunkArgs& a, int n, int len, int& tiles, int& walk) {
@@ -39,7 +39,8 @@ struct TilePlan {
       tiles_of(a, n, len, tiles, walk);
     }
   }
-  __device__ __forceinline__ int cut() const { return piece_tiles == 0 ? 1 : (walk + piece_tiles - 1) / piece_tiles; }
+  // (in fp32: a count one too high where walks are of millions of tiles is the same everywhere)
+  __device__ __forceinline__ int cut() const { return piece_tiles == 0 ? 1 : int((float(walk) - 0.5f) * __builtin_amdgcn_rcpf(float(piece_tiles))) + 1; }
   static constexpr int kAtOnce = 256;  // sequences whose loads go out together
   // of the sequences from .. from + kAtOnce - 1: units and pieces of this lane's
   __device__ __forceinline__ void sums(const ChunkArgs& a, int from, int& count, int& pieces) {
@@ -54,14 +55,8 @@ struct TilePlan {
     }
   }
   __device__ __forceinline__ static int all(int v) { return __builtin_amdgcn_readlane(sum_upto(v), 63); }
-  template <typename F>
-  __device__ __forceinline__ static float all(float v, F&& f) {
-#pragma unroll
-    for (int d = 1; d < 16; d *= 2) v = f(v, __shfl_xor(v, d));
-    return over_rows(v, f);
-  }
-  // A call's time by an estimate in key tiles, for walks cut into pieces of at most S: rounds of whole pieces, or what list scheduling takes at most, and per piece its way in and out and its
-  // partial results.  Taken is the best of whole walks and of one to four rounds.
+  // A call's time by an estimate, in key tiles of two workgroups on a compute unit (2.06 us; 1.6 us of one alone), for walks cut into pieces: rounds of whole pieces, or what list
+  // scheduling takes at most, a round's way in and out, and partial results written and read again (47 ns a piece).  Taken is the best of whole walks and six cuts.
   template <int D>
   __device__ __forceinline__ void make(const ChunkArgs& a) {
     piece_tiles = 0;
@@ -87,9 +82,11 @@ struct TilePlan {
       }
     }
     units = total = all(count);
-    if (a.slots == 0 || units == 0) return;
-    work = all(work, added), most = all(most, larger);
-    const float slots = float(a.slots), share = work / slots;
+    if (a.slots == 0 || units == 0 || units >= 2 * a.slots) return;
+    work = over_wave(work, added), most = over_wave(most, larger);
+    // (KV heads that only a part of their group reads have fewer rows)
+    const float whole = float(a.q_cnt) / float(a.kv_used * a.gmax), slots = float(a.slots), share = work * whole / slots;
+    if (a.parts == 1 || (a.parts == 0 && most <= 1.3f * share)) return;  // (longest first, whole walks end together)
     if (a.n_seq > 64) {  // (not looked at piece by piece)
       if (units >= a.slots || most <= 1.5f * share) return;
       piece_tiles = max(kMinPiece, int(ceilf(share)));
@@ -103,21 +100,34 @@ struct TilePlan {
       piece_tiles = 0, total = units;
       return;
     }
-    auto estimate = [&](int S, int pieces) {
-      const float longest = fminf(float(S), most), rounds = ceilf(float(pieces) / slots);
-      return fminf(rounds * longest, share + 0.5f * longest) + 3.0f * rounds + (pieces > units ? float(pieces) * (1.0f / 85) : 0.0f);
+    const auto longest_of = [&] { return over_wave(tiles > 0 ? float(walk) * __builtin_amdgcn_rcpf(float(cut())) : 0.0f, larger); };
+    auto estimate = [&](float longest, int all_pieces) {
+      const float pieces = float(all_pieces) * whole, rounds = ceilf(pieces / slots);
+      const float walks = 2.0f * pieces <= slots ? 0.78f * longest : fminf(rounds * longest, fmaxf(longest, share + 0.5f * longest));
+      return walks + 3.0f * rounds + (all_pieces > units ? pieces * (1.0f / 45) : 0.0f);
     };
-    float best = estimate(1 << 30, units);
+    float best = estimate(most, units);
     int best_tiles = 0;
-    for (int j = 1; j <= 8; ++j) {
-      const float room = j <= 4 ? slots * float(j) : slots * float(j - 4) - float(units);
-      if (room <= 0.f) continue;
-      piece_tiles = max(kMinPiece, int(ceilf(work / room)));
+    if (a.parts > 1) best = INFINITY;
+    // each wavefront looks at every fourth cut
+    __shared__ float best_of[kWaves];
+    __shared__ int tiles_of_best[kWaves], total_of_best[kWaves];
+    const int wave = uniform(threadIdx.x >> 6);
+    for (int j = wave; j < (a.parts > 0 ? 1 : 6); j += kWaves) {
+      const float S = a.parts > 0 ? most / float(a.parts) : j < 3 ? most / float(j + 2) : work * whole / (j == 3 ? slots : j == 4 ? 0.5f * slots : fmaxf(slots - float(units) * whole, 1.0f));
+      piece_tiles = max(kMinPiece, int(ceilf(S)));
       const int pieces = all(a.kv_used * tiles * cut());
-      const float t = estimate(piece_tiles, pieces);
-      if (pieces <= 2 * a.slots && t < best) best = t, best_tiles = piece_tiles, total = pieces;
+      if (pieces > 2 * a.slots || pieces == units) continue;
+      const float t = estimate(longest_of(), pieces);
+      if (t < best) best = t, best_tiles = piece_tiles, total = pieces;
     }
-    piece_tiles = best_tiles;
+    if ((threadIdx.x & 63) == 0) best_of[wave] = best, tiles_of_best[wave] = best_tiles, total_of_best[wave] = total;
+    __syncthreads();
+    best = best_of[0], best_tiles = tiles_of_best[0], total = total_of_best[0];
+#pragma unroll
+    for (int k = 1; k < kWaves; ++k)
+      if (best_of[k] < best) best = best_of[k], best_tiles = tiles_of_best[k], total = total_of_best[k];
+    piece_tiles = uniform(best_tiles), total = uniform(total);
   }
   // Row tiles of this lane's sequence whose walks have `least` key tiles or more: row tile t's last row is min(rows, 128 (t + 1)) - 1, of token len - n + row / gmax.
   __device__ __forceinline__ int tiles_from(const ChunkArgs& a, int least) const {
@@ -237,9 +247,10 @@ __device__ __forceinline__ void chunk_tiles(const ChunkArgs& a, const int wg, un
   TilePlan plan;
   plan.make<D>(a);
   if (wg == 0 && threadIdx.x == 0 && a.plan) a.plan[0] = plan.units, a.plan[1] = plan.total, a.plan[2] = plan.piece_tiles;  // for the kernel that joins
-  // runs of pieces on one XCD (workgroup b runs on XCD b % 8), turned by one with every eight of them, so that no XCD has all the long ones
+  // Runs of pieces on one XCD (workgroup b runs on XCD b % 8, and there on shader engine b / 8 % 4), turned by one with every eight of them and inside, so that no XCD and no
+  // engine has all the long ones (four sequences of 2048 tokens, 14 heads: without the second, compute units ended after 67 to 103 us)
   const int in_xcd = wg / 8, round = in_xcd / kRun;
-  const int id = uniform((round * 8 + ((wg - round) & 7)) * kRun + in_xcd % kRun);
+  const int id = uniform((round * 8 + ((wg - round) & 7)) * kRun + (in_xcd + round) % kRun);
   if (id >= plan.total) return;
   plan.find(a, id);
   const int seq = uniform(plan.seq), start = uniform(plan.seq_start), n = uniform(plan.seq_n), len = uniform(plan.seq_len), used = min(n, a.max_new);
@@ -251,14 +262,19 @@ __device__ __forceinline__ void chunk_tiles(const ChunkArgs& a, const int wg, un
   const int walk = (end + kTileKeys - 1) / kTileKeys;
   const int t_lo = int(int64_t(piece) * walk / n_pieces), t_hi = int(int64_t(piece + 1) * walk / n_pieces);
 
+  // the tile's row r is of token token0 + (rest0 + r) / G; the quotient of such small numbers by a product with the reciprocal
+  const int token0 = row0 / G, rest0 = row0 - token0 * G;
+  const float per_G = 1.0f / float(G);
+  auto token_of = [&](int r) { return token0 + int((float(rest0 + r) + 0.5f) * per_G); };
+
   // this wavefront's rows: their queries, and how many tokens they see
   const int w0 = row0 + wave * 16 * QB;
-  const int all_see = len - n + w0 / G + 1, most = w0 < rows ? len - n + (min(rows, w0 + 16 * QB) - 1) / G + 1 : 0;
+  const int all_see = len - n + token_of(wave * 16 * QB) + 1, most = w0 < rows ? len - n + token_of(min(rows - row0, wave * 16 * QB + 16 * QB) - 1) + 1 : 0;
   bf16x8 qf[QB][KS];
   int sees[QB];
 #pragma unroll
   for (int qb = 0; qb < QB; ++qb) {
-    const int rr = w0 + qb * 16 + lq, i = rr / G, j = j0 + rr - i * G;
+    const int rr = w0 + qb * 16 + lq, i = token_of(rr - row0), j = j0 + rr - i * G;
     sees[qb] = rr < rows ? len - n + i + 1 : 0;
 #pragma unroll
     for (int ks = 0; ks < KS; ++ks) qf[qb][ks] = bf16x8{};
@@ -533,7 +549,7 @@ __device__ __forceinline__ void chunk_tiles(const ChunkArgs& a, const int wg, un
 
 #pragma unroll
   for (int qb = 0; qb < QB; ++qb) {
-    const int rr = w0 + qb * 16 + lq, i = rr / G, j = j0 + rr - i * G;
+    const int rr = w0 + qb * 16 + lq, i = token_of(rr - row0), j = j0 + rr - i * G;
     const float l = over_rows(l_run[qb], added);
     if (n_pieces > 1) {
       float* const to = a.tile_parts + (int64_t(id) * kTileRows + (rr - row0)) * (D + kPartPad);
@@ -542,22 +558,37 @@ __device__ __forceinline__ void chunk_tiles(const ChunkArgs& a, const int wg, un
       if (lh == 0) to[D] = m_run[qb], to[D + 1] = l;
       continue;
     }
-    if (rr >= rows) continue;
+    // through the LDS, so that whole rows are stored: 16-byte chunk c of the wavefront's row r at slot c ^ swz(r)
     const float inv = l == 0.f ? 0.f : 1.0f / l;
-    uint16_t* const cp = a.C + int64_t(start + i) * a.ldc + int64_t(j) * D + lh * 4;
+    if (qb == 0) __syncthreads();  // the last tile has been read
+    int l16 = lane;
+    arrived(l16);
+    const int q16 = l16 & 15, h4 = l16 >> 4;
+    unsigned char* const to = lds + (wave * 32 + qb * 16 + q16) * D * 2 + (h4 & 1) * 8;
 #pragma unroll
     for (int db = 0; db < DB; ++db) {
       ntp_gemm::u16x4 o;
 #pragma unroll
       for (int r = 0; r < 4; ++r) o[r] = ntp_gemm::f32_to_bf16(acc[qb][db][r] * inv);
-      *reinterpret_cast<ntp_gemm::u16x4*>(cp + db * 16) = o;
+      *reinterpret_cast<ntp_gemm::u16x4*>(to + ((uint32_t(db * 2 + (h4 >> 1)) ^ tile_swz<D>(q16)) * 16u)) = o;
     }
-    if (lh == 0 && a.LSE) a.LSE[int64_t(j) * a.M + start + i] = ((l == 0.f ? 0.f : m_run[qb]) + log2f(l)) * 0.6931471805599453f;
+    if (rr < rows && lh == 0 && a.LSE) a.LSE[int64_t(j) * a.M + start + i] = ((l == 0.f ? 0.f : m_run[qb]) + log2f(l)) * 0.6931471805599453f;
+  }
+  if (n_pieces > 1) return;
+  constexpr int CH = D / 8, PER = 64 / CH;  // chunks of a row, rows of a store
+  int l64 = threadIdx.x & 63;
+  arrived(l64);  // (what follows from it is not worth registers through the walk)
+#pragma unroll
+  for (int k = 0; k < 32 / PER; ++k) {
+    const int r = k * PER + l64 / CH, c = l64 % CH, rr = w0 + r, i = token_of(rr - row0), j = j0 + rr - i * G;
+    if (rr < rows)
+      *reinterpret_cast<u32x4*>(a.C + int64_t(start + i) * a.ldc + int64_t(j) * D + c * 8) =
+          *reinterpret_cast<const u32x4*>(lds + (wave * 32 + r) * D * 2 + ((uint32_t(c) ^ tile_swz<D>(r & 15)) * 16u));
   }
 }
 
 // The pieces of row tiles put together: workgroup number wg of n takes every n-th of (unit, some of its rows).  D / 8 lanes a row, eight pieces' loads at a time; where there are
-// many pieces, all groups of lanes take one row's pieces in turn.
+// more pieces, several groups of lanes take a row's pieces in turn.
 template <int D>
 __device__ __forceinline__ void chunk_tiles_join(const ChunkArgs& a, const int wg, const int n_wgs) {
   constexpr int L = D / 8, G = kThreads / L, W = D + kPartPad, AT_ONCE = 8;  // lanes of a row, groups of lanes, floats of a partial row
@@ -568,27 +599,27 @@ __device__ __forceinline__ void chunk_tiles_join(const ChunkArgs& a, const int w
   if (plan.total == plan.units) return;
   plan.load(a, threadIdx.x & 63);
   const int grp = threadIdx.x / L, c = int(threadIdx.x) % L * 8;
-  const bool lengthy = plan.total >= 16 * plan.units;
-  const int per_unit = lengthy ? kTileRows : kTileRows / G;
+  int ways = 1;  // groups of lanes of a row
+  while (ways < G && plan.total > ways * AT_ONCE * plan.units) ways *= 2;
+  const int per_unit = kTileRows / (G / ways), way = grp % ways;
   for (int job = wg; job < plan.units * per_unit; job += n_wgs) {
     const int first = plan.find_unit(a, job / per_unit), np = plan.n_pieces;
     if (np == 1) continue;
     const Heads hd(a, a.kv_first + plan.head);
-    const int heads = hd.j1 - hd.j0, in_tile = lengthy ? job % per_unit : job % per_unit * G + grp, rr = plan.tile * kTileRows + in_tile;
+    const int heads = hd.j1 - hd.j0, in_tile = job % per_unit * (G / ways) + grp / ways, rr = plan.tile * kTileRows + in_tile;
     const bool there = rr < min(plan.seq_n, a.max_new) * heads;
     const float* const p0 = a.tile_parts + (int64_t(first) * kTileRows + in_tile) * W;
     const int64_t next = int64_t(plan.tiles_there) * kTileRows * W;
     float top = -INFINITY, sum = 0.f;
     f32x4 lo = {0.f, 0.f, 0.f, 0.f}, hi = lo;
-    const int by = lengthy ? G : 1;
-    for (int p = lengthy ? grp : 0; there && p < np; p += by * AT_ONCE) {
+    for (int p = way; there && p < np; p += ways * AT_ONCE) {
       float m[AT_ONCE], l[AT_ONCE];
       f32x4 x[AT_ONCE], y[AT_ONCE];
 #pragma unroll
       for (int k = 0; k < AT_ONCE; ++k) {
         m[k] = -INFINITY, l[k] = 0.f, x[k] = y[k] = f32x4{0.f, 0.f, 0.f, 0.f};
-        if (p + k * by < np) {
-          const float* const q = p0 + (p + k * by) * next;
+        if (p + k * ways < np) {
+          const float* const q = p0 + (p + k * ways) * next;
           m[k] = q[D], l[k] = q[D + 1], x[k] = *reinterpret_cast<const f32x4*>(q + c), y[k] = *reinterpret_cast<const f32x4*>(q + c + 4);
         }
       }
@@ -603,21 +634,21 @@ __device__ __forceinline__ void chunk_tiles_join(const ChunkArgs& a, const int w
         sum = fmaf(w, l[k], sum), lo += w * x[k], hi += w * y[k];
       }
     }
-    if (lengthy) {  // (the same in the whole workgroup)
+    if (ways > 1) {  // (the same in the whole workgroup)
       rows_of[grp][c / 8][0] = lo, rows_of[grp][c / 8][1] = hi;
       if (c == 0) sums_of[grp] = float2{top, sum};
       __syncthreads();
-      if (grp == 0) {
-        for (int k = 1; k < G; ++k) top = fmaxf(top, sums_of[k].x);
+      if (way == 0) {
+        for (int k = 1; k < ways; ++k) top = fmaxf(top, sums_of[grp + k].x);
         const float base = top == -INFINITY ? 0.f : top;
         sum = 0.f, lo = hi = f32x4{0.f, 0.f, 0.f, 0.f};
-        for (int k = 0; k < G; ++k) {
-          const float w = fast_exp2(sums_of[k].x - base);
-          sum = fmaf(w, sums_of[k].y, sum), lo += w * rows_of[k][c / 8][0], hi += w * rows_of[k][c / 8][1];
+        for (int k = 0; k < ways; ++k) {
+          const float w = fast_exp2(sums_of[grp + k].x - base);
+          sum = fmaf(w, sums_of[grp + k].y, sum), lo += w * rows_of[grp + k][c / 8][0], hi += w * rows_of[grp + k][c / 8][1];
         }
       }
       __syncthreads();
-      if (grp > 0) continue;
+      if (way > 0) continue;
     }
     if (!there) continue;
     const float inv = sum == 0.f ? 0.f : 1.0f / sum;

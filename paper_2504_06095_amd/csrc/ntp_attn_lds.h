@@ -153,6 +153,22 @@ __device__ __forceinline__ int sum_upto(int v) {
   return v;
 }
 
+// Over all lanes of a wavefront, for values of at least 0 (f: their sum or maximum), the same way.
+template <int CTRL, int ROWS, typename F>
+__device__ __forceinline__ float dpp_with(float v, F&& f) {
+  return f(v, __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, v), CTRL, ROWS, 0xf, false)));
+}
+template <typename F>
+__device__ __forceinline__ float over_wave(float v, F&& f) {
+  v = dpp_with<0x111, 0xf>(v, f);
+  v = dpp_with<0x112, 0xf>(v, f);
+  v = dpp_with<0x114, 0xf>(v, f);
+  v = dpp_with<0x118, 0xf>(v, f);
+  v = dpp_with<0x142, 0xa>(v, f);
+  v = dpp_with<0x143, 0xc>(v, f);
+  return __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, v), 63));
+}
+
 }  // namespace ntp_attn
 
 #endif  // NTP_ATTN_LDS_H_

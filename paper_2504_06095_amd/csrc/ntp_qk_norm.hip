@@ -21,7 +21,7 @@ using ntp::off16;
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
-constexpr int kThreads = 256, kMaxTokens = 8, kMaxPairs = 64;
+constexpr int kMaxThreads = 1024, kMaxTokens = 8, kMaxPairs = 64;
 
 __device__ __forceinline__ float bf_lo(uint32_t v) { return __builtin_bit_cast(float, v << 16); }
 __device__ __forceinline__ float bf_hi(uint32_t v) { return __builtin_bit_cast(float, v & 0xffff0000u); }
@@ -33,6 +33,12 @@ __device__ __forceinline__ void store_16(uint16_t* p, u32x4 v) { __builtin_nonte
 __device__ __forceinline__ void unpack(u32x4 v, float (&f)[8]) {
 #pragma unroll
   for (int k = 0; k < 4; ++k) f[2 * k] = bf_lo(v[k]), f[2 * k + 1] = bf_hi(v[k]);
+}
+// (what was unpacked from v before is unpacked again, and holds no registers in between)
+__device__ __forceinline__ void anew(u32x4& v) {
+#if defined(__HIP_DEVICE_COMPILE__)
+  asm volatile("" : "+v"(v));
+#endif
 }
 __device__ __forceinline__ u32x4 pack(const float (&f)[8]) { return u32x4{bf_pack(f[0], f[1]), bf_pack(f[2], f[3]), bf_pack(f[4], f[5]), bf_pack(f[6], f[7])}; }
 
@@ -67,8 +73,10 @@ __device__ __forceinline__ float over_same(float v) {
 }
 
 // cos and sin of the positions' angles of a workgroup's tokens, formed and reduced to less than half a turn in fp64
-__device__ __forceinline__ void angles(float2 (*cs)[kMaxPairs], const int32_t* positions, const double* inv_freq, int64_t row0, int rows, int half) {
-  for (int i = threadIdx.x; i < rows * half; i += kThreads) {
+__device__ __forceinline__ void angles(float2 (*cs)[kMaxPairs], const int32_t* positions, const double* inv_freq, int row0, int M, int tokens, int half) {
+  const int rows = min(tokens, M - row0);
+#pragma unroll 1
+  for (int i = threadIdx.x; i < rows * half; i += int(blockDim.x)) {
     const int t = i / half, p = i % half;
     double turns = double(positions[row0 + t]) * inv_freq[p] * 0.15915494309189533577;  // 1 / (2 pi)
     turns -= rint(turns);
@@ -98,7 +106,31 @@ __device__ __forceinline__ void turn(float (&x)[8], float (&y)[8], const float2*
   }
 }
 
+// How a workgroup takes its tokens: `tokens` at a time, kHead = head_dim / 16 lanes a head, so that a thread has one head of one of them and its weights in registers; rows of more
+// heads than a workgroup has room for in several passes.  The next tokens' elements are on their way while these are worked on.
+struct Deal {
+  int32_t heads, tokens, threads, wgs;
+};
+template <int D>
+struct Place {
+  static constexpr int kHead = D / 16;
+  int j, token, head, stride;  // number in the head, token of the workgroup's, head, heads of a pass
+  int c0, c1;                  // a rotated head's elements: pairs number 8 j .. 8 j + 7, or two chunks behind the rotated part
+  bool turned;
+  __device__ __forceinline__ Place(const Deal& d, int rotary_dim, int interleaved) {
+    j = int(threadIdx.x) & (kHead - 1);
+    stride = min(d.heads, d.threads / kHead);
+    token = (int(threadIdx.x) / kHead) / stride;
+    head = (int(threadIdx.x) / kHead) % stride;
+    const int rot = rotary_dim / 16;
+    turned = j < rot;
+    c0 = (turned ? (interleaved ? 2 * j : j) : 2 * j) * 8;
+    c1 = (turned ? (interleaved ? 2 * j + 1 : j + rot) : 2 * j + 1) * 8;
+  }
+};
+
 struct AppendArgs {
+  Deal deal;
   const uint16_t *QKV, *q_gamma, *k_gamma;
   uint16_t *Qout, *Kout;
   unsigned char *K, *V;  // pages
@@ -107,7 +139,7 @@ struct AppendArgs {
   const int64_t* slots;
   const double* inv_freq;
   int64_t M, ldqkv, ldq, ldk, page_stride, exp_stride, n_slots;
-  int32_t q_cnt, kv_cnt, rotary_dim, interleaved, page_size, page_log2, tokens;
+  int32_t q_cnt, kv_cnt, rotary_dim, interleaved, page_size, page_log2;
   float eps;
 };
 
@@ -129,226 +161,224 @@ __device__ __forceinline__ u32x2 to_e4m3(const float (&f)[8], float down) {
 }
 
 template <int D, bool FP8>
-__global__ __launch_bounds__(kThreads) void qk_norm_append_kernel(const AppendArgs a) {
-  constexpr int kHead = D / 16, kLog2 = D == 128 ? 3 : 2;  // lanes of a head
-  __shared__ float2 cs[kMaxTokens][kMaxPairs];
-  __shared__ int64_t slot_of[kMaxTokens];
-  const int64_t row0 = int64_t(blockIdx.x) * a.tokens;
-  const int rows = int(std::min<int64_t>(a.tokens, a.M - row0));
-  const int j = int(threadIdx.x) & (kHead - 1), rot = a.rotary_dim / 16;
-  const bool turned = j < rot;
-  // this lane's 8 + 8 elements of a query or key head: pairs number 8 j .. 8 j + 7, or two chunks behind the rotated part; of a value head
-  const int c0 = (turned ? (a.interleaved ? 2 * j : j) : 2 * j) * 8, c1 = (turned ? (a.interleaved ? 2 * j + 1 : j + rot) : 2 * j + 1) * 8;
-  const int v0 = j * 8, v1 = (j + kHead) * 8;
-  const int heads = a.q_cnt + 2 * a.kv_cnt, per_row = heads << kLog2;
-  int t = int(threadIdx.x) / per_row, at = int(threadIdx.x) % per_row;
-  const int dt = kThreads / per_row, dat = kThreads % per_row;
-  constexpr int kItems = 2;  // of a thread, whose loads go out together; the first ones before the angles are formed
-  int tn[kItems], hn[kItems];
-  u32x4 xw[kItems], yw[kItems];
-  auto fetch = [&] {
-#pragma unroll
-    for (int n = 0; n < kItems; ++n) {
-      tn[n] = t, hn[n] = at >> kLog2;
-      if (t < rows) {
-        const bool v = hn[n] >= a.q_cnt + a.kv_cnt;
-        const uint16_t* const src = a.QKV + (row0 + t) * a.ldqkv + int64_t(hn[n]) * D;
-        xw[n] = load_16(src + (v ? v0 : c0));
-        yw[n] = load_16(src + (v ? v1 : c1));
+__global__ __launch_bounds__(kMaxThreads) void qk_norm_append_kernel(const AppendArgs a) {
+  __shared__ float2 cs[2][kMaxTokens][kMaxPairs];
+  const Place<D> at(a.deal, a.rotary_dim, a.interleaved);
+  const int M = int(a.M), step = int(gridDim.x) * a.deal.tokens, half = a.rotary_dim / 2;
+  for (int head = at.head; head - at.head < a.deal.heads; head += at.stride) {  // (one pass but for very many heads)
+    const bool is_q = head < a.q_cnt, is_v = head >= a.q_cnt + a.kv_cnt, mine = head < a.deal.heads && at.token < a.deal.tokens;
+    const uint16_t* const gamma = is_q ? a.q_gamma : is_v ? nullptr : a.k_gamma;
+    const bool turned = at.turned && !is_v;
+    const int c0 = is_v ? at.j * 8 : at.c0, c1 = is_v ? (at.j + at.kHead) * 8 : at.c1, g = is_q ? head : head - a.q_cnt - (is_v ? a.kv_cnt : 0);
+    u32x4 gw0{}, gw1{};
+    if (gamma && mine) gw0 = load_16(gamma + c0), gw1 = load_16(gamma + c1);
+    u32x4 xw{}, yw{};
+    int64_t slot = -1;
+    int row0 = int(blockIdx.x) * a.deal.tokens;
+    // (not formed from the row each time: 64-bit products)
+    const int64_t first = row0 + at.token, ldout = is_q ? a.ldq : a.ldk;
+    const uint16_t* src = a.QKV + first * a.ldqkv + int64_t(head) * D;
+    uint16_t* const out0 = is_q ? a.Qout : is_v ? nullptr : a.Kout;
+    uint16_t* out = out0 + first * ldout + int64_t(g) * D;
+    auto fetch = [&] {
+      if (mine && row0 + at.token < M) {
+        xw = load_16(src + c0);
+        yw = load_16(src + c1);
+        if (!is_q && a.slots) slot = a.slots[row0 + at.token];
       }
-      t += dt;
-      at += dat;
-      if (at >= per_row) at -= per_row, ++t;
-    }
-  };
-  fetch();
-  if (int(threadIdx.x) < rows) slot_of[threadIdx.x] = a.slots ? a.slots[row0 + threadIdx.x] : -1;
-  u32x4 gq0{}, gq1{}, gk0{}, gk1{};
-  if (a.q_gamma) gq0 = load_16(a.q_gamma + c0), gq1 = load_16(a.q_gamma + c1);
-  if (a.k_gamma) gk0 = load_16(a.k_gamma + c0), gk1 = load_16(a.k_gamma + c1);
-  angles(cs, a.positions, a.inv_freq, row0, rows, a.rotary_dim / 2);
-  __syncthreads();
-
-  while (tn[0] < rows) {
-#pragma unroll
-    for (int n = 0; n < kItems; ++n) {
-      if (tn[n] >= rows) continue;  // (all lanes of a head together)
-      const int head = hn[n];
-      const int64_t row = row0 + tn[n];
-      const bool is_q = head < a.q_cnt, is_v = head >= a.q_cnt + a.kv_cnt;
-      const bool norm = is_q ? a.q_gamma != nullptr : !is_v && a.k_gamma != nullptr;
-      float x[8], y[8];
-      unpack(xw[n], x);
-      unpack(yw[n], y);
-      if (norm) {
-        float ss = 0.f;
-#pragma unroll
-        for (int k = 0; k < 8; ++k) ss = fmaf(x[k], x[k], fmaf(y[k], y[k], ss));
-        ss = over_head<D>(ss, add);
-        const float rstd = rsqrtf(ss * (1.0f / D) + a.eps);
-        float g[8];
-        unpack(is_q ? gq0 : gk0, g);
-#pragma unroll
-        for (int k = 0; k < 8; ++k) x[k] = x[k] * rstd * g[k];
-        unpack(is_q ? gq1 : gk1, g);
-#pragma unroll
-        for (int k = 0; k < 8; ++k) y[k] = y[k] * rstd * g[k];
-      }
-      if (turned && !is_v) turn(x, y, &cs[tn[n]][8 * j], a.interleaved, 1.0f);
-      const bool changed = norm || (turned && !is_v);  // (what is copied is copied bit for bit)
-      const u32x4 xb = changed ? pack(x) : xw[n], yb = changed ? pack(y) : yw[n];
-      const int g = is_v ? head - a.q_cnt - a.kv_cnt : head - a.q_cnt;
-      uint16_t* const out = is_q ? (a.Qout ? a.Qout + row * a.ldq + int64_t(head) * D : nullptr) : !is_v && a.Kout ? a.Kout + row * a.ldk + int64_t(g) * D : nullptr;
-      if (out) {
-        store_16(out + c0, xb);
-        store_16(out + c1, yb);
-      }
-      const int64_t slot = slot_of[tn[n]];
-      if (is_q || slot < 0 || slot >= a.n_slots) continue;
-      const int64_t page = slot >> a.page_log2, in_head = int64_t(g) * a.page_size + (slot & (a.page_size - 1)), place = page * a.page_stride + in_head * D;
-      const int p0 = is_v ? v0 : c0, p1 = is_v ? v1 : c1;
-      if constexpr (!FP8) {
-        uint16_t* const to = reinterpret_cast<uint16_t*>(is_v ? a.V : a.K) + place;
-        store_16(to + p0, xb);
-        store_16(to + p1, yb);
-      } else {
-        float top = 0.f;
-#pragma unroll
-        for (int k = 0; k < 8; ++k) {
-          const float p = fabsf(x[k]), q = fabsf(y[k]);
-          top = fmaxf(top, fmaxf(p < INFINITY ? p : 0.f, q < INFINITY ? q : 0.f));
-        }
-        top = over_head<D>(top, [](float p, float q) { return fmaxf(p, q); });
-        // 448 = 1.75 * 2^8: one more than the exponent of top / 2^8 where its mantissa is above 1.75
-        int code = int((__builtin_bit_cast(uint32_t, top) + 0x1fffffu) >> 23) - 8;
-        code = top == 0.f ? 127 : std::max(code, 16);
-        const float down = __builtin_bit_cast(float, uint32_t(254 - code) << 23);
-        unsigned char* const to = (is_v ? a.V : a.K) + place;
-        *reinterpret_cast<u32x2*>(to + p0) = to_e4m3(x, down);
-        *reinterpret_cast<u32x2*>(to + p1) = to_e4m3(y, down);
-        if (j == 0) (is_v ? a.V_exp : a.K_exp)[page * a.exp_stride + in_head] = uint8_t(code);
-      }
-    }
+      src += int64_t(step) * a.ldqkv;
+    };
     fetch();
+    __syncthreads();  // (the pass before has used the angles)
+    if (row0 < M) angles(cs[0], a.positions, a.inv_freq, row0, M, a.deal.tokens, half);
+    for (int buf = 0; row0 < M; buf ^= 1) {
+      __syncthreads();
+      const bool there = mine && row0 + at.token < M;
+      const int64_t to_slot = slot;
+      u32x4 xr = xw, yr = yw;
+      row0 += step;
+      fetch();
+      if (there) {  // (all lanes of a head together)
+        float x[8], y[8];
+        unpack(xr, x);
+        unpack(yr, y);
+        if (gamma) {
+          float ss = 0.f;
+#pragma unroll
+          for (int k = 0; k < 8; ++k) ss = fmaf(x[k], x[k], fmaf(y[k], y[k], ss));
+          ss = over_head<D>(ss, add);
+          const float rstd = rsqrtf(ss * (1.0f / D) + a.eps);
+          float w[8];
+          unpack(gw0, w);
+#pragma unroll
+          for (int k = 0; k < 8; ++k) x[k] = x[k] * rstd * w[k];
+          unpack(gw1, w);
+#pragma unroll
+          for (int k = 0; k < 8; ++k) y[k] = y[k] * rstd * w[k];
+        }
+        if (turned) turn(x, y, &cs[buf][at.token][8 * at.j], a.interleaved, 1.0f);
+        const bool changed = gamma || turned;  // (what is copied is copied bit for bit)
+        const u32x4 xb = changed ? pack(x) : xr, yb = changed ? pack(y) : yr;
+        if (out0) {
+          store_16(out + c0, xb);
+          store_16(out + c1, yb);
+        }
+        if (!is_q && to_slot >= 0 && to_slot < a.n_slots) {
+          const int64_t page = to_slot >> a.page_log2, in_head = int64_t(g) * a.page_size + (to_slot & (a.page_size - 1)), place = page * a.page_stride + in_head * D;
+          if constexpr (!FP8) {
+            uint16_t* const to = reinterpret_cast<uint16_t*>(is_v ? a.V : a.K) + place;
+            store_16(to + c0, xb);
+            store_16(to + c1, yb);
+          } else {
+            float top = 0.f;
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+              const float p = fabsf(x[k]), q = fabsf(y[k]);
+              top = fmaxf(top, fmaxf(p < INFINITY ? p : 0.f, q < INFINITY ? q : 0.f));
+            }
+            top = over_head<D>(top, [](float p, float q) { return fmaxf(p, q); });
+            // 448 = 1.75 * 2^8: one more than the exponent of top / 2^8 where its mantissa is above 1.75
+            int code = int((__builtin_bit_cast(uint32_t, top) + 0x1fffffu) >> 23) - 8;
+            code = top == 0.f ? 127 : max(code, 16);
+            const float down = __builtin_bit_cast(float, uint32_t(254 - code) << 23);
+            unsigned char* const to = (is_v ? a.V : a.K) + place;
+            *reinterpret_cast<u32x2*>(to + c0) = to_e4m3(x, down);
+            *reinterpret_cast<u32x2*>(to + c1) = to_e4m3(y, down);
+            if (at.j == 0) (is_v ? a.V_exp : a.K_exp)[page * a.exp_stride + in_head] = uint8_t(code);
+          }
+        }
+      }
+      out += int64_t(step) * ldout;
+      if (row0 < M) angles(cs[buf ^ 1], a.positions, a.inv_freq, row0, M, a.deal.tokens, half);
+    }
   }
 }
 
 // ---- gradient ---------------------------------------------------------------------------------------
-// The query heads' part and the key heads' have workgroups of their own (fewer registers than sums of both gammas in one: 4 wavefronts a SIMD more).
-struct BwdSide {
-  const uint16_t *x, *up, *gamma;  // the first head's columns of QKV, its gradient, and the weights of its norm (NULL: none)
-  uint16_t* out;                   // the first head's columns of dQKV
-  float* d_gamma;                  // where parts is NULL: one workgroup of the side writes it itself; NULL: not wanted
-  int64_t ldup;
-  int32_t heads, tokens, wgs, wanted;  // heads; tokens of a workgroup at a time; workgroups; whether the gamma's gradient is formed
-};
 struct BwdArgs {
-  BwdSide q, k;
-  float* parts;  // [workgroup][D] partial sums of the gammas' gradients
+  Deal deal;
+  const uint16_t *QKV, *dQ, *dK, *q_gamma, *k_gamma;
+  uint16_t* dQKV;            // NULL: the gammas' gradients alone
+  float* parts;              // [workgroup][2][D] partial sums of the gammas' gradients
+  float *d_q, *d_k;          // where parts is NULL: one workgroup writes what is wanted of them itself
   const int32_t* positions;
   const double* inv_freq;
-  int64_t M, ldx, ldout;
-  int32_t rotary_dim, interleaved, accumulate, store;
+  int64_t M, ldqkv, lddq, lddk, lddqkv;
+  int32_t q_cnt, rotary_dim, interleaved, accumulate;
   float eps;
 };
 
 template <int D>
-__global__ __launch_bounds__(kThreads) void qk_norm_bwd_kernel(const BwdArgs a) {
-  constexpr int kHead = D / 16, kLog2 = D == 128 ? 3 : 2;
-  __shared__ float2 cs[kMaxTokens][kMaxPairs];
-  __shared__ float sums[kThreads / 64][D];
-  const bool is_q = int(blockIdx.x) < a.q.wgs;
-  const BwdSide& s = is_q ? a.q : a.k;
-  const int wg = int(blockIdx.x) - (is_q ? 0 : a.q.wgs);
-  const int j = int(threadIdx.x) & (kHead - 1), rot = a.rotary_dim / 16;
-  const bool turned = j < rot;
-  const int c0 = (turned ? (a.interleaved ? 2 * j : j) : 2 * j) * 8, c1 = (turned ? (a.interleaved ? 2 * j + 1 : j + rot) : 2 * j + 1) * 8;
-  u32x4 gw0{}, gw1{};
-  if (s.gamma) gw0 = load_16(s.gamma + c0), gw1 = load_16(s.gamma + c1);
-  float dg[16] = {};
-  const int per_row = s.heads << kLog2;
-  const int dt = kThreads / per_row, dat = kThreads % per_row;
-  for (int64_t row0 = int64_t(wg) * s.tokens; row0 < a.M; row0 += int64_t(s.wgs) * s.tokens) {
-    const int rows = int(std::min<int64_t>(s.tokens, a.M - row0));
-    int t = int(threadIdx.x) / per_row, at = int(threadIdx.x) % per_row;
-    u32x4 xw[4];
+__global__ __launch_bounds__(kMaxThreads) void qk_norm_bwd_kernel(const BwdArgs a) {
+  __shared__ float2 cs[2][kMaxTokens][kMaxPairs];
+  __shared__ float sums[kMaxThreads / 64][2][D];
+  const Place<D> at(a.deal, a.rotary_dim, a.interleaved);
+  const int M = int(a.M), step = int(gridDim.x) * a.deal.tokens;
+  const int half = a.rotary_dim / 2, wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+  const bool wanted = a.parts || a.d_q || a.d_k;
+  if (wanted)
+    for (int i = lane; i < 2 * D; i += 64) sums[wave][i / D][i % D] = 0.f;
+  for (int head = at.head; head - at.head < a.deal.heads; head += at.stride) {  // (one pass but for very many heads)
+    const bool is_q = head < a.q_cnt, mine = head < a.deal.heads && at.token < a.deal.tokens;
+    const uint16_t* const gamma = is_q ? a.q_gamma : a.k_gamma;
+    u32x4 gw0{}, gw1{};
+    if (gamma && mine) gw0 = load_16(gamma + at.c0), gw1 = load_16(gamma + at.c1);
+    float dg[16] = {};
+    u32x4 xw{}, yw{}, uw{}, ww{};
+    int row0 = int(blockIdx.x) * a.deal.tokens;
+    // (not formed from the row each time: three 64-bit products)
+    const int64_t first = row0 + at.token, up_step = int64_t(step) * (is_q ? a.lddq : a.lddk);
+    const uint16_t* src = a.QKV + first * a.ldqkv + int64_t(head) * D;
+    const uint16_t* up = is_q ? a.dQ + first * a.lddq + int64_t(head) * D : a.dK + first * a.lddk + int64_t(head - a.q_cnt) * D;
+    uint16_t* out = a.dQKV + first * a.lddqkv + int64_t(head) * D;
     auto fetch = [&] {
-      if (t >= rows) return;
-      const int64_t row = row0 + t, col = int64_t(at >> kLog2) * D;
-      const uint16_t *const src = s.x + row * a.ldx + col, *const up = s.up + row * s.ldup + col;
-      xw[0] = load_16(src + c0), xw[1] = load_16(src + c1), xw[2] = load_16(up + c0), xw[3] = load_16(up + c1);
+      if (mine && row0 + at.token < M) xw = load_16(src + at.c0), yw = load_16(src + at.c1), uw = load_16(up + at.c0), ww = load_16(up + at.c1);
+      src += int64_t(step) * a.ldqkv, up += up_step;
     };
-    fetch();  // (on its way while the angles are formed)
-    __syncthreads();  // the angles of the rows before have been used
-    angles(cs, a.positions, a.inv_freq, row0, rows, a.rotary_dim / 2);
-    __syncthreads();
-    while (t < rows) {
+    fetch();
+    __syncthreads();  // (the pass before has used the angles)
+    if (row0 < M) angles(cs[0], a.positions, a.inv_freq, row0, M, a.deal.tokens, half);
+    for (int buf = 0; row0 < M; buf ^= 1) {
+      __syncthreads();
+      const bool there = mine && row0 + at.token < M;
+      u32x4 xr = xw, yr = yw;
       float x[8], y[8], u[8], w[8];
-      unpack(xw[0], x);
-      unpack(xw[1], y);
-      unpack(xw[2], u);
-      unpack(xw[3], w);
-      uint16_t* const out = s.out + (row0 + t) * a.ldout + int64_t(at >> kLog2) * D;
-      const float2* const angle = &cs[t][8 * j];
-      t += dt;
-      at += dat;
-      if (at >= per_row) at -= per_row, ++t;
+      unpack(uw, u);
+      unpack(ww, w);
+      row0 += step;
       fetch();
-      if (turned) turn(u, w, angle, a.interleaved, -1.0f);
-      if (s.gamma) {
-        float g0[8], g1[8], ss = 0.f, dot = 0.f;
-        unpack(gw0, g0);
-        unpack(gw1, g1);
+      if (there) {
+        if (at.turned) turn(u, w, &cs[buf][at.token][8 * at.j], a.interleaved, -1.0f);
+        if (gamma) {
+          float g0[8], g1[8], ss = 0.f, dot = 0.f;
+          unpack(xr, x);
+          unpack(yr, y);
+          unpack(gw0, g0);
+          unpack(gw1, g1);
 #pragma unroll
-        for (int k = 0; k < 8; ++k) {
-          ss = fmaf(x[k], x[k], fmaf(y[k], y[k], ss));
-          dot = fmaf(u[k] * g0[k], x[k], fmaf(w[k] * g1[k], y[k], dot));
+          for (int k = 0; k < 8; ++k) {
+            ss = fmaf(x[k], x[k], fmaf(y[k], y[k], ss));
+            dot = fmaf(u[k] * g0[k], x[k], fmaf(w[k] * g1[k], y[k], dot));
+          }
+          ss = over_head<D>(ss, add);
+          dot = over_head<D>(dot, add);
+          const float rstd = rsqrtf(ss * (1.0f / D) + a.eps), mean = dot * rstd * (1.0f / D);
+          anew(xr), anew(yr), anew(gw0), anew(gw1);
+          unpack(xr, x);
+          unpack(yr, y);
+          unpack(gw0, g0);
+          unpack(gw1, g1);
+#pragma unroll
+          for (int k = 0; k < 8; ++k) {
+            const float xh = x[k] * rstd, yh = y[k] * rstd;
+            dg[k] = fmaf(u[k], xh, dg[k]), dg[8 + k] = fmaf(w[k], yh, dg[8 + k]);
+            u[k] = (u[k] * g0[k] - xh * mean) * rstd;
+            w[k] = (w[k] * g1[k] - yh * mean) * rstd;
+          }
         }
-        ss = over_head<D>(ss, add);
-        dot = over_head<D>(dot, add);
-        const float rstd = rsqrtf(ss * (1.0f / D) + a.eps), mean = dot * rstd * (1.0f / D);
-#pragma unroll
-        for (int k = 0; k < 8; ++k) {
-          const float xh = x[k] * rstd, yh = y[k] * rstd;
-          dg[k] = fmaf(u[k], xh, dg[k]), dg[8 + k] = fmaf(w[k], yh, dg[8 + k]);
-          u[k] = (u[k] * g0[k] - xh * mean) * rstd;
-          w[k] = (w[k] * g1[k] - yh * mean) * rstd;
+        if (a.dQKV) {
+          store_16(out + at.c0, pack(u));
+          store_16(out + at.c1, pack(w));
         }
       }
-      if (a.store) {
-        store_16(out + c0, pack(u));
-        store_16(out + c1, pack(w));
+      out += int64_t(step) * a.lddqkv;
+      if (row0 < M) angles(cs[buf ^ 1], a.positions, a.inv_freq, row0, M, a.deal.tokens, half);
+    }
+    if (wanted) {  // heads of both kinds may stand in a wavefront: one kind after the other
+#pragma unroll
+      for (int kind = 0; kind < 2; ++kind) {
+        if (!__any(mine && is_q == (kind == 0))) continue;
+#pragma unroll
+        for (int k = 0; k < 16; ++k) {
+          const float v = over_same<D>(mine && is_q == (kind == 0) ? dg[k] : 0.f);
+          if (lane < at.kHead) sums[wave][kind][(k < 8 ? at.c0 : at.c1 - 8) + k] += v;
+        }
       }
     }
   }
-  if (!s.wanted) return;
-  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
-#pragma unroll
-  for (int k = 0; k < 16; ++k) dg[k] = over_same<D>(dg[k]);
-  if (lane < kHead) {
-#pragma unroll
-    for (int k = 0; k < 8; ++k) sums[wave][c0 + k] = dg[k], sums[wave][c1 + k] = dg[8 + k];
-  }
+  if (!wanted) return;
   __syncthreads();
-  const int c = threadIdx.x;
-  if (c >= D) return;
-  const float v = (sums[0][c] + sums[1][c]) + (sums[2][c] + sums[3][c]);
-  if (a.parts) a.parts[int64_t(blockIdx.x) * D + c] = v;
-  else s.d_gamma[c] = a.accumulate ? s.d_gamma[c] + v : v;
+  const int waves = int(blockDim.x) >> 6;
+  for (int i = threadIdx.x; i < 2 * D; i += int(blockDim.x)) {
+    const int kind = i / D, c = i % D;
+    float v = 0.f;
+    for (int k = 0; k < waves; ++k) v += sums[k][kind][c];
+    float* const out = kind ? a.d_k : a.d_q;
+    if (a.parts) a.parts[int64_t(blockIdx.x) * 2 * D + i] = v;
+    else if (out) out[c] = a.accumulate ? out[c] + v : v;
+  }
 }
 
-// Adds up the partial sums of one gamma's gradient (blockIdx.y; the first n_q are the query heads'), 16 columns a workgroup, 64 of them side by side.
-constexpr int kSumThreads = 1024;
+// Adds up n partial sums of one gamma's gradient (blockIdx.y), 16 columns a workgroup, 64 of them side by side.
 template <int D>
-__global__ __launch_bounds__(kSumThreads) void qk_norm_sum_kernel(const float* parts, int n_q, int n_k, float* d_q, float* d_k, int accumulate) {
+__global__ __launch_bounds__(kMaxThreads) void qk_norm_sum_kernel(const float* parts, int n, float* d_q, float* d_k, int accumulate) {
   __shared__ float rows[64][17];
   float* const out = blockIdx.y == 0 ? d_q : d_k;
   if (!out) return;
-  const int n = blockIdx.y == 0 ? n_q : n_k, c = threadIdx.x & 15, r = threadIdx.x >> 4, col = int(blockIdx.x) * 16 + c;
-  parts += blockIdx.y == 0 ? 0 : int64_t(n_q) * D;
+  const int c = threadIdx.x & 15, r = threadIdx.x >> 4, col = int(blockIdx.x) * 16 + c;
   float sum = 0.f;
 #pragma unroll 8
-  for (int i = r; i < n; i += 64) sum += parts[int64_t(i) * D + col];
+  for (int i = r; i < n; i += 64) sum += parts[int64_t(i) * 2 * D + blockIdx.y * D + col];
   rows[r][c] = sum;
   __syncthreads();
   for (int half = 32; half > 0; half /= 2) {
@@ -363,7 +393,7 @@ int check_shape(const ntp_kv_append_shape_t* s) {
   if (s->head_dim != 64 && s->head_dim != 128) return NTP_ERR_UNSUPPORTED;
   if (s->rotary_dim > s->head_dim || s->rotary_dim % 16) return NTP_ERR_INVALID_ARG;
   const int64_t w = (s->q_cnt + 2 * int64_t(s->kv_cnt)) * s->head_dim;
-  return s->M > 0x7fffffffll || w > 0x7fffffffll / 16 ? NTP_ERR_UNSUPPORTED : NTP_OK;
+  return s->M > 0x7fffffffll - (1 << 20) || w > 0x7fffffffll / 16 ? NTP_ERR_UNSUPPORTED : NTP_OK;
 }
 int check_norm(const ntp_qk_norm_t* n) {
   if (!n || (!n->q_gamma && !n->k_gamma)) return NTP_OK;
@@ -371,23 +401,21 @@ int check_norm(const ntp_qk_norm_t* n) {
   return off16(n->q_gamma) || off16(n->k_gamma) ? NTP_ERR_ALIGNMENT : NTP_OK;
 }
 bool off(const void* p, int bytes) { return (reinterpret_cast<uintptr_t>(p) & (bytes - 1)) != 0; }
-// Tokens of a workgroup: at least an item for every thread where rows are short (as ntp_kv_append.hip), as long as there are `wgs` workgroups.
-int32_t tokens_of(int64_t M, int64_t items_per_row, int64_t wgs) {
-  const int64_t most = std::max<int64_t>(1, std::min<int64_t>(kMaxTokens, 384 / std::max<int64_t>(items_per_row, 1)));
-  return int32_t(std::max<int64_t>(1, std::min(most, M / wgs)));
-}
-
-// Workgroups of both sides of the gradient, in proportion to their heads: up to four on every compute unit.
-void bwd_sides(const ntp_handle* h, const ntp_kv_append_shape_t* s, BwdSide* q, BwdSide* k) {
-  const int64_t all = 4 * int64_t(h->compute_units), heads = std::max(s->q_cnt + s->kv_cnt, 1);
-  auto side = [&](BwdSide* d, int32_t n) {
-    const int64_t room = std::max<int64_t>(1, all * n / heads);
-    d->heads = n;
-    d->tokens = tokens_of(s->M, int64_t(n) * (s->head_dim / 16), std::max<int64_t>(1, room / 2));
-    d->wgs = n == 0 ? 0 : int32_t(std::min<int64_t>((s->M + d->tokens - 1) / d->tokens, room));
-  };
-  side(q, s->q_cnt);
-  side(k, s->kv_cnt);
+constexpr int kAppendRoom = 2048, kBwdRoom = 1024;  // threads of a compute unit's workgroups
+// Tokens at a time: as many as leave few of the workgroup's threads without a head, and fill half of the largest workgroup, as long as there are two workgroups for every compute
+// unit; as many workgroups as the compute units have room for.
+Deal deal_of(const ntp_handle* h, int64_t M, int32_t heads, int32_t head_dim, int32_t room) {
+  Deal d{heads, 1, kMaxThreads, 0};
+  const int64_t lanes = int64_t(heads) * (head_dim / 16);
+  if (lanes == 0 || M == 0) return d;
+  double best = 0;
+  for (int32_t t = 1; t <= kMaxTokens && (t == 1 || (lanes * t <= kMaxThreads && M / t >= 2 * int64_t(h->compute_units))); ++t) {
+    const int64_t threads = std::min<int64_t>(kMaxThreads, (lanes * t + 63) / 64 * 64);
+    const double used = lanes > kMaxThreads ? 1.0 : double(lanes * t) / double(threads);
+    if (used > best + 0.02 || (used > best - 0.02 && threads <= kMaxThreads / 2)) best = std::max(best, used), d.tokens = t, d.threads = int32_t(threads);
+  }
+  d.wgs = int32_t(std::min<int64_t>((M + d.tokens - 1) / d.tokens, int64_t(h->compute_units) * std::max(1, room / d.threads)));
+  return d;
 }
 
 }  // namespace
@@ -395,9 +423,8 @@ void bwd_sides(const ntp_handle* h, const ntp_kv_append_shape_t* s, BwdSide* q, 
 int ntp::qk_norm_workspace_wish(const ntp_handle* h, const ntp_kv_append_shape_t* s, int64_t* bytes) {
   const int st = check_shape(s);
   if (st != NTP_OK) return NTP_ERR_INVALID_ARG;
-  BwdSide q{}, k{};
-  bwd_sides(h, s, &q, &k);
-  *bytes = s->M == 0 || q.wgs + k.wgs <= 2 ? 0 : int64_t(q.wgs + k.wgs) * s->head_dim * 4;
+  const Deal d = deal_of(h, s->M, s->q_cnt + s->kv_cnt, s->head_dim, kBwdRoom);
+  *bytes = d.wgs <= 1 ? 0 : int64_t(d.wgs) * 2 * s->head_dim * 4;
   return NTP_OK;
 }
 
@@ -420,8 +447,7 @@ extern "C" int ntp_qk_norm_append_shard(ntp_handle_t* h, const ntp_kv_append_sha
       (ntp::rows_overlap(Kout, ldk, wk, QKV, ldqkv, w, s->M) && (Kout != in + wq || (ldk != ldqkv && !one))) || ntp::rows_overlap(Qout, ldq, wq, Kout, ldk, wk, s->M))
     return NTP_ERR_INVALID_ARG;
   AppendArgs a{};
-  a.tokens = tokens_of(s->M, w / 16, 2 * int64_t(h->compute_units));
-  if ((s->M + a.tokens - 1) / a.tokens * kThreads > 0xffffffffll) return NTP_ERR_UNSUPPORTED;  // a launch counts its threads in 32 bits
+  a.deal = deal_of(h, s->M, int32_t(w / d), s->head_dim, kAppendRoom);
   if (h->device < 0) return NTP_ERR_NO_DEVICE;
   a.QKV = in, a.Qout = static_cast<uint16_t*>(Qout), a.Kout = static_cast<uint16_t*>(Kout);
   a.positions = positions, a.inv_freq = inv_freq;
@@ -439,11 +465,11 @@ extern "C" int ntp_qk_norm_append_shard(ntp_handle_t* h, const ntp_kv_append_sha
   if (ntp::timing_on(h))
     ntp::timing_begin(h, stream, fp8 ? "qk_norm_append8" : "qk_norm_append", 0.0,
                       2.0 * double(s->M) * double(w + (Qout ? wq : 0) + (Kout ? wk : 0)) + double(s->M) * double(pages ? 2 * wk : 0) * (fp8 ? 1 : 2));
-  const dim3 grid{uint32_t((s->M + a.tokens - 1) / a.tokens)};
-  if (d == 128 && fp8) hipLaunchKernelGGL((qk_norm_append_kernel<128, true>), grid, dim3(kThreads), 0, hs, a);
-  else if (d == 128) hipLaunchKernelGGL((qk_norm_append_kernel<128, false>), grid, dim3(kThreads), 0, hs, a);
-  else if (fp8) hipLaunchKernelGGL((qk_norm_append_kernel<64, true>), grid, dim3(kThreads), 0, hs, a);
-  else hipLaunchKernelGGL((qk_norm_append_kernel<64, false>), grid, dim3(kThreads), 0, hs, a);
+  const dim3 grid{uint32_t(a.deal.wgs)}, block{uint32_t(a.deal.threads)};
+  if (d == 128 && fp8) hipLaunchKernelGGL((qk_norm_append_kernel<128, true>), grid, block, 0, hs, a);
+  else if (d == 128) hipLaunchKernelGGL((qk_norm_append_kernel<128, false>), grid, block, 0, hs, a);
+  else if (fp8) hipLaunchKernelGGL((qk_norm_append_kernel<64, true>), grid, block, 0, hs, a);
+  else hipLaunchKernelGGL((qk_norm_append_kernel<64, false>), grid, block, 0, hs, a);
   const bool ok = hipGetLastError() == hipSuccess;
   ntp::timing_end(h, stream);
   return ok ? NTP_OK : NTP_ERR_LAUNCH;
@@ -476,48 +502,41 @@ extern "C" int ntp_qk_norm_shard_bwd(ntp_handle_t* h, const ntp_kv_append_shape_
   }
   if (h->device < 0) return NTP_ERR_NO_DEVICE;
   BwdArgs a{};
-  bwd_sides(h, s, &a.q, &a.k);
-  a.q.x = static_cast<const uint16_t*>(QKV), a.k.x = a.q.x + wq, a.q.up = static_cast<const uint16_t*>(dQ), a.k.up = static_cast<const uint16_t*>(dK);
-  a.q.out = static_cast<uint16_t*>(dQKV), a.k.out = a.q.out + wq, a.q.ldup = lddq, a.k.ldup = lddk;
-  if (norm) a.q.gamma = static_cast<const uint16_t*>(norm->q_gamma), a.k.gamma = static_cast<const uint16_t*>(norm->k_gamma), a.eps = norm->eps;
-  a.positions = positions, a.inv_freq = inv_freq, a.M = rows ? s->M : 0, a.ldx = ldqkv, a.ldout = lddqkv;
-  a.rotary_dim = s->rotary_dim, a.interleaved = s->interleaved != 0, a.accumulate = accumulate;
-  if (!rows) a.q.wgs = a.k.wgs = 0;
+  a.deal = deal_of(h, rows ? s->M : 0, s->q_cnt + s->kv_cnt, s->head_dim, kBwdRoom);
+  a.QKV = static_cast<const uint16_t*>(QKV), a.dQ = static_cast<const uint16_t*>(dQ), a.dK = static_cast<const uint16_t*>(dK), a.dQKV = static_cast<uint16_t*>(dQKV);
+  if (norm) a.q_gamma = static_cast<const uint16_t*>(norm->q_gamma), a.k_gamma = static_cast<const uint16_t*>(norm->k_gamma), a.eps = norm->eps;
+  a.positions = positions, a.inv_freq = inv_freq, a.M = rows ? s->M : 0, a.ldqkv = ldqkv, a.lddq = lddq, a.lddk = lddk, a.lddqkv = lddqkv;
+  a.q_cnt = s->q_cnt, a.rotary_dim = s->rotary_dim, a.interleaved = s->interleaved != 0, a.accumulate = accumulate;
   hipStream_t hs = static_cast<hipStream_t>(stream);
-  const bool sums = d_q_gamma || d_k_gamma, few = a.q.wgs <= 1 && a.k.wgs <= 1, room = h->workspace && h->workspace_bytes >= int64_t(a.q.wgs + a.k.wgs) * d * 4;
-  auto launch = [&] {
-    const dim3 grid{uint32_t(a.q.wgs + a.k.wgs)};
-    if (d == 128) hipLaunchKernelGGL(qk_norm_bwd_kernel<128>, grid, dim3(kThreads), 0, hs, a);
-    else hipLaunchKernelGGL(qk_norm_bwd_kernel<64>, grid, dim3(kThreads), 0, hs, a);
+  const int32_t n = a.deal.wgs;
+  const bool sums = d_q_gamma || d_k_gamma, room = h->workspace && h->workspace_bytes >= int64_t(n) * 2 * d * 4;
+  auto launch = [&](int32_t wgs) {
+    const dim3 grid{uint32_t(wgs)}, block{uint32_t(a.deal.threads)};
+    if (d == 128) hipLaunchKernelGGL(qk_norm_bwd_kernel<128>, grid, block, 0, hs, a);
+    else hipLaunchKernelGGL(qk_norm_bwd_kernel<64>, grid, block, 0, hs, a);
     return hipGetLastError() == hipSuccess;
   };
-  auto add_up = [&](float* d_q, float* d_k) {
-    const dim3 grid{uint32_t(d / 16), 2};
-    if (d == 128) hipLaunchKernelGGL(qk_norm_sum_kernel<128>, grid, dim3(kSumThreads), 0, hs, a.parts, a.q.wgs, a.k.wgs, d_q, d_k, accumulate);
-    else hipLaunchKernelGGL(qk_norm_sum_kernel<64>, grid, dim3(kSumThreads), 0, hs, a.parts, a.q.wgs, a.k.wgs, d_q, d_k, accumulate);
+  auto add_up = [&] {
+    const dim3 grid{uint32_t(d / 16), 2}, block{kMaxThreads};
+    if (d == 128) hipLaunchKernelGGL(qk_norm_sum_kernel<128>, grid, block, 0, hs, a.parts, n, d_q_gamma, d_k_gamma, accumulate);
+    else hipLaunchKernelGGL(qk_norm_sum_kernel<64>, grid, block, 0, hs, a.parts, n, d_q_gamma, d_k_gamma, accumulate);
     return hipGetLastError() == hipSuccess;
   };
   if (ntp::timing_on(h)) ntp::timing_begin(h, stream, "qk_norm_bwd", 0.0, 6.0 * double(a.M) * double(wq + wk));
   bool ok = true;
-  a.store = 1;
-  a.q.wanted = d_q_gamma != nullptr, a.k.wanted = d_k_gamma != nullptr;
-  if (sums && room && !few) {
+  if (n == 0) {  // a sum of nothing
+    ok = add_up();
+  } else if (sums && n > 1 && room) {
     a.parts = static_cast<float*>(h->workspace);
-    ok = launch() && add_up(d_q_gamma, d_k_gamma);
+    ok = launch(n) && add_up();
   } else {
-    if (sums) {
-      float* const none_q = a.q.wgs == 0 ? d_q_gamma : nullptr;  // a sum over no heads or no tokens
-      float* const none_k = a.k.wgs == 0 ? d_k_gamma : nullptr;
-      if (none_q || none_k) ok = add_up(none_q, none_k);
-      a.q.d_gamma = d_q_gamma, a.k.d_gamma = d_k_gamma;
-      if (!few) {  // one workgroup of each side forms them, before dQKV may take the place of dQ and dK
-        const int32_t n_q = a.q.wgs, n_k = a.k.wgs;
-        a.q.wgs = std::min(n_q, 1), a.k.wgs = std::min(n_k, 1), a.store = 0;
-        ok = ok && launch();
-        a.q.wgs = n_q, a.k.wgs = n_k, a.store = 1, a.q.wanted = a.k.wanted = 0;
-      }
+    if (sums) {  // one workgroup forms them, before dQKV may take the place of dQ and dK
+      a.d_q = d_q_gamma, a.d_k = d_k_gamma;
+      if (n > 1) a.dQKV = nullptr;
+      ok = launch(1);
+      a.d_q = a.d_k = nullptr, a.dQKV = static_cast<uint16_t*>(dQKV);
     }
-    if (a.q.wgs + a.k.wgs > 0) ok = ok && launch();
+    if (!sums || n > 1) ok = ok && launch(n);
   }
   ntp::timing_end(h, stream);
   return ok ? NTP_OK : NTP_ERR_LAUNCH;
