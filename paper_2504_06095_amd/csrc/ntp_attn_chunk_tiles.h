@@ -454,16 +454,25 @@ __device__ __forceinline__ void chunk_tiles(const ChunkArgs& a, const int wg, un
     k_products(std::integral_constant<int, KG - 1>{});
 
     const uint32_t gone = uint32_t(bad_now >> (((t - t_lo) & 15) << 2)) & 15u;  // blocks whose pages there are not
-    const bool edge = kv0 + kTileKeys > all_see || gone != 0 || w0 + 16 * QB > rows;
+    const bool edge = kv0 + kTileKeys > all_see || w0 + 16 * QB > rows;
+    if (gone != 0) {
+#pragma unroll
+      for (int kb = 0; kb < 4; ++kb)
+        if ((gone >> kb) & 1u) {
+#pragma unroll
+          for (int qb = 0; qb < QB; ++qb) st[kb][qb] = f32x4{-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+        }
+    }
     bf16x8 pf[QB][2];
 #pragma unroll
     for (int qb = 0; qb < QB; ++qb) {
       if (edge) {
+        const int room = sees[qb] - kv0 - lh * 4;
 #pragma unroll
         for (int kb = 0; kb < 4; ++kb)
 #pragma unroll
           for (int r = 0; r < 4; ++r)
-            if (kv0 + kb * 16 + lh * 4 + r >= sees[qb] || ((gone >> kb) & 1u)) st[kb][qb][r] = -INFINITY;
+            if (kb * 16 + r >= room) st[kb][qb][r] = -INFINITY;
       }
       float mx = -INFINITY;
 #pragma unroll
@@ -471,9 +480,18 @@ __device__ __forceinline__ void chunk_tiles(const ChunkArgs& a, const int wg, un
 #pragma unroll
         for (int r = 0; r < 4; ++r) mx = fmaxf(mx, st[kb][qb][r]);
       mx = over_rows(mx, larger) * a.scale_log2;
-      const float m_new = fmaxf(m_run[qb], mx);
-      const float m_use = m_new == -INFINITY ? 0.f : m_new;
-      const float alpha = fast_exp2(m_run[qb] - m_use);
+      // The reference that weights are relative to moves only where a score passes it by a factor of 2^8: a row's maximum moves with most of its first tiles, and each time all
+      // of its outputs would be scaled (57 vector instructions a block; prompts of up to 2048 tokens 106 -> 95 us).  Weights of up to 2^8 are as exact as those of up to 1.
+      const bool moves = mx > m_run[qb] + 8.0f;
+      if (__any(moves)) {
+        const float m_new = moves ? mx : m_run[qb];
+        const float alpha = m_new == -INFINITY ? 1.0f : fast_exp2(m_run[qb] - m_new);
+        l_run[qb] *= alpha;
+        m_run[qb] = m_new;
+#pragma unroll
+        for (int db = 0; db < DB; ++db) acc[qb][db] *= alpha;
+      }
+      const float m_use = m_run[qb] == -INFINITY ? 0.f : m_run[qb];  // (no score above -inf so far: weights of 0)
       float ls = 0.f;
       float pr[4][4];
 #pragma unroll
@@ -483,12 +501,7 @@ __device__ __forceinline__ void chunk_tiles(const ChunkArgs& a, const int wg, un
           pr[kb][r] = fast_exp2(fmaf(st[kb][qb][r], a.scale_log2, -m_use));
           ls += pr[kb][r];
         }
-      l_run[qb] = l_run[qb] * alpha + ls;
-      m_run[qb] = m_new;
-      if (__any(alpha != 1.0f)) {
-#pragma unroll
-        for (int db = 0; db < DB; ++db) acc[qb][db] *= alpha;
-      }
+      l_run[qb] += ls;
       // weights as bf16: half a step of 2^-8 each, of a mean of values that is rounded to the same
 #pragma unroll
       for (int s2 = 0; s2 < 2; ++s2)
