@@ -76,7 +76,7 @@ int check_chunk_shape(const ntp_attn_chunk_shape_t* s) {
 }
 
 struct ChunkChoice {
-  int32_t kv_first, kv_used, gmax, cap, qb;
+  int32_t kv_first, kv_used, gmax, g_first, g_last, cap, qb;
   int32_t row_wgs, shares, rows;    // workgroups that take sequences of few rows; shares of their line (0: workgroup = unit); most rows of a unit
   int64_t units;                    // such units at most
   int64_t tiles;                    // (sequence, KV head, row tile)s of the others at most
@@ -90,7 +90,9 @@ ChunkChoice choose_chunk(const ntp_handle* h, int64_t ws_bytes, const ntp_attn_c
   if (s->q_cnt == 0 || s->n_seq == 0 || most == 0) return c;
   c.kv_first = s->q_off / s->group - s->kv_off;
   c.kv_used = (s->q_off + s->q_cnt - 1) / s->group - s->kv_off - c.kv_first + 1;
-  c.gmax = std::min(s->group, s->q_cnt);
+  c.g_first = std::min(s->group - s->q_off % s->group, s->q_cnt);
+  c.g_last = c.kv_used > 1 ? (s->q_off + s->q_cnt - 1) % s->group + 1 : c.g_first;
+  c.gmax = c.kv_used > 2 ? s->group : std::max(c.g_first, c.g_last);
   c.qb = most * c.gmax <= 16 ? 1 : 2;
   const bool tiles = most * c.gmax > 32;
   c.cap = tiles && (s->n_seq == 1 || c.gmax > 32) ? 0 : 16 * c.qb;
@@ -99,8 +101,9 @@ ChunkChoice choose_chunk(const ntp_handle* h, int64_t ws_bytes, const ntp_attn_c
     c.rows = int32_t(std::min<int64_t>(c.cap, most * c.gmax));
   }
   if (tiles) {
-    const int64_t all = s->M * c.gmax;
-    c.tiles = c.kv_used * std::min<int64_t>(s->n_seq * ((most * c.gmax + kTileRows - 1) / kTileRows), all / kTileRows + std::min<int64_t>(s->n_seq, all / (c.cap + 1)));
+    const int64_t seqs = std::min<int64_t>(s->n_seq, s->M * c.gmax / (c.cap + 1));  // that are not of few rows
+    auto tiles_of = [&](int32_t G) { return std::min<int64_t>(s->n_seq * ((most * G + kTileRows - 1) / kTileRows), s->M * G / kTileRows + seqs); };
+    c.tiles = tiles_of(c.g_first) + std::max(c.kv_used - 2, 0) * tiles_of(c.gmax) + (c.kv_used > 1 ? tiles_of(c.g_last) : 0);
   }
   const int64_t step = s->head_dim == 128 ? 128 : 256, steps = std::max<int64_t>((s->max_len + step - 1) / step, 1);  // (8-bit steps of up to 16 rows are twice as long)
   if (c.units > 0 && steps > 4 && (steps > 8 || c.units < h->compute_units / 2)) {
@@ -179,7 +182,7 @@ extern "C" int ntp_attn_chunk_shard(ntp_handle_t* h, const ntp_attn_chunk_shape_
   a.ldq = ldq, a.ldc = ldc, a.ldt = ldt, a.page_stride = pages->page_stride, a.exp_stride = pages->exp_stride;
   a.M = int32_t(s->M), a.n_pages = int32_t(pages->n_pages), a.n_seq = s->n_seq, a.max_new = s->max_new, a.max_len = s->max_len;
   a.q_cnt = s->q_cnt, a.q_off = s->q_off, a.kv_off = s->kv_off, a.group = s->group, a.page_size = pages->page_size, a.page_log2 = ntp::log2_of(pages->page_size);
-  a.kv_first = c.kv_first, a.kv_used = c.kv_used, a.gmax = c.gmax, a.cap = c.cap, a.shares = c.shares, a.row_wgs = c.row_wgs, a.slots = c.slots, a.parts = int32_t(h->opt[NTP_OPT_ATTN_PARTS]);
+  a.kv_first = c.kv_first, a.kv_used = c.kv_used, a.gmax = c.gmax, a.g_first = c.g_first, a.g_last = c.g_last, a.cap = c.cap, a.shares = c.shares, a.row_wgs = c.row_wgs, a.slots = c.slots, a.parts = int32_t(h->opt[NTP_OPT_ATTN_PARTS]);
   a.scale_log2 = float(1.4426950408889634 / std::sqrt(double(s->head_dim)));
   hipStream_t hs = static_cast<hipStream_t>(stream);
   if (ntp::timing_on(h)) ntp::timing_begin(h, stream, fp8 ? "attn_chunk8" : "attn_chunk", 4.0 * double(s->M) * double(s->max_len) * s->head_dim * s->q_cnt, 0.0);

@@ -20,10 +20,29 @@ constexpr int kRun = 4;       // neighbouring pieces, which read the same tokens
 template <int D, bool FP8>
 constexpr int kPlaces = D == 64 && !FP8 ? 3 : 2;  // workgroups that a compute unit has room for (8-bit tiles of 64 columns: a third takes registers that a walk needs)
 
-// Row tiles and key tiles (of its last row) of a sequence; no row tiles where it is one of few rows.
-__device__ __forceinline__ void tiles_of(const ChunkArgs& a, int n, int len, int& tiles, int& walk) {
+// Of a sequence's KV heads: the first and the last that are read may be read by a part of their group only.
+struct PerHead {
+  int first, middle, last;
+  __device__ __forceinline__ int all(const ChunkArgs& a, int times = 1) const { return times * (first + max(a.kv_used - 2, 0) * middle + (a.kv_used > 1 ? last : 0)); }
+  // entry x of all heads', `times` of them for each here: its head and the number in it
+  __device__ __forceinline__ int find(const ChunkArgs& a, int times, int& x) const {
+    if (x < times * first) return 0;
+    x -= times * first;
+    const int m = middle > 0 ? min(x / (times * middle), max(a.kv_used - 2, 0)) : max(a.kv_used - 2, 0);
+    x -= m * times * middle;
+    return 1 + m;
+  }
+  __device__ __forceinline__ int of(const ChunkArgs& a, int head) const { return head == 0 ? first : head < a.kv_used - 1 ? middle : last; }
+};
+
+// Row tiles, by KV head, and key tiles (of its last row) of a sequence; no row tiles where it is one of few rows.
+__device__ __forceinline__ void tiles_of(const ChunkArgs& a, int n, int len, PerHead& tiles, int& walk) {
   const int used = min(n, a.max_new);
-  tiles = used > a.cap / a.gmax ? int((int64_t(used) * a.gmax + kTileRows - 1) / kTileRows) : 0;
+  tiles = PerHead{0, 0, 0};
+  if (used > a.cap / a.gmax) {
+    auto rows = [&](int G) { return int((int64_t(used) * G + kTileRows - 1) / kTileRows); };
+    tiles = PerHead{rows(a.g_first), rows(a.gmax), rows(a.g_last)};
+  }
   walk = max(1, (max(len - n + used, 0) + kTileKeys - 1) / kTileKeys);
 }
 
@@ -31,9 +50,10 @@ __device__ __forceinline__ void tiles_of(const ChunkArgs& a, int n, int len, int
 // last (the longest walk) on; all tiles of a sequence are cut into the same number.
 struct TilePlan {
   int units, total, piece_tiles;  // (sequence, KV head, row tile)s; pieces; key tiles of a piece at most (0: whole)
-  int start, n, len, tiles, walk;  // this lane's sequence of 64
+  int start, n, len, walk;         // this lane's sequence of 64
+  PerHead tiles;
   __device__ __forceinline__ void load(const ChunkArgs& a, int i) {
-    start = n = len = tiles = 0, walk = 1;
+    start = n = len = 0, walk = 1, tiles = PerHead{0, 0, 0};
     if (i < a.n_seq) {
       extent(a, i, start, n, len);
       tiles_of(a, n, len, tiles, walk);
@@ -50,8 +70,8 @@ struct TilePlan {
       TilePlan p;
       p.load(a, from + k * 64 + int(threadIdx.x & 63));
       p.piece_tiles = piece_tiles;
-      count += a.kv_used * p.tiles;
-      pieces += a.kv_used * p.tiles * p.cut();
+      count += p.tiles.all(a);
+      pieces += p.tiles.all(a, p.cut());
     }
   }
   __device__ __forceinline__ static int all(int v) { return __builtin_amdgcn_readlane(sum_upto(v), 63); }
@@ -64,7 +84,7 @@ struct TilePlan {
     float work = 0.f, most = 0.f;
     load(a, threadIdx.x & 63);
     auto add = [&](const TilePlan& p) {
-      const int c = a.kv_used * p.tiles;
+      const int c = p.tiles.all(a);
       count += c;
       work += float(c) * (float(p.walk) - float(min(p.n, a.max_new)) * (0.5f / kTileKeys));  // (half a triangle less)
       if (c > 0) most = fmaxf(most, float(p.walk));
@@ -84,8 +104,7 @@ struct TilePlan {
     units = total = all(count);
     if (a.slots == 0 || units == 0 || units >= 2 * a.slots) return;
     work = over_wave(work, added), most = over_wave(most, larger);
-    // (KV heads that only a part of their group reads have fewer rows)
-    const float whole = float(a.q_cnt) / float(a.kv_used * a.gmax), slots = float(a.slots), share = work * whole / slots;
+    const float slots = float(a.slots), share = work / slots;
     if (a.parts == 1 || (a.parts == 0 && most <= 1.3f * share)) return;  // (longest first, whole walks end together)
     if (a.n_seq > 64) {  // (not looked at piece by piece)
       if (units >= a.slots || most <= 1.5f * share) return;
@@ -100,9 +119,9 @@ struct TilePlan {
       piece_tiles = 0, total = units;
       return;
     }
-    const auto longest_of = [&] { return over_wave(tiles > 0 ? float(walk) * __builtin_amdgcn_rcpf(float(cut())) : 0.0f, larger); };
+    const auto longest_of = [&] { return over_wave(tiles.all(a) > 0 ? float(walk) * __builtin_amdgcn_rcpf(float(cut())) : 0.0f, larger); };
     auto estimate = [&](float longest, int all_pieces) {
-      const float pieces = float(all_pieces) * whole, rounds = ceilf(pieces / slots);
+      const float pieces = float(all_pieces), rounds = ceilf(pieces / slots);
       const float walks = 2.0f * pieces <= slots ? 0.78f * longest : fminf(rounds * longest, fmaxf(longest, share + 0.5f * longest));
       return walks + 3.0f * rounds + (all_pieces > units ? pieces * (1.0f / 45) : 0.0f);
     };
@@ -114,9 +133,9 @@ struct TilePlan {
     __shared__ int tiles_of_best[kWaves], total_of_best[kWaves];
     const int wave = uniform(threadIdx.x >> 6);
     for (int j = wave; j < (a.parts > 0 ? 1 : 6); j += kWaves) {
-      const float S = a.parts > 0 ? most / float(a.parts) : j < 3 ? most / float(j + 2) : work * whole / (j == 3 ? slots : j == 4 ? 0.5f * slots : fmaxf(slots - float(units) * whole, 1.0f));
+      const float S = a.parts > 0 ? most / float(a.parts) : j < 3 ? most / float(j + 2) : work / (j == 3 ? slots : j == 4 ? 0.5f * slots : fmaxf(slots - float(units), 1.0f));
       piece_tiles = max(kMinPiece, int(ceilf(S)));
-      const int pieces = all(a.kv_used * tiles * cut());
+      const int pieces = all(tiles.all(a, cut()));
       if (pieces > 2 * a.slots || pieces == units) continue;
       const float t = estimate(longest_of(), pieces);
       if (t < best) best = t, best_tiles = piece_tiles, total = pieces;
@@ -129,12 +148,13 @@ struct TilePlan {
       if (best_of[k] < best) best = best_of[k], best_tiles = tiles_of_best[k], total = total_of_best[k];
     piece_tiles = uniform(best_tiles), total = uniform(total);
   }
-  // Row tiles of this lane's sequence whose walks have `least` key tiles or more: row tile t's last row is min(rows, 128 (t + 1)) - 1, of token len - n + row / gmax.
-  __device__ __forceinline__ int tiles_from(const ChunkArgs& a, int least) const {
+  // Row tiles of this lane's sequence whose walks have `least` key tiles or more: row tile t's last row is min(rows, 128 (t + 1)) - 1, of token len - n + row / G.
+  __device__ __forceinline__ PerHead tiles_from(const ChunkArgs& a, int least) const {
     const int used = min(n, a.max_new), m = (least - 1) * kTileKeys - (len - n);  // (tokens of the chunk behind which the walk is so long)
     if (least <= 0 || m <= 0) return tiles;
-    if (m >= used) return 0;
-    return tiles - (m * a.gmax + kTileRows) / kTileRows + 1;
+    if (m >= used) return PerHead{0, 0, 0};
+    auto from = [&](int t, int G) { return t > 0 ? t - (m * G + kTileRows) / kTileRows + 1 : 0; };
+    return PerHead{from(tiles.first, a.g_first), from(tiles.middle, a.gmax), from(tiles.last, a.g_last)};
   }
   static constexpr int kLevel = 8;  // key tiles
   // x < total: its sequence, KV head, row tile, and piece.  Where there are more whole walks than places, the longest come first, whosever they are, by levels of their lengths: tiles of a
@@ -142,20 +162,23 @@ struct TilePlan {
   int seq, head, tile, piece, n_pieces, seq_start, seq_n, seq_len;
   __device__ __forceinline__ void find(const ChunkArgs& a, int x) {
     if (piece_tiles == 0 && a.n_seq <= 64) {
-      auto upto = [&](int level) { return all(a.kv_used * tiles_from(a, level * kLevel)); };
+      auto upto = [&](int level) { return all(tiles_from(a, level * kLevel).all(a)); };
       int lo = 0, hi = a.max_len / (kTileKeys * kLevel) + 1, longer = 0;  // the level: the highest with more than x tiles in it and above it
       while (hi - lo > 1) {
         const int mid = (lo + hi) / 2, count = upto(mid);
         if (count > x) lo = mid;
         else hi = mid, longer = count;
       }
-      const int above = tiles_from(a, (lo + 1) * kLevel), here = tiles_from(a, lo * kLevel) - above, sum = sum_upto(a.kv_used * here);
+      const PerHead above = tiles_from(a, (lo + 1) * kLevel), from = tiles_from(a, lo * kLevel);
+      const PerHead here = {from.first - above.first, from.middle - above.middle, from.last - above.last};
+      const int mine = here.all(a), sum = sum_upto(mine);
       const int at = __builtin_ctzll(__ballot(longer + sum > x));
       auto of = [&](int v) { return __builtin_amdgcn_readlane(v, at); };
-      const int rest = x - longer - (of(sum) - a.kv_used * of(here));
+      const PerHead h = {of(here.first), of(here.middle), of(here.last)}, up = {of(above.first), of(above.middle), of(above.last)}, t = {of(tiles.first), of(tiles.middle), of(tiles.last)};
+      int rest = x - longer - (of(sum) - of(mine));
       n_pieces = 1, piece = 0;
-      head = rest / of(here);
-      tile = of(tiles) - 1 - of(above) - rest % of(here);
+      head = h.find(a, 1, rest);
+      tile = t.of(a, head) - 1 - up.of(a, head) - rest;
       seq = at, seq_start = of(start), seq_n = of(n), seq_len = of(len);
       return;
     }
@@ -171,18 +194,18 @@ struct TilePlan {
       load(a, from + int(threadIdx.x & 63));
     }
     for (;;) {
-      const int mine = a.kv_used * tiles * cut(), upto = sum_upto(mine);
+      const int mine = tiles.all(a, cut()), upto = sum_upto(mine);
       const uint64_t behind = __ballot(before + upto > x);
       if (behind) {
         const int at = __builtin_ctzll(behind);
         auto of = [&](int v) { return __builtin_amdgcn_readlane(v, at); };
-        const int t = of(tiles);
+        const PerHead h = {of(tiles.first), of(tiles.middle), of(tiles.last)};
         n_pieces = of(cut());
         int rest = x - before - (of(upto) - of(mine));
+        head = h.find(a, n_pieces, rest);
+        const int t = h.of(a, head);
         tile = t - 1 - rest % t;
-        rest /= t;
-        piece = rest % n_pieces;
-        head = rest / n_pieces;
+        piece = rest / t;
         seq = from + at, seq_start = of(start), seq_n = of(n), seq_len = of(len);
         return;
       }
@@ -207,17 +230,20 @@ struct TilePlan {
       load(a, from + int(threadIdx.x & 63));
     }
     for (;;) {
-      const int mine = a.kv_used * tiles, upto = sum_upto(mine), pieces_upto = sum_upto(mine * cut());
+      const int mine = tiles.all(a), cut_up = tiles.all(a, cut()), upto = sum_upto(mine), pieces_upto = sum_upto(cut_up);
       const uint64_t behind = __ballot(before + upto > unit);
       if (behind) {
         const int at = __builtin_ctzll(behind);
         auto of = [&](int v) { return __builtin_amdgcn_readlane(v, at); };
-        tiles_there = of(tiles);
+        const PerHead h = {of(tiles.first), of(tiles.middle), of(tiles.last)};
         n_pieces = of(cut());
-        const int rest = unit - before - (of(upto) - of(mine)), place = rest % tiles_there;
-        head = rest / tiles_there, tile = tiles_there - 1 - place;
+        const int number = unit - before - (of(upto) - of(mine));
+        int place = number;
+        head = h.find(a, 1, place);
+        tiles_there = h.of(a, head);
+        tile = tiles_there - 1 - place;
         seq_start = of(start), seq_n = of(n);
-        return pieces + of(pieces_upto) - of(mine * cut()) + head * n_pieces * tiles_there + place;
+        return pieces + of(pieces_upto) - of(cut_up) + (number - place) * n_pieces + place;
       }
       before += __builtin_amdgcn_readlane(upto, 63);
       pieces += __builtin_amdgcn_readlane(pieces_upto, 63);
@@ -420,16 +446,17 @@ __device__ __forceinline__ void chunk_tiles(const ChunkArgs& a, const int wg, un
     f32x4 st[4][QB];
     auto k_products = [&](auto grp) {
       constexpr int q = decltype(grp)::value;
+      // (a product of every block in turn: none waits for the one before)
 #pragma unroll
-      for (int k = 0; k < PER; ++k)
+      for (int ks = 0; ks < KS; ++ks) {
 #pragma unroll
-        for (int qb = 0; qb < QB; ++qb) {
-          st[q * PER + k][qb] = f32x4{0.f, 0.f, 0.f, 0.f};
+        for (int k = 0; k < PER; ++k)
 #pragma unroll
-          for (int ks = 0; ks < KS; ++ks)
-            st[q * PER + k][qb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, kf[q][k * KS + ks]), qf[qb][ks], st[q * PER + k][qb], 0, 0, 0);
-        }
-      __builtin_amdgcn_sched_barrier(0);
+          for (int qb = 0; qb < QB; ++qb)
+            st[q * PER + k][qb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, kf[q][k * KS + ks]), qf[qb][ks],
+                                                                          ks == 0 ? f32x4{0.f, 0.f, 0.f, 0.f} : st[q * PER + k][qb], 0, 0, 0);
+        __builtin_amdgcn_sched_barrier(0);
+      }
     };
     // value fragments, eight reads (two 16-column blocks) a group: [group][(db % 2) * 4 + kb], tokens kb * 16 ..
     constexpr int VG = DB / 2;
@@ -444,6 +471,7 @@ __device__ __forceinline__ void chunk_tiles(const ChunkArgs& a, const int wg, un
     using I1 = std::integral_constant<int, 1>;
     k_reads(I0{});
     lds_reads_done(kf[0]);
+    __builtin_amdgcn_s_setprio(1);
     if constexpr (KG == 2) {
       k_reads(I1{});
       k_products(I0{});
@@ -452,6 +480,7 @@ __device__ __forceinline__ void chunk_tiles(const ChunkArgs& a, const int wg, un
     v_reads(I0{});
     v_reads(I1{});
     k_products(std::integral_constant<int, KG - 1>{});
+    __builtin_amdgcn_s_setprio(0);
 
     const uint32_t gone = uint32_t(bad_now >> (((t - t_lo) & 15) << 2)) & 15u;  // blocks whose pages there are not
     const bool edge = kv0 + kTileKeys > all_see || w0 + 16 * QB > rows;
@@ -515,20 +544,22 @@ __device__ __forceinline__ void chunk_tiles(const ChunkArgs& a, const int wg, un
     auto v_products = [&](auto grp) {
       constexpr int q = decltype(grp)::value;
 #pragma unroll
-      for (int d2 = 0; d2 < 2; ++d2)
+      for (int s2 = 0; s2 < 2; ++s2) {
 #pragma unroll
-        for (int s2 = 0; s2 < 2; ++s2) {
+        for (int d2 = 0; d2 < 2; ++d2) {
           const u32x2 lo = vf[q][d2 * 4 + s2 * 2], hi = vf[q][d2 * 4 + s2 * 2 + 1];
           const u32x4 both = {lo[0], lo[1], hi[0], hi[1]};
 #pragma unroll
           for (int qb = 0; qb < QB; ++qb)
             acc[qb][q * 2 + d2] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, both), pf[qb][s2], acc[qb][q * 2 + d2], 0, 0, 0);
         }
-      __builtin_amdgcn_sched_barrier(0);
+        __builtin_amdgcn_sched_barrier(0);
+      }
     };
     lds_reads_done(vf[0]);
     lds_reads_tied(vf[1]);
     __builtin_amdgcn_sched_barrier(0);
+    __builtin_amdgcn_s_setprio(1);
     if constexpr (VG == 4) {
       using I2 = std::integral_constant<int, 2>;
       using I3 = std::integral_constant<int, 3>;
@@ -544,6 +575,7 @@ __device__ __forceinline__ void chunk_tiles(const ChunkArgs& a, const int wg, un
       v_products(I0{});
       v_products(I1{});
     }
+    __builtin_amdgcn_s_setprio(0);
   };
 
   if (t_lo < t_hi) {
