@@ -163,7 +163,8 @@ struct TilePlan {
   __device__ __forceinline__ void find(const ChunkArgs& a, int x) {
     if (piece_tiles == 0 && a.n_seq <= 64) {
       auto upto = [&](int level) { return all(tiles_from(a, level * kLevel).all(a)); };
-      int lo = 0, hi = a.max_len / (kTileKeys * kLevel) + 1, longer = 0;  // the level: the highest with more than x tiles in it and above it
+      // the level: the highest with more than x tiles in it and above it (none has `hi`: no walk is longer than max_len's)
+      int lo = 0, hi = (a.max_len + kTileKeys - 1) / kTileKeys / kLevel + 1, longer = 0;
       while (hi - lo > 1) {
         const int mid = (lo + hi) / 2, count = upto(mid);
         if (count > x) lo = mid;

@@ -209,3 +209,52 @@ def test_nothing_to_do():
     Q, C = (torch.full((3, 128), 5.0, dtype=torch.bfloat16, device="cuda") for _ in range(2))
     N.ntp_attn_chunk_shard(N.attn_chunk_shape(3, 1, 3, 40, plan, 2), N.kv_pages(e, e), Q, torch.tensor([0, 3], dtype=torch.int32, device="cuda"), z(1, 3), z(1) + 40, C)
     assert not bool(C.any())  # a cache without pages: no row sees anything
+
+
+@pytest.mark.parametrize("fmt", [16, 8])
+@pytest.mark.parametrize("length", [448, 449, 503, 511, 512, 513, 961, 1023, 1024, 1025])
+def test_whole_walks_around_the_lengths_of_their_levels(length, fmt):
+    """Walks are taken longest first by levels of 512 tokens: max_len just below, at and behind a level's border (below it the highest level once had no walks looked for, and row
+    tiles came out of the lengths' range)."""
+    _say(f"whole walks, 9 sequences of {length}, {fmt} bits")
+    c = Case([length - 6] * 9, [length] * 9, 4, 4, 128, 16, 0, 0, 1, fmt)
+    c.check(*c.run(False))
+    c.check(*c.run(True))
+
+
+@pytest.mark.parametrize("fmt,d", [(16, 64), (8, 128)])
+def test_more_whole_walks_than_places(fmt, d):
+    news = [600, 130, 33, 511, 640, 129, 577, 600, 1, 600]
+    lengths = [600, 200, 700, 511, 1000, 129, 700, 640, 30, 1100]
+    c = Case(news, lengths, 15, 5, d, 64, 1, 0, 4, fmt, padded=3) if d == 64 else Case(news, lengths, 14, 14, d, 64, 0, 0, 1, fmt, padded=3)
+    c.check(*c.run(True))
+
+
+@pytest.mark.parametrize("fmt", [16, 8])
+@pytest.mark.parametrize("workspace", [False, True], ids=["whole", "cut"])
+@pytest.mark.parametrize("long_ones", [1, 40])
+def test_hundreds_of_sequences(long_ones, workspace, fmt):
+    rng = np.random.default_rng(7)
+    n = 700
+    news, lengths = [1] * n, [int(x) for x in rng.integers(0, 90, n)]
+    for i in rng.choice(n, long_ones, replace=False):
+        news[i] = int(rng.integers(33, 150))
+        lengths[i] = news[i] + int(rng.integers(0, 1200 if long_ones > 1 else 5000))
+    _say(f"{n} sequences, {long_ones} of them with chunks, {fmt} bits")
+    c = Case(news, lengths, 2, 1, 64, 16, 0, 0, 2, fmt)
+    c.check(*c.run(workspace))
+
+
+@pytest.mark.parametrize("parts", [1, 2, 5, 16])
+def test_parts_by_option(parts):
+    import torch
+    c = Case([200, 1, 77], [1500, 300, 2100], 6, 2, 128, 32, 0, 0, 3, 16)
+    want, _ = c.run(True)
+    N, h = c.N, c.N.ntp_create()
+    N.ntp_set_option(N.binding.NTP_OPT_ATTN_PARTS, parts, handle=h)
+    N.ntp_set_workspace(torch.empty(N.ntp_workspace_bytes(N.binding.NTP_CALL_ATTN_CHUNK_SHARD, c.shape, handle=h), dtype=torch.uint8, device="cuda"), handle=h)
+    C, LSE = torch.full_like(want, 77.0), torch.full((6, c.M), 77.0, device="cuda")
+    N.ntp_attn_chunk_shard(c.shape, c.pages, c.Q, c.starts_dev, c.table, c.len_dev, C, LSE, handle=h)
+    torch.cuda.synchronize()
+    c.check(C, LSE)
+    N.ntp_destroy(h)
