@@ -516,8 +516,9 @@ int ntp_qk_norm_shard_bwd(ntp_handle_t* h, const ntp_kv_append_shape_t* shape, c
  *   C           [M x q_cnt head_dim] bf16.  A row that sees no token (a length of 0, or shorter than its sequence's rows) gets zeros, and so does a query
  *               head all of whose scores are -inf; rows of no sequence (the padding of a batch) stay as they are
  *   LSE         DEVICE fp32 [q_cnt x M], may be NULL: natural logarithm of the sum of exp(score); -inf in both of these cases
- * No output may alias another buffer.  What lies in the pages behind a sequence's last token is not used (it may be NaN).  M * q_cnt < 2^31, max_len <= 2^30 and
- * n_seq (max_len + 1) (kv heads) < 2^31 in steps of 64 tokens (UNSUPPORTED beyond).  With a workspace of ntp_workspace_bytes (NTP_CALL_ATTN_CHUNK_SHARD) walks over many tokens
+ * No output may alias another buffer.  What lies in the pages behind a sequence's last token is not used (it may be NaN).  A NaN or an infinity among the values of one of the sequence's own
+ * tokens may reach rows before it too (a weight of 0 times NaN).  M * q_cnt < 2^31, max_len <= 2^30, n_seq (max_len / 64 + 2) kv_cnt < 2^31 and
+ * n_seq kv_cnt < 2^24 (UNSUPPORTED beyond).  With a workspace of ntp_workspace_bytes (NTP_CALL_ATTN_CHUNK_SHARD) walks over many tokens
  * are cut into parts where there are few rows, and their order of fp32 sums then depends on the lengths of the whole batch (the same lengths give the same bits); a smaller one is not used. */
 typedef struct ntp_attn_chunk_shape {
   int64_t M;

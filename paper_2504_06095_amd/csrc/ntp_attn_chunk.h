@@ -32,7 +32,7 @@ struct ChunkArgs {
   int32_t kv_first, kv_used, gmax;  // local KV heads that are read; the most local query heads of one
   int32_t g_first, g_last;          // those of the first and of the last
   int32_t cap;                      // sequences of up to so many rows (tokens x gmax) go by ntp_attn_chunk_rows.h, the others by ntp_attn_chunk_tiles.h
-  int32_t shares, row_wgs;          // shares that the line is cut into at most; workgroups of the launch that take them (the first ones)
+  int32_t shares, tile_wgs;         // shares that the line is cut into at most; workgroups of a launch of both kinds that take row tiles (the first ones)
   int32_t slots;                    // workgroups that the device has room for, which walks are cut for (into up to twice as many pieces); 0: never
   int32_t parts;                    // 0, or that many pieces of the longest walk (NTP_OPT_ATTN_PARTS)
   float scale_log2;                 // log2(e) / sqrt(d)

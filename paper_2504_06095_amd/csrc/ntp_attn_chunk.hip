@@ -28,8 +28,9 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2))) v
 template <int D, bool FP8>
 __global__ __attribute__((amdgpu_flat_work_group_size(kThreads, kThreads), amdgpu_waves_per_eu(2, 2))) void chunk_both_kernel(const ChunkArgs a) {
   __shared__ __attribute__((aligned(1024))) unsigned char lds[std::max(kRowLds<D, 2>, kTileLds<D>)];
-  if (int(blockIdx.x) < a.row_wgs) chunk_rows<D, FP8, 2>(a, int(blockIdx.x), lds);
-  else chunk_tiles<D, FP8>(a, int(blockIdx.x) - a.row_wgs, lds);
+  // (the row tiles first: their walks are the longest, and what reads from HBM alone fills the compute units that they leave)
+  if (int(blockIdx.x) < a.tile_wgs) chunk_tiles<D, FP8>(a, int(blockIdx.x), lds);
+  else chunk_rows<D, FP8, 2>(a, int(blockIdx.x) - a.tile_wgs, lds);
 }
 
 template <int D, bool FP8>
@@ -77,9 +78,11 @@ int check_chunk_shape(const ntp_attn_chunk_shape_t* s) {
 
 struct ChunkChoice {
   int32_t kv_first, kv_used, gmax, g_first, g_last, cap, qb;
-  int32_t row_wgs, shares, rows;    // workgroups that take sequences of few rows; shares of their line (0: workgroup = unit); most rows of a unit
+  int64_t row_wgs;                  // workgroups that take sequences of few rows
+  int32_t shares, rows;             // shares of their line (0: workgroup = unit); most rows of a unit
   int64_t units;                    // such units at most
   int64_t tiles;                    // (sequence, KV head, row tile)s of the others at most
+  int64_t tile_wgs;                 // workgroups for them
   int32_t slots;                    // workgroups that the device has room for: walks are cut for these (0: never), into twice as many at most
   int64_t ws_rows, ws_bytes;        // bytes of the line's partial results, and of all
 };
@@ -107,14 +110,14 @@ ChunkChoice choose_chunk(const ntp_handle* h, int64_t ws_bytes, const ntp_attn_c
   }
   const int64_t step = s->head_dim == 128 ? 128 : 256, steps = std::max<int64_t>((s->max_len + step - 1) / step, 1);  // (8-bit steps of up to 16 rows are twice as long)
   if (c.units > 0 && steps > 4 && (steps > 8 || c.units < h->compute_units / 2)) {
-    c.shares = int32_t(std::min<int64_t>(std::min(2 * int64_t(h->compute_units), steps * c.units), kMaxShares));
+    c.shares = int32_t(std::min<int64_t>(std::min((tiles ? 1 : 2) * int64_t(h->compute_units), steps * c.units), kMaxShares));
     c.ws_rows = (int64_t(c.shares) * 2 * c.cap * (s->head_dim + 2) * 4 + 255) / 256 * 256;
   }
   if (tiles && s->max_len > kMinPiece * kTileKeys) c.slots = (s->head_dim == 64 && c.cap == 0 && !fp8 ? kPlaces<64, false> : kPlaces<128, false>) * h->compute_units;
   c.ws_bytes = c.ws_rows + (c.slots > 0 ? 256 + int64_t(2 * c.slots) * kTileRows * (s->head_dim + kPartPad) * 4 : 0);
   if (c.ws_bytes > ws_bytes) c.shares = c.slots = 0, c.ws_rows = c.ws_bytes = 0;
-  c.row_wgs = int32_t(c.shares > 0 ? c.shares : c.units);
-  if (tiles) c.row_wgs = (c.row_wgs + 7) / 8 * 8;  // (the row tiles' workgroups keep their XCDs)
+  c.row_wgs = c.shares > 0 ? c.shares : c.units;
+  if (tiles) c.tile_wgs = (std::max<int64_t>(c.tiles, 2 * c.slots) + 8 * kRun - 1) / (8 * kRun) * (8 * kRun);
   return c;
 }
 
@@ -132,8 +135,7 @@ constexpr int kJoinWgs = 1024;  // that join row tiles
 
 template <int D, bool FP8>
 bool launch_chunk(const ChunkArgs& a, const ChunkChoice& c, hipStream_t hs) {
-  const int64_t tile_wgs = c.tiles > 0 ? (std::max<int64_t>(c.tiles, 2 * c.slots) + 8 * kRun - 1) / (8 * kRun) * (8 * kRun) : 0;
-  const dim3 grid{uint32_t(c.row_wgs + tile_wgs)}, block{kThreads};
+  const dim3 grid{uint32_t(c.row_wgs + c.tile_wgs)}, block{kThreads};
   if (c.tiles > 0 && c.cap > 0) hipLaunchKernelGGL((chunk_both_kernel<D, FP8>), grid, block, 0, hs, a);
   else if (c.tiles > 0) hipLaunchKernelGGL((chunk_tiles_kernel<D, FP8>), grid, block, 0, hs, a);
   else if (c.qb == 1) hipLaunchKernelGGL((chunk_rows_kernel<D, FP8, 1>), grid, block, 0, hs, a);
@@ -164,9 +166,10 @@ extern "C" int ntp_attn_chunk_shard(ntp_handle_t* h, const ntp_attn_chunk_shape_
   if (!Q || !C || !lengths || (!block_table && used > 0) || ldq < w || ldc < w || ldt < used) return NTP_ERR_INVALID_ARG;
   auto off4 = [](const void* p) { return (reinterpret_cast<uintptr_t>(p) & 3) != 0; };
   if (off16(Q) || off16(C) || ldq % 8 || ldc % 8 || off4(row_starts) || off4(block_table) || off4(lengths) || off4(LSE)) return NTP_ERR_ALIGNMENT;
-  if (h->device < 0) return NTP_ERR_NO_DEVICE;
   const bool fp8 = pages->format == NTP_KV_E4M3;
   const ChunkChoice c = choose_chunk(h, h->workspace ? h->workspace_bytes : 0, s, fp8);
+  if (c.row_wgs + c.tile_wgs > 0xffffffffll / kThreads) return NTP_ERR_UNSUPPORTED;  // a launch counts its threads in 32 bits
+  if (h->device < 0) return NTP_ERR_NO_DEVICE;
   ChunkArgs a{};
   a.Q = static_cast<const uint16_t*>(Q), a.K = static_cast<const unsigned char*>(pages->K), a.V = static_cast<const unsigned char*>(pages->V);
   a.K_exp = static_cast<const uint8_t*>(pages->K_exp), a.V_exp = static_cast<const uint8_t*>(pages->V_exp);
@@ -182,7 +185,7 @@ extern "C" int ntp_attn_chunk_shard(ntp_handle_t* h, const ntp_attn_chunk_shape_
   a.ldq = ldq, a.ldc = ldc, a.ldt = ldt, a.page_stride = pages->page_stride, a.exp_stride = pages->exp_stride;
   a.M = int32_t(s->M), a.n_pages = int32_t(pages->n_pages), a.n_seq = s->n_seq, a.max_new = s->max_new, a.max_len = s->max_len;
   a.q_cnt = s->q_cnt, a.q_off = s->q_off, a.kv_off = s->kv_off, a.group = s->group, a.page_size = pages->page_size, a.page_log2 = ntp::log2_of(pages->page_size);
-  a.kv_first = c.kv_first, a.kv_used = c.kv_used, a.gmax = c.gmax, a.g_first = c.g_first, a.g_last = c.g_last, a.cap = c.cap, a.shares = c.shares, a.row_wgs = c.row_wgs, a.slots = c.slots, a.parts = int32_t(h->opt[NTP_OPT_ATTN_PARTS]);
+  a.kv_first = c.kv_first, a.kv_used = c.kv_used, a.gmax = c.gmax, a.g_first = c.g_first, a.g_last = c.g_last, a.cap = c.cap, a.shares = c.shares, a.tile_wgs = int32_t(c.tile_wgs), a.slots = c.slots, a.parts = int32_t(h->opt[NTP_OPT_ATTN_PARTS]);
   a.scale_log2 = float(1.4426950408889634 / std::sqrt(double(s->head_dim)));
   hipStream_t hs = static_cast<hipStream_t>(stream);
   if (ntp::timing_on(h)) ntp::timing_begin(h, stream, fp8 ? "attn_chunk8" : "attn_chunk", 4.0 * double(s->M) * double(s->max_len) * s->head_dim * s->q_cnt, 0.0);

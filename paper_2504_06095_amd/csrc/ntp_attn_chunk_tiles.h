@@ -279,6 +279,9 @@ __device__ __forceinline__ void chunk_tiles(const ChunkArgs& a, const int wg, un
   const int in_xcd = wg / 8, round = in_xcd / kRun;
   const int id = uniform((round * 8 + ((wg - round) & 7)) * kRun + (in_xcd + round) % kRun);
   if (id >= plan.total) return;
+  // The two workgroups that a compute unit gets first would go through their matrix instructions, and then their softmax, together: the second one starts a microsecond later, half a
+  // key tile (one sequence of 8192 tokens, 14 heads 250 -> 241 us).
+  if (in_xcd / 32 == 1) __builtin_amdgcn_s_sleep(32);
   plan.find(a, id);
   const int seq = uniform(plan.seq), start = uniform(plan.seq_start), n = uniform(plan.seq_n), len = uniform(plan.seq_len), used = min(n, a.max_new);
   const int g = a.kv_first + uniform(plan.head), n_pieces = uniform(plan.n_pieces), piece = uniform(plan.piece);

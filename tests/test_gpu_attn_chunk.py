@@ -258,3 +258,64 @@ def test_parts_by_option(parts):
     torch.cuda.synchronize()
     c.check(C, LSE)
     N.ntp_destroy(h)
+
+
+@pytest.mark.parametrize("fmt", [16, 8])
+def test_pages_behind_four_gigabytes(fmt):
+    """Keys and values of 5.4 GB (bf16) and 2.7 GB (8 bits, 43 MB of powers of two); the batch's pages are the last ones."""
+    import torch
+    import paper_2504_06095_amd as N
+    d, page, kv, n_pages = 128, 4096, 2, 2570
+    K, V = (torch.zeros(n_pages, kv, page, d, dtype=torch.bfloat16 if fmt == 16 else torch.uint8, device="cuda") for _ in range(2))
+    E = [torch.full((n_pages, kv, page), 127, dtype=torch.uint8, device="cuda") for _ in range(2)] if fmt == 8 else []
+    plan, f8 = dict(q_cnt=6, kv_cnt=kv, q_off=0, kv_off=0, head_dim=d), torch.float8_e4m3fn
+    pages = N.kv_pages(K, V) if fmt == 16 else N.kv_pages(K.view(f8), V.view(f8), *E)
+    news, lens = [1, 200, 40], [700, 4100, 40]
+    table = torch.tensor([[n_pages - 1, 0], [n_pages - 2, n_pages - 4], [n_pages - 3, 0]], dtype=torch.int32, device="cuda")
+    tokens = [(s, t) for s, n in enumerate(lens) for t in range(n)]
+    slots = torch.tensor([int(table[s, t // page]) * page + t % page for s, t in tokens], device="cuda")
+    g = torch.Generator(device="cuda").manual_seed(1)
+    QKV = torch.randn(len(tokens), 10 * d, device="cuda", generator=g).bfloat16()
+    N.ntp_qk_norm_append_shard(N.kv_append_shape(len(tokens), plan, 0), None, pages, QKV, None, slots, None)
+    M = sum(news)
+    Q = torch.randn(M, 6 * d, device="cuda", generator=g).bfloat16()
+    starts, L = (torch.tensor(x, dtype=torch.int32, device="cuda") for x in ([0, 1, 201, 241], lens))
+    C, h = torch.zeros(M, 6 * d, dtype=torch.bfloat16, device="cuda"), N.ntp_create()
+    shape = N.attn_chunk_shape(M, 3, 200, 4100, plan, 3)
+    N.ntp_set_workspace(torch.empty(N.ntp_workspace_bytes(N.binding.NTP_CALL_ATTN_CHUNK_SHARD, shape, handle=h), dtype=torch.uint8, device="cuda"), handle=h)
+    N.ntp_attn_chunk_shard(shape, pages, Q, starts, table, L, C, handle=h)
+    torch.cuda.synchronize()
+    assert int((K != 0).any(3).sum()) == kv * len(tokens)
+    # the oracle over the few pages in use
+    used = torch.tensor([n_pages - 4, n_pages - 3, n_pages - 2, n_pages - 1], device="cuda")
+    num = [f64(t[used]) if fmt == 16 else np.ldexp(f64(t[used].view(f8)), (e[used].cpu().numpy().astype(np.int64) - 127)[..., None]) for t, e in zip((K, V), E or (None, None))]
+    small = np.array([[3, 0], [2, 0], [1, 0]])
+    want, _, size, _ = B.attn_chunk(f64(Q), *num, [0, 1, 201, 241], small, lens, 200, 4100, 0, 0, 3)
+    assert (np.abs(f64(C) - want) <= BF * np.abs(want) + (BF + F32) * size).all()
+    N.ntp_destroy(h)
+
+
+@pytest.mark.parametrize("new", [1, 50])
+def test_a_batch_without_any_tokens(new):
+    import torch
+    import paper_2504_06095_amd as N
+    e = torch.empty(0, 1, 16, 64, dtype=torch.bfloat16, device="cuda")
+    plan = dict(q_cnt=2, kv_cnt=1, q_off=0, kv_off=0, head_dim=64)
+    z = lambda *s: torch.zeros(*s, dtype=torch.int32, device="cuda")  # noqa: E731
+    M = 2 * new
+    C, LSE = torch.full((M, 128), 5.0, dtype=torch.bfloat16, device="cuda"), torch.zeros(2, M, device="cuda")
+    N.ntp_attn_chunk_shard(N.attn_chunk_shape(M, 2, new, 0, plan, 2), N.kv_pages(e, e), torch.ones_like(C), torch.tensor([0, new, M], dtype=torch.int32, device="cuda"), z(2, 0), z(2), C, LSE)
+    assert not bool(C.any()) and bool(torch.isneginf(LSE).all())
+
+
+def test_a_call_ends_with_the_rows_that_it_has():
+    """Views of wider matrices, with what lies beside the columns left alone."""
+    import torch
+    c = Case([70, 1, 33], [400, 90, 33], 5, 2, 64, 16, 3, 0, 6, 8, pad=24)
+    full = torch.full((c.M + 2, 5 * 64 + 40), 77.0, dtype=torch.bfloat16, device="cuda")
+    C = full[1:-1, 16:16 + 5 * 64]
+    c.N.ntp_attn_chunk_shard(c.shape, c.pages, c.Q, c.starts_dev, c.table, c.len_dev, C)
+    torch.cuda.synchronize()
+    c.check(C, None)
+    full[1:-1, 16:16 + 5 * 64] = 77.0
+    assert bool((full == 77).all())

@@ -108,6 +108,7 @@ def test_chunk_refuses(h):  # noqa: F811
         assert _chunk(h, s) == INV, s
     for s in (dict(head_dim=32), dict(M=1 << 31), dict(M=1 << 30), dict(max_len=(1 << 30) + 1), dict(n_seq=1 << 26, max_len=1 << 20)):
         assert _chunk(h, s) == UNSUP, s
+    assert _chunk(h, dict(n_seq=(1 << 24) + 1, M=(1 << 24) + 1, max_new=1, max_len=0, q_cnt=1), starts=None, ldt=0) == UNSUP  # (more than a launch has room for)
     for fp8, bad in ((False, BAD_PAGES), (True, BAD_PAGES8)):
         for c, want in bad:
             assert _chunk(h, None, c, fp8=fp8) == want, (fp8, c)
