@@ -486,7 +486,8 @@ typedef struct ntp_kv_pages { /* DEVICE */
  * head_dim elements becomes, before it is rotated,
  *   x / sqrt(sum x^2 / head_dim + eps) .* gamma       (sums and results fp32, rounded once behind the rotation: to bf16 in Qout, Kout and bf16 pages, to e4m3 in 8-bit ones)
  * with gamma = q_gamma for query heads and k_gamma for key heads (DEVICE bf16 [head_dim], 16-byte aligned; NULL: those heads have no norm; norm itself may be
- * NULL: neither has).  eps > 0 where there is a gamma.  Value heads are appended as they are.  Everything else as ntp_kv_append_shard: shape, positions, slots (NULL exactly where pages is), inv_freq,
+ * NULL: neither has).  eps > 0 where there is a gamma.  Value heads are appended as they are.  (Of 8-bit pages the pieces of rows with the same slot may be
+ * the numbers of one and the power of two of the other.)  Everything else as ntp_kv_append_shard: shape, positions, slots (NULL exactly where pages is), inv_freq,
  * what may be NULL, what is refused, and Qout and Kout in place of QKV's own columns. */
 typedef struct ntp_qk_norm {
   const void *q_gamma, *k_gamma;
@@ -517,8 +518,8 @@ int ntp_qk_norm_shard_bwd(ntp_handle_t* h, const ntp_kv_append_shape_t* shape, c
  *               head all of whose scores are -inf; rows of no sequence (the padding of a batch) stay as they are
  *   LSE         DEVICE fp32 [q_cnt x M], may be NULL: natural logarithm of the sum of exp(score); -inf in both of these cases
  * No output may alias another buffer.  What lies in the pages behind a sequence's last token is not used (it may be NaN).  A NaN or an infinity among the values of one of the sequence's own
- * tokens may reach rows before it too (a weight of 0 times NaN).  M * q_cnt < 2^31, max_len <= 2^30, n_seq (max_len / 64 + 2) kv_cnt < 2^31 and
- * n_seq kv_cnt < 2^24 (UNSUPPORTED beyond).  With a workspace of ntp_workspace_bytes (NTP_CALL_ATTN_CHUNK_SHARD) walks over many tokens
+ * tokens may reach rows before it too (a weight of 0 times NaN).  M * q_cnt < 2^31, q_cnt <= 2^20, max_len <= 2^30,
+ * n_seq (max_len / 64 + 2) kv_cnt < 2^31, n_seq (min(M, max_new) q_cnt / 128 + kv_cnt) < 2^31 and n_seq kv_cnt < 2^24 (UNSUPPORTED beyond).  With a workspace of ntp_workspace_bytes (NTP_CALL_ATTN_CHUNK_SHARD) walks over many tokens
  * are cut into parts where there are few rows, and their order of fp32 sums then depends on the lengths of the whole batch (the same lengths give the same bits); a smaller one is not used. */
 typedef struct ntp_attn_chunk_shape {
   int64_t M;

@@ -66,8 +66,11 @@ int check_chunk_shape(const ntp_attn_chunk_shape_t* s) {
   if (!s || s->M < 0 || s->n_seq < 0 || s->max_new < 0 || s->max_len < 0 || s->q_cnt < 0 || s->kv_cnt < 0 || s->q_off < 0 || s->kv_off < 0 || s->group < 1) return NTP_ERR_INVALID_ARG;
   if (s->head_dim != 64 && s->head_dim != 128) return NTP_ERR_UNSUPPORTED;
   if (s->max_len > 1 << 30 || int64_t(s->q_off) + s->q_cnt > 0x7fffffffll || s->M > 0x7fffffffll || s->M * std::max(s->q_cnt, 1) > 0x7fffffffll ||
-      int64_t(s->n_seq) * ((int64_t(s->max_len) + 63) / 64 + 1) * std::max(s->kv_cnt, 1) > 0x7fffffffll)
+      int64_t(s->n_seq) * ((int64_t(s->max_len) + 63) / 64 + 1) * std::max(s->kv_cnt, 1) > 0x7fffffffll || s->q_cnt > 1 << 20)
     return NTP_ERR_UNSUPPORTED;
+  // row tiles are counted in 32 bits, also where row_starts gives every sequence as many rows as there may be
+  const int64_t per_seq = std::min<int64_t>(s->max_new, s->M) * s->q_cnt / kTileRows + s->kv_cnt;
+  if (per_seq > 0x7fffffffll / std::max(s->n_seq, 1)) return NTP_ERR_UNSUPPORTED;
   // the KV heads of the local query heads ascend: the first and the last must be local
   if (s->q_cnt > 0) {
     const int64_t first = int64_t(s->q_off) / s->group - s->kv_off, last = (int64_t(s->q_off) + s->q_cnt - 1) / s->group - s->kv_off;

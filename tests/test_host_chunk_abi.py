@@ -109,6 +109,8 @@ def test_chunk_refuses(h):  # noqa: F811
     for s in (dict(head_dim=32), dict(M=1 << 31), dict(M=1 << 30), dict(max_len=(1 << 30) + 1), dict(n_seq=1 << 26, max_len=1 << 20)):
         assert _chunk(h, s) == UNSUP, s
     assert _chunk(h, dict(n_seq=(1 << 24) + 1, M=(1 << 24) + 1, max_new=1, max_len=0, q_cnt=1), starts=None, ldt=0) == UNSUP  # (more than a launch has room for)
+    assert _chunk(h, dict(n_seq=1 << 17, M=1 << 21, max_new=1 << 21, max_len=0, q_cnt=6), ldt=0) == UNSUP  # (row tiles past 2^31, were every sequence as long)
+    assert _chunk(h, dict(q_cnt=(1 << 20) + 8, group=1 << 21, M=1, n_seq=1, max_new=1), ldq=1 << 30, ldc=1 << 30) == UNSUP
     for fp8, bad in ((False, BAD_PAGES), (True, BAD_PAGES8)):
         for c, want in bad:
             assert _chunk(h, None, c, fp8=fp8) == want, (fp8, c)
