@@ -38,14 +38,16 @@ struct ChunkArgs {
   float scale_log2;                 // log2(e) / sqrt(d)
 };
 
-// A sequence's first row, its rows, and its tokens.
+// A sequence's first row, its rows, and its tokens; none where i is behind the last.  No branch, so that all loads, also those of several sequences, go out together.
 __device__ __forceinline__ void extent(const ChunkArgs& a, int i, int& start, int& n, int& len) {
-  start = i, n = 1;
-  if (a.starts) {
-    start = min(max(a.starts[i], 0), a.M);
-    n = max(min(max(a.starts[i + 1], 0), a.M) - start, 0);
-  }
-  len = min(max(a.lengths[i], 0), a.max_len);
+  const int at = min(i, a.n_seq - 1);
+  const bool packed = a.starts != nullptr, there = i < a.n_seq;
+  const int32_t* const starts = packed ? a.starts : a.lengths;  // (anything that may be read)
+  const int tokens = a.lengths[at], from = starts[at], to = starts[packed ? at + 1 : at];
+  start = packed ? min(max(from, 0), a.M) : at;
+  n = packed ? max(min(max(to, 0), a.M) - start, 0) : 1;
+  n = there ? n : 0;
+  len = there ? min(max(tokens, 0), a.max_len) : 0;
 }
 
 // The local query heads j0 .. j1 - 1 of a local KV head.

@@ -51,11 +51,8 @@ struct RowLine {
   __device__ __forceinline__ void load(const ChunkArgs& a, int from) {
     const int i = from + int(threadIdx.x & 63);
     base = from;
-    start = n = len = mine = 0;
-    if (i < a.n_seq) {
-      extent(a, i, start, n, len);
-      mine = row_steps<STEP>(a, n, len);
-    }
+    extent(a, i, start, n, len);
+    mine = row_steps<STEP>(a, n, len);
     upto = sum_upto(mine);
   }
   __device__ __forceinline__ int last() const { return __builtin_amdgcn_readlane(upto, 63); }
@@ -66,10 +63,8 @@ struct RowLine {
     for (int k = 0; k < kAtOnce / 64; ++k) {
       const int i = from + k * 64 + int(threadIdx.x & 63);
       int s, n, len;
-      if (i < a.n_seq) {
-        extent(a, i, s, n, len);
-        sum += row_steps<STEP>(a, n, len);
-      }
+      extent(a, i, s, n, len);
+      sum += row_steps<STEP>(a, n, len);
     }
     return __builtin_amdgcn_readlane(sum_upto(sum), 63);
   }

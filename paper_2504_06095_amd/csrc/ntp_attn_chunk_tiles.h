@@ -53,11 +53,8 @@ struct TilePlan {
   int start, n, len, walk;         // this lane's sequence of 64
   PerHead tiles;
   __device__ __forceinline__ void load(const ChunkArgs& a, int i) {
-    start = n = len = 0, walk = 1, tiles = PerHead{0, 0, 0};
-    if (i < a.n_seq) {
-      extent(a, i, start, n, len);
-      tiles_of(a, n, len, tiles, walk);
-    }
+    extent(a, i, start, n, len);
+    tiles_of(a, n, len, tiles, walk);
   }
   // (in fp32: a count one too high where walks are of millions of tiles is the same everywhere)
   __device__ __forceinline__ int cut() const { return piece_tiles == 0 ? 1 : int((float(walk) - 0.5f) * __builtin_amdgcn_rcpf(float(piece_tiles))) + 1; }
@@ -215,7 +212,7 @@ struct TilePlan {
       load(a, from + int(threadIdx.x & 63));
     }
   }
-  // unit < units: the same of it, and the number of its first piece; the unit's pieces lie `tiles_there` apart
+  // unit < units: the same of it, and the number of its first piece; the unit's pieces lie `tiles_there` apart.  -1: there is no such unit
   int tiles_there;
   __device__ __forceinline__ int find_unit(const ChunkArgs& a, int unit) {
     int from = 0, before = 0, pieces = 0;
@@ -230,7 +227,7 @@ struct TilePlan {
       }
       load(a, from + int(threadIdx.x & 63));
     }
-    for (;;) {
+    for (; from < a.n_seq;) {
       const int mine = tiles.all(a), cut_up = tiles.all(a, cut()), upto = sum_upto(mine), pieces_upto = sum_upto(cut_up);
       const uint64_t behind = __ballot(before + upto > unit);
       if (behind) {
@@ -251,6 +248,7 @@ struct TilePlan {
       from += 64;
       load(a, from + int(threadIdx.x & 63));
     }
+    return -1;
   }
 };
 
@@ -300,18 +298,25 @@ __device__ __forceinline__ void chunk_tiles(const ChunkArgs& a, const int wg, un
   // this wavefront's rows: their queries, and how many tokens they see
   const int w0 = row0 + wave * 16 * QB;
   const int all_see = len - n + token_of(wave * 16 * QB) + 1, most = w0 < rows ? len - n + token_of(min(rows - row0, wave * 16 * QB + 16 * QB) - 1) + 1 : 0;
+  // Page numbers of 16 tiles' four blocks, one a lane, and which of them there are not; the next 16 tiles' are on their way.
+  const int32_t* const row_of_table = a.table + int64_t(seq) * a.ldt;
+  const __amdgpu_buffer_rsrc_t of_table = view(row_of_table, ((end + a.page_size - 1) >> a.page_log2) * 4);  // (reads behind it give 0)
+  auto pages_from = [&](int t) {
+    const int key = (t + lane / 4) * kTileKeys + (lane & 3) * kBlock;
+    return int32_t(__builtin_amdgcn_raw_buffer_load_b32(of_table, (key >> a.page_log2) * 4, 0, 0));
+  };
+  auto missing = [&](int pg) { return __ballot(pg < 0 || pg >= a.n_pages); };
+  int32_t pages = pages_from(t_lo), pages_next = pages_from(t_lo + 16);
+  // (the queries behind them: the first tile is requested before these are there)
   bf16x8 qf[QB][KS];
   int sees[QB];
 #pragma unroll
   for (int qb = 0; qb < QB; ++qb) {
-    const int rr = w0 + qb * 16 + lq, i = token_of(rr - row0), j = j0 + rr - i * G;
-    sees[qb] = rr < rows ? len - n + i + 1 : 0;
+    const int rr = w0 + qb * 16 + lq, at = min(rr, rows - 1), i = token_of(at - row0), j = j0 + at - i * G;
+    sees[qb] = rr < rows ? len - n + i + 1 : 0;  // (rows behind the last: its queries, which see nothing)
+    const uint16_t* const q = a.Q + int64_t(start + i) * a.ldq + int64_t(j) * D + lh * 8;
 #pragma unroll
-    for (int ks = 0; ks < KS; ++ks) qf[qb][ks] = bf16x8{};
-    if (rr < rows) {
-#pragma unroll
-      for (int ks = 0; ks < KS; ++ks) qf[qb][ks] = *reinterpret_cast<const bf16x8*>(a.Q + int64_t(start + i) * a.ldq + int64_t(j) * D + ks * 32 + lh * 8);
-    }
+    for (int ks = 0; ks < KS; ++ks) qf[qb][ks] = *reinterpret_cast<const bf16x8*>(q + ks * 32);
   }
   f32x4 acc[QB][DB];
   float m_run[QB], l_run[QB];
@@ -322,19 +327,8 @@ __device__ __forceinline__ void chunk_tiles(const ChunkArgs& a, const int wg, un
     m_run[qb] = -INFINITY, l_run[qb] = 0.f;
   }
 
-  // Page numbers of 16 tiles' four blocks, one a lane, and which of them there are not; the next 16 tiles' are on their way.
-  const int32_t* const row_of_table = a.table + int64_t(seq) * a.ldt;
-  auto pages_from = [&](int t) {
-    const int key = (t + lane / 4) * kTileKeys + (lane & 3) * kBlock;
-    return key < end ? row_of_table[key >> a.page_log2] : 0;
-  };
-  auto missing = [&](int pg) { return __ballot(pg < 0 || pg >= a.n_pages); };
-  int32_t pages = pages_from(t_lo), pages_next = pages_from(t_lo + 16);
+  arrived(pages);
   uint64_t bad = missing(pages), bad_now = bad;  // (bad_now: of the tiles that are multiplied, which follow those that are requested)
-#pragma unroll
-  for (int qb = 0; qb < QB; ++qb)
-#pragma unroll
-    for (int ks = 0; ks < KS; ++ks) arrived(qf[qb][ks]);
 
   // this wavefront's block of tile t: where it is, and how many of its tokens count
   auto place = [&](int t, int& valid, int64_t& page, int64_t& in) {
@@ -591,6 +585,10 @@ __device__ __forceinline__ void chunk_tiles(const ChunkArgs& a, const int wg, un
       request(t_lo, 0);
     }
   }
+#pragma unroll
+  for (int qb = 0; qb < QB; ++qb)
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) arrived(qf[qb][ks]);
   for (int t = t_lo; t < t_hi; t += 2) {
     tile_step(std::integral_constant<int, 0>{}, t);
     if (t + 1 < t_hi) tile_step(std::integral_constant<int, 1>{}, t + 1);
@@ -645,7 +643,8 @@ __device__ __forceinline__ void chunk_tiles_join(const ChunkArgs& a, const int w
   __shared__ float2 sums_of[G];
   TilePlan plan;
   plan.units = a.plan[0], plan.total = a.plan[1], plan.piece_tiles = a.plan[2];
-  if (plan.total == plan.units) return;
+  // (Numbers that something else wrote there, a call on another stream with the same workspace, must not lead out of it: this and the test of the last piece's place.)
+  if (plan.total == plan.units || plan.units < 0 || plan.units >= 2 * a.slots) return;
   plan.load(a, threadIdx.x & 63);
   const int grp = threadIdx.x / L, c = int(threadIdx.x) % L * 8;
   int ways = 1;  // groups of lanes of a row
@@ -653,7 +652,7 @@ __device__ __forceinline__ void chunk_tiles_join(const ChunkArgs& a, const int w
   const int per_unit = kTileRows / (G / ways), way = grp % ways;
   for (int job = wg; job < plan.units * per_unit; job += n_wgs) {
     const int first = plan.find_unit(a, job / per_unit), np = plan.n_pieces;
-    if (np == 1) continue;
+    if (first < 0 || np <= 1 || first + int64_t(np - 1) * plan.tiles_there >= 2 * a.slots) continue;
     const Heads hd(a, a.kv_first + plan.head);
     const int heads = hd.j1 - hd.j0, in_tile = job % per_unit * (G / ways) + grp / ways, rr = plan.tile * kTileRows + in_tile;
     const bool there = rr < min(plan.seq_n, a.max_new) * heads;
