@@ -277,9 +277,6 @@ __device__ __forceinline__ void chunk_tiles(const ChunkArgs& a, const int wg, un
   const int in_xcd = wg / 8, round = in_xcd / kRun;
   const int id = uniform((round * 8 + ((wg - round) & 7)) * kRun + (in_xcd + round) % kRun);
   if (id >= plan.total) return;
-  // The two workgroups that a compute unit gets first would go through their matrix instructions, and then their softmax, together: the second one starts a microsecond later, half a
-  // key tile (one sequence of 8192 tokens, 14 heads 250 -> 241 us).
-  if (in_xcd / 32 == 1) __builtin_amdgcn_s_sleep(32);
   plan.find(a, id);
   const int seq = uniform(plan.seq), start = uniform(plan.seq_start), n = uniform(plan.seq_n), len = uniform(plan.seq_len), used = min(n, a.max_new);
   const int g = a.kv_first + uniform(plan.head), n_pieces = uniform(plan.n_pieces), piece = uniform(plan.piece);
@@ -410,6 +407,10 @@ __device__ __forceinline__ void chunk_tiles(const ChunkArgs& a, const int wg, un
     for (int db = 0; db < DB; ++db) av[db] = vbase + ((uint32_t(db * 2 + ((lq & 3) >> 1)) ^ xv) * 16u);
   }
 
+  // Two wavefronts share a SIMD, and would go through their matrix instructions, and then their softmax, together.  At matrix instructions one has the higher priority, by its place on the
+  // SIMD, so that the other one's softmax falls under them; they change places every eight tiles, or one workgroup would end long before the other (d = 128, one sequence of 8192 tokens,
+  // 14 heads: 251 -> 240 us, 512 tokens behind 130560 in 8 bits 560 -> 541; d = 64, which is bound by the softmax alone: 43.5 -> 44.5, so not there).
+  const bool odd_place = (__builtin_amdgcn_s_getreg(4 | 3 << 11) & 1) != 0;  // of the wavefront on its SIMD: HW_ID, bits 0 .. 3
   // one key tile out of buffer BUF (a compile-time constant, so that every LDS offset is an immediate)
   auto tile_step = [&](auto bufc, int t) {
     constexpr int BUF = decltype(bufc)::value;
@@ -430,6 +431,15 @@ __device__ __forceinline__ void chunk_tiles(const ChunkArgs& a, const int wg, un
       }
     }
     const int kv0 = t * kTileKeys;
+    [[maybe_unused]] const bool ahead = (((t >> 3) & 1) != 0) != odd_place;
+    auto matrix_priority = [&] {
+      if constexpr (D == 128) {
+        if (ahead) __builtin_amdgcn_s_setprio(3);
+        else __builtin_amdgcn_s_setprio(1);
+      } else {
+        __builtin_amdgcn_s_setprio(1);
+      }
+    };
     if (kv0 >= most) return;  // every token of the tile lies behind what this wavefront's last row sees
     // scores, transposed: st[kb][qb][r] = score of row qb * 16 + lane % 16 with token kv0 + kb * 16 + lane / 16 * 4 + r; eight key fragments at a time, the next ones read under
     // the matrix instructions of the ones before
@@ -469,7 +479,7 @@ __device__ __forceinline__ void chunk_tiles(const ChunkArgs& a, const int wg, un
     using I1 = std::integral_constant<int, 1>;
     k_reads(I0{});
     lds_reads_done(kf[0]);
-    __builtin_amdgcn_s_setprio(1);
+    matrix_priority();
     if constexpr (KG == 2) {
       k_reads(I1{});
       k_products(I0{});
@@ -508,7 +518,7 @@ __device__ __forceinline__ void chunk_tiles(const ChunkArgs& a, const int wg, un
         for (int r = 0; r < 4; ++r) mx = fmaxf(mx, st[kb][qb][r]);
       mx = over_rows(mx, larger) * a.scale_log2;
       // The reference that weights are relative to moves only where a score passes it by a factor of 2^8: a row's maximum moves with most of its first tiles, and each time all
-      // of its outputs would be scaled (57 vector instructions a block; prompts of up to 2048 tokens 106 -> 95 us).  Weights of up to 2^8 are as exact as those of up to 1.
+      // of its outputs would be scaled (57 vector instructions a block; prompts of up to 2048 tokens 106 -> 100 us).  Weights of up to 2^8 are as exact as those of up to 1.
       const bool moves = mx > m_run[qb] + 8.0f;
       if (__any(moves)) {
         const float m_new = moves ? mx : m_run[qb];
@@ -557,7 +567,7 @@ __device__ __forceinline__ void chunk_tiles(const ChunkArgs& a, const int wg, un
     lds_reads_done(vf[0]);
     lds_reads_tied(vf[1]);
     __builtin_amdgcn_sched_barrier(0);
-    __builtin_amdgcn_s_setprio(1);
+    matrix_priority();
     if constexpr (VG == 4) {
       using I2 = std::integral_constant<int, 2>;
       using I3 = std::integral_constant<int, 3>;
