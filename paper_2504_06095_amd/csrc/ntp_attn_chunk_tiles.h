@@ -407,10 +407,11 @@ __device__ __forceinline__ void chunk_tiles(const ChunkArgs& a, const int wg, un
     for (int db = 0; db < DB; ++db) av[db] = vbase + ((uint32_t(db * 2 + ((lq & 3) >> 1)) ^ xv) * 16u);
   }
 
-  // Two wavefronts share a SIMD, and would go through their matrix instructions, and then their softmax, together.  At matrix instructions one has the higher priority, by its place on the
-  // SIMD, so that the other one's softmax falls under them; they change places every eight tiles, or one workgroup would end long before the other (d = 128, one sequence of 8192 tokens,
-  // 14 heads: 251 -> 240 us, 512 tokens behind 130560 in 8 bits 560 -> 541; d = 64, which is bound by the softmax alone: 43.5 -> 44.5, so not there).
-  const bool odd_place = (__builtin_amdgcn_s_getreg(4 | 3 << 11) & 1) != 0;  // of the wavefront on its SIMD: HW_ID, bits 0 .. 3
+  // Two wavefronts share a SIMD, and would go through their matrix instructions, and then their softmax, together.  With a priority for each phase, the highest for the last product, one comes
+  // before the other and the other one's vector work falls under its matrix instructions (one sequence of 8192 tokens, 14 heads: 251 us with one priority for both products -> 235; 512
+  // tokens behind 130560, 16 heads: 514 -> 487).  8-bit pages: what turns the next tile to bf16 waits for the softmax too (512 tokens behind 130560: 558 -> 540, so 520; bf16 of 64 columns,
+  // which has none of it: 164 -> 172, so not there).
+  constexpr int FIRST = FP8 ? 2 : 1, SOFTMAX = FP8 ? 1 : 0, SECOND = 3;
   // one key tile out of buffer BUF (a compile-time constant, so that every LDS offset is an immediate)
   auto tile_step = [&](auto bufc, int t) {
     constexpr int BUF = decltype(bufc)::value;
@@ -431,15 +432,6 @@ __device__ __forceinline__ void chunk_tiles(const ChunkArgs& a, const int wg, un
       }
     }
     const int kv0 = t * kTileKeys;
-    [[maybe_unused]] const bool ahead = (((t >> 3) & 1) != 0) != odd_place;
-    auto matrix_priority = [&] {
-      if constexpr (D == 128) {
-        if (ahead) __builtin_amdgcn_s_setprio(3);
-        else __builtin_amdgcn_s_setprio(1);
-      } else {
-        __builtin_amdgcn_s_setprio(1);
-      }
-    };
     if (kv0 >= most) return;  // every token of the tile lies behind what this wavefront's last row sees
     // scores, transposed: st[kb][qb][r] = score of row qb * 16 + lane % 16 with token kv0 + kb * 16 + lane / 16 * 4 + r; eight key fragments at a time, the next ones read under
     // the matrix instructions of the ones before
@@ -479,7 +471,7 @@ __device__ __forceinline__ void chunk_tiles(const ChunkArgs& a, const int wg, un
     using I1 = std::integral_constant<int, 1>;
     k_reads(I0{});
     lds_reads_done(kf[0]);
-    matrix_priority();
+    __builtin_amdgcn_s_setprio(FIRST);
     if constexpr (KG == 2) {
       k_reads(I1{});
       k_products(I0{});
@@ -488,7 +480,7 @@ __device__ __forceinline__ void chunk_tiles(const ChunkArgs& a, const int wg, un
     v_reads(I0{});
     v_reads(I1{});
     k_products(std::integral_constant<int, KG - 1>{});
-    __builtin_amdgcn_s_setprio(0);
+    __builtin_amdgcn_s_setprio(SOFTMAX);
 
     const uint32_t gone = uint32_t(bad_now >> (((t - t_lo) & 15) << 2)) & 15u;  // blocks whose pages there are not
     const bool edge = kv0 + kTileKeys > all_see || w0 + 16 * QB > rows;
@@ -567,7 +559,7 @@ __device__ __forceinline__ void chunk_tiles(const ChunkArgs& a, const int wg, un
     lds_reads_done(vf[0]);
     lds_reads_tied(vf[1]);
     __builtin_amdgcn_sched_barrier(0);
-    matrix_priority();
+    __builtin_amdgcn_s_setprio(SECOND);
     if constexpr (VG == 4) {
       using I2 = std::integral_constant<int, 2>;
       using I3 = std::integral_constant<int, 3>;
