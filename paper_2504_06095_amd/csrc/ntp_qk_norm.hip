@@ -81,8 +81,10 @@ __device__ __forceinline__ void angles(float2 (*cs)[kMaxPairs], const int32_t* p
     double turns = double(positions[row0 + t]) * inv_freq[p] * 0.15915494309189533577;  // 1 / (2 pi)
     turns -= rint(turns);
     float s, c;
-    sincospif(2.0f * float(turns), &s, &c);
-    cs[t][p] = float2{c, s};
+    const float near = float(turns);
+    sincospif(2.0f * near, &s, &c);
+    const float rest = float(turns - double(near)) * 6.28318530717958648f;  // of the angle; up to 9e-8, more than fp32 rounds sine and cosine by
+    cs[t][p] = float2{fmaf(-s, rest, c), fmaf(c, rest, s)};
   }
 }
 
