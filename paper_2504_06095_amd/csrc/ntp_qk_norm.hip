@@ -73,7 +73,7 @@ __device__ __forceinline__ float over_same(float v) {
 }
 
 // cos and sin of the positions' angles of a workgroup's tokens, formed and reduced to less than half a turn in fp64
-__device__ __forceinline__ void angles(float2 (*cs)[kMaxPairs], const int32_t* positions, const double* inv_freq, int row0, int M, int tokens, int half) {
+__device__ __forceinline__ void angles(float2 (*cs)[kMaxPairs], const int32_t* positions, const double* inv_freq, int row0, int M, int tokens, int half, bool exact) {
   const int rows = min(tokens, M - row0);
 #pragma unroll 1
   for (int i = threadIdx.x; i < rows * half; i += int(blockDim.x)) {
@@ -83,7 +83,8 @@ __device__ __forceinline__ void angles(float2 (*cs)[kMaxPairs], const int32_t* p
     float s, c;
     const float near = float(turns);
     sincospif(2.0f * near, &s, &c);
-    const float rest = float(turns - double(near)) * 6.28318530717958648f;  // of the angle; up to 9e-8, more than fp32 rounds sine and cosine by
+    // What that rounding left of the angle, up to 9e-8, more than sine and cosine are rounded by.  Without norms the call is ntp_kv_append_shard's, bit for bit, which goes without.
+    const float rest = exact ? float(turns - double(near)) * 6.28318530717958648f : 0.f;
     cs[t][p] = float2{fmaf(-s, rest, c), fmaf(c, rest, s)};
   }
 }
@@ -167,6 +168,7 @@ __global__ __launch_bounds__(kMaxThreads) void qk_norm_append_kernel(const Appen
   __shared__ float2 cs[2][kMaxTokens][kMaxPairs];
   const Place<D> at(a.deal, a.rotary_dim, a.interleaved);
   const int M = int(a.M), step = int(gridDim.x) * a.deal.tokens, half = a.rotary_dim / 2;
+  const bool exact = a.q_gamma || a.k_gamma;
   for (int head = at.head; head - at.head < a.deal.heads; head += at.stride) {  // (one pass but for very many heads)
     const bool is_q = head < a.q_cnt, is_v = head >= a.q_cnt + a.kv_cnt, mine = head < a.deal.heads && at.token < a.deal.tokens;
     const uint16_t* const gamma = is_q ? a.q_gamma : is_v ? nullptr : a.k_gamma;
@@ -192,7 +194,7 @@ __global__ __launch_bounds__(kMaxThreads) void qk_norm_append_kernel(const Appen
     };
     fetch();
     __syncthreads();  // (the pass before has used the angles)
-    if (row0 < M) angles(cs[0], a.positions, a.inv_freq, row0, M, a.deal.tokens, half);
+    if (row0 < M) angles(cs[0], a.positions, a.inv_freq, row0, M, a.deal.tokens, half, exact);
     for (int buf = 0; row0 < M; buf ^= 1) {
       __syncthreads();
       const bool there = mine && row0 + at.token < M;
@@ -209,14 +211,16 @@ __global__ __launch_bounds__(kMaxThreads) void qk_norm_append_kernel(const Appen
 #pragma unroll
           for (int k = 0; k < 8; ++k) ss = fmaf(x[k], x[k], fmaf(y[k], y[k], ss));
           ss = over_head<D>(ss, add);
-          const float rstd = rsqrtf(ss * (1.0f / D) + a.eps);
+          // (products of two bf16 numbers are exact; a step of Newton's takes the reciprocal root from one step of fp32 to half of one: e4m3 borders show what fp32 loses)
+          const float mean = ss * (1.0f / D) + a.eps, root = rsqrtf(mean);
+          const float rstd = mean < INFINITY ? fmaf(0.5f * root, fmaf(-mean * root, root, 1.0f), root) : root;
           float w[8];
           unpack(gw0, w);
 #pragma unroll
-          for (int k = 0; k < 8; ++k) x[k] = x[k] * rstd * w[k];
+          for (int k = 0; k < 8; ++k) x[k] = x[k] * w[k] * rstd;
           unpack(gw1, w);
 #pragma unroll
-          for (int k = 0; k < 8; ++k) y[k] = y[k] * rstd * w[k];
+          for (int k = 0; k < 8; ++k) y[k] = y[k] * w[k] * rstd;
         }
         if (turned) turn(x, y, &cs[buf][at.token][8 * at.j], a.interleaved, 1.0f);
         const bool changed = gamma || turned;  // (what is copied is copied bit for bit)
@@ -251,7 +255,7 @@ __global__ __launch_bounds__(kMaxThreads) void qk_norm_append_kernel(const Appen
         }
       }
       out += int64_t(step) * ldout;
-      if (row0 < M) angles(cs[buf ^ 1], a.positions, a.inv_freq, row0, M, a.deal.tokens, half);
+      if (row0 < M) angles(cs[buf ^ 1], a.positions, a.inv_freq, row0, M, a.deal.tokens, half, exact);
     }
   }
 }
@@ -277,7 +281,7 @@ __global__ __launch_bounds__(kMaxThreads) void qk_norm_bwd_kernel(const BwdArgs 
   const Place<D> at(a.deal, a.rotary_dim, a.interleaved);
   const int M = int(a.M), step = int(gridDim.x) * a.deal.tokens;
   const int half = a.rotary_dim / 2, wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
-  const bool wanted = a.parts || a.d_q || a.d_k;
+  const bool wanted = a.parts || a.d_q || a.d_k, exact = a.q_gamma || a.k_gamma;
   if (wanted)
     for (int i = lane; i < 2 * D; i += 64) sums[wave][i / D][i % D] = 0.f;
   for (int head = at.head; head - at.head < a.deal.heads; head += at.stride) {  // (one pass but for very many heads)
@@ -299,7 +303,7 @@ __global__ __launch_bounds__(kMaxThreads) void qk_norm_bwd_kernel(const BwdArgs 
     };
     fetch();
     __syncthreads();  // (the pass before has used the angles)
-    if (row0 < M) angles(cs[0], a.positions, a.inv_freq, row0, M, a.deal.tokens, half);
+    if (row0 < M) angles(cs[0], a.positions, a.inv_freq, row0, M, a.deal.tokens, half, exact);
     for (int buf = 0; row0 < M; buf ^= 1) {
       __syncthreads();
       const bool there = mine && row0 + at.token < M;
@@ -344,7 +348,7 @@ __global__ __launch_bounds__(kMaxThreads) void qk_norm_bwd_kernel(const BwdArgs 
         }
       }
       out += int64_t(step) * a.lddqkv;
-      if (row0 < M) angles(cs[buf ^ 1], a.positions, a.inv_freq, row0, M, a.deal.tokens, half);
+      if (row0 < M) angles(cs[buf ^ 1], a.positions, a.inv_freq, row0, M, a.deal.tokens, half, exact);
     }
     if (wanted) {  // heads of both kinds may stand in a wavefront: one kind after the other
 #pragma unroll
