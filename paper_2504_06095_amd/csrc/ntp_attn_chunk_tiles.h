@@ -1,4 +1,6 @@
-// Chunk attention, sequences of many rows: the matrix instructions bound it.
+// Chunk attention, sequences of many rows: 4 d operations a (row, token) on the matrix pipe, about five vector instructions beside them for the softmax, which bound it together (512
+// tokens behind 130560, 16 heads on one KV head: bf16 471 us, 1.16 PFLOP/s, 8 bits 522, the pipe busy for 44 % and the vector unit for 53 % of it; one prompt of 8192 tokens, 14 heads:
+// 231 us, 1.04 PFLOP/s; d = 64: 164 us).
 //
 // A workgroup takes 128 rows (token i, head h of a KV head's G: number i G + h) of a sequence and KV head, a wavefront 32 of them in two blocks of 16, and walks over the
 // tokens that they see in tiles of 64, which all wavefronts share: two buffers a matrix, one barrier a tile, two workgroups a compute unit.  Grouped heads stand in one tile,
@@ -6,7 +8,8 @@
 // 16); 8-bit ones through registers, where they become bf16 (exact: e4m3 times a power of two) before the LDS, once for all wavefronts: converted where fragments
 // are read it would be four times the work, on the vector unit that the softmax needs.
 //
-// Where a batch has fewer tiles than the GPU has room for, walks are cut into pieces, by the lengths on the device, whose partial results a second kernel joins.
+// Where a batch has fewer tiles than the GPU has room for, walks are cut into pieces, by the lengths on the device, whose partial results a second kernel joins
+// (512 tokens behind 130560: 64 tiles in 512 pieces; their join 9 us).
 #ifndef NTP_ATTN_CHUNK_TILES_H_
 #define NTP_ATTN_CHUNK_TILES_H_
 
