@@ -518,7 +518,10 @@ int ntp_qk_norm_shard_bwd(ntp_handle_t* h, const ntp_kv_append_shape_t* shape, c
  *               head all of whose scores are -inf; rows of no sequence (the padding of a batch) stay as they are
  *   LSE         DEVICE fp32 [q_cnt x M], may be NULL: natural logarithm of the sum of exp(score); -inf in both of these cases
  * No output may alias another buffer.  What lies in the pages behind a sequence's last token is not used (it may be NaN).  A NaN or an infinity among the values of one of the sequence's own
- * tokens may reach rows before it too (a weight of 0 times NaN).  M * q_cnt < 2^31, q_cnt <= 2^20, max_len <= 2^30,
+ * tokens may reach rows before it too (a weight of 0 times NaN).
+ * Scores, sums and the products' sums are fp32.  A softmax weight goes into the product with the values as its bf16 rounding and what that leaves (2^-16 of it is lost) where a sequence has up to 32 rows
+ * (its new tokens, at most max_new, times the most query heads that a KV head has), beside whatever else, and as its bf16 rounding alone (2^-8 of it) where it has more, where a KV head has more than 32
+ * query heads, and in a batch of one sequence with room for more (min(M, max_new)).  M * q_cnt < 2^31, q_cnt <= 2^20, max_len <= 2^30,
  * n_seq (max_len / 64 + 2) kv_cnt < 2^31, n_seq (min(M, max_new) q_cnt / 128 + kv_cnt) < 2^31 and n_seq kv_cnt < 2^24 (UNSUPPORTED beyond).  With a workspace of ntp_workspace_bytes (NTP_CALL_ATTN_CHUNK_SHARD) walks over many tokens
  * are cut into parts where there are few rows, and their order of fp32 sums then depends on the lengths of the whole batch (the same lengths give the same bits); a smaller one is not used. */
 typedef struct ntp_attn_chunk_shape {

@@ -336,10 +336,9 @@ __device__ __forceinline__ void chunk_rows(const ChunkArgs& a, const int wg, uns
             if (!there || key0 + t >= sees[qb]) st[qb][b][r] = -INFINITY;
         }
     }
-    // weights as operand B of the second product, per 32 tokens: bf16, half a step of 2^-8 each; with one block of rows, where registers and matrix instructions are plenty, also what
-    // that leaves, rounded to bf16 too, in a product of its own (as ntp_attn_decode.hip)
-    constexpr bool REST = QB == 1;
-    bf16x8 pf[QB][NB / 2], pr[REST ? NB / 2 : 1];
+    // weights as operand B of the second product, per 32 tokens: bf16, and what that leaves, rounded to bf16 too, in a product of its own (as ntp_attn_decode.hip): 2^-16 of a weight
+    // is lost, whatever else is in the batch.  The matrix pipe has room for it: HBM and latency bound these walks
+    bf16x8 pf[QB][NB / 2], pr[QB][NB / 2];
 #pragma unroll
     for (int qb = 0; qb < QB; ++qb) {
       float mx = -INFINITY;
@@ -360,7 +359,7 @@ __device__ __forceinline__ void chunk_rows(const ChunkArgs& a, const int wg, uns
           if constexpr (FP8) p *= pv[b][r];
           const __bf16 top = static_cast<__bf16>(p);
           pf[qb][b / 2][(b & 1) * 4 + r] = top;
-          if constexpr (REST) pr[b / 2][(b & 1) * 4 + r] = static_cast<__bf16>(p - static_cast<float>(top));
+          pr[qb][b / 2][(b & 1) * 4 + r] = static_cast<__bf16>(p - static_cast<float>(top));
         }
       l_run[qb] = l_run[qb] * alpha + ls;  // of this lane's tokens; the four lane groups are added at the end
       m_run[qb] = m_new;
@@ -396,7 +395,7 @@ __device__ __forceinline__ void chunk_rows(const ChunkArgs& a, const int wg, uns
 #pragma unroll
         for (int qb = 0; qb < QB; ++qb) {
           acc[qb][db] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v8, pf[qb][s2], acc[qb][db], 0, 0, 0);
-          if constexpr (REST) acc[qb][db] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v8, pr[s2], acc[qb][db], 0, 0, 0);
+          acc[qb][db] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v8, pr[qb][s2], acc[qb][db], 0, 0, 0);
         }
       }
     if constexpr (MORE) {
