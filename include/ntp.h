@@ -470,8 +470,8 @@ int ntp_attn_decode_shard(ntp_handle_t* h, const ntp_attn_decode_shape_t* shape,
  * elements (NTP_KV_E4M3): element (page, g, t, c) is an e4m3 number (OCP, no infinities) at page * page_stride + (g * page_size + t) * head_dim + c,
  * and the token's values of head g are those numbers times 2^(b - 127), b the byte at page * exp_stride + g * page_size + t of K_exp or V_exp (the E8M0
  * code).  b is the smallest for which no finite value of the head is above 448 * 2^(b - 127), at least 16 (heads of values below 448 * 2^-111 lose precision), and
- * 127 for a head of zeros; values are rounded once, to the nearest number (ties to even), NaN and infinities become NaN.  Bytes that a caller writes itself
- * lie in 16 .. 246.
+ * 127 for a head of zeros; values are rounded once, to the nearest number (ties to even; at b = 247 to 240 at most, whose 2^120-fold is the largest that bf16 holds), NaN and infinities
+ * become NaN.  Bytes that a caller writes itself lie in 16 .. 247, at 247 with numbers of up to 240.
  *   page_size as ntp_kv_cache_t; page_stride: elements, at least kv_cnt * page_size * head_dim and a multiple of 8 (E4M3: of 16); exp_stride:
  *   bytes, at least kv_cnt * page_size and a multiple of 16 (K_exp, V_exp and exp_stride count with E4M3 only); all base pointers 16-byte aligned. */
 #define NTP_KV_BF16 0

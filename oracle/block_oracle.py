@@ -174,11 +174,13 @@ def to_e4m3(u):
 
 
 def heads_to_8_bits(x):
-    """e4m3 numbers and bytes of heads x [..., d]: values above the type's range of the head's largest finite one, NaN for what is not finite."""
+    """e4m3 numbers and bytes of heads x [..., d]: values above the type's range of the head's largest finite one, NaN for what is not finite.  At byte 247 numbers of at most 240: 256 2^120 is no
+    number of bf16."""
     fine = np.isfinite(x)
     code = e4m3_code(np.where(fine, np.abs(x), 0.0).max(-1))
     u = np.where(fine, x, 0.0) * np.ldexp(1.0, 127 - code)[..., None]
-    return np.where(fine, to_e4m3(u), np.nan), code
+    top = np.where(code > 246, 240.0, 448.0)[..., None]
+    return np.where(fine, np.clip(to_e4m3(u), -top, top), np.nan), code
 
 
 def attn_chunk(Q, K, V, starts, table, lengths, max_new, max_len, q_off, kv_off, group):

@@ -166,6 +166,15 @@ __device__ __forceinline__ u32x2 to_e4m3(const float (&f)[8], float down) {
   return out;
 }
 
+// In units of 2^120 the number 256, next to values above 248, would be 2^128, which neither fp32 nor bf16 holds: 240 instead.  Codes 0x78 become 0x77; there are none between them and NaN.
+__device__ __forceinline__ void most_240(u32x2& v, bool where) {
+#pragma unroll
+  for (int w = 0; w < 2; ++w) {
+    const uint32_t high = ((v[w] & 0x78787878u) + 0x08080808u) >> 7, nan = ((v[w] & 0x07070707u) + 0x01010101u) >> 3;
+    v[w] -= where ? high & ~nan & 0x01010101u : 0u;
+  }
+}
+
 template <int D, bool FP8>
 __global__ __launch_bounds__(kMaxThreads) void qk_norm_append_kernel(const AppendArgs a) {
   __shared__ float2 cs[2][kMaxTokens][kMaxPairs];
@@ -251,8 +260,10 @@ __global__ __launch_bounds__(kMaxThreads) void qk_norm_append_kernel(const Appen
             code = top == 0.f ? 127 : max(code, 16);
             const float down = __builtin_bit_cast(float, uint32_t(254 - code) << 23);
             unsigned char* const to = (is_v ? a.V : a.K) + place;
-            *reinterpret_cast<u32x2*>(to + c0) = to_e4m3(x, down);
-            *reinterpret_cast<u32x2*>(to + c1) = to_e4m3(y, down);
+            u32x2 x8 = to_e4m3(x, down), y8 = to_e4m3(y, down);
+            if (__any(code > 246)) most_240(x8, code > 246), most_240(y8, code > 246);  // (nearly no wavefront)
+            *reinterpret_cast<u32x2*>(to + c0) = x8;
+            *reinterpret_cast<u32x2*>(to + c1) = y8;
             if (at.j == 0) (is_v ? a.V_exp : a.K_exp)[page * a.exp_stride + in_head] = uint8_t(code);
           }
         }
