@@ -107,8 +107,8 @@ struct TilePlan {
     const float slots = float(a.slots), share = work / slots;
     if (a.parts == 1 || (a.parts == 0 && most <= 1.3f * share)) return;  // (longest first, whole walks end together)
     if (a.n_seq > 64) {  // (not looked at piece by piece)
-      if (units >= a.slots || most <= 1.5f * share) return;
-      piece_tiles = max(kMinPiece, int(ceilf(share)));
+      if (a.parts == 0 && (units >= a.slots || most <= 1.5f * share)) return;
+      piece_tiles = max(kMinPiece, int(ceilf(a.parts > 0 ? most / float(a.parts) : share)));
       int pieces = 0, c, p;
       for (int from = 0; from < a.n_seq; from += kAtOnce) {
         sums(a, from, c, p);
