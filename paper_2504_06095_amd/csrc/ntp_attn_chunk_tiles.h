@@ -86,7 +86,8 @@ struct TilePlan {
     auto add = [&](const TilePlan& p) {
       const int c = p.tiles.all(a);
       count += c;
-      work += float(c) * (float(p.walk) - float(min(p.n, a.max_new)) * (0.5f / kTileKeys));  // (half a triangle less)
+      const int used = min(p.n, a.max_new), rows = min(used, max(p.len - p.n + used, 0));  // (rows that see something)
+      work += float(c) * (float(p.walk) - float(rows) * (0.5f / kTileKeys));  // (half a triangle less)
       if (c > 0) most = fmaxf(most, float(p.walk));
     };
     if (a.n_seq <= 64) {

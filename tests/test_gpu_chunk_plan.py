@@ -42,3 +42,16 @@ def test_parts_are_those_of_the_option(others, fmt, d):
         C, LSE, written = _run(c, parts)
         assert _pieces(c, written, whole) == 2 * pieces
         c.check(C, LSE)
+
+
+@pytest.mark.parametrize("fmt", [16, 8])
+@pytest.mark.parametrize("others", [10, 68])
+def test_sequences_shorter_than_their_rows_do_not_count_against_the_work(others, fmt):
+    """64 tokens behind 31936 (8 row tiles of 500 key tiles), whose walks are worth cutting, beside 2048 rows of a sequence of 5 tokens (256
+    row tiles of one): rows that see nothing save no work.  8 * 499.5 + 256 key tiles at most are 8.3 for each of 512 places, and 16.6 for half of them: 30 pieces a walk at least."""
+    _say(f"a long walk beside rows that see nothing and {others} single tokens, {fmt} bits")
+    c = Case([1] * others + [2048, 64], [i % 50 for i in range(others)] + [5, 32000], 16, 1, 64, 64, 0, 0, 16, fmt, seed=2)
+    _, _, whole = _run(c, 1)
+    C, LSE, written = _run(c)
+    assert _pieces(c, written, whole) >= 8 * 30
+    c.check(C, LSE)
