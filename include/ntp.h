@@ -500,7 +500,8 @@ int ntp_qk_norm_append_shard(ntp_handle_t* h, const ntp_kv_append_shape_t* shape
 /* Gradient of the norms and the rotation.  QKV: what the forward call read (not overwritten in place); dQ [M x q_cnt head_dim], dK [M x kv_cnt head_dim]: gradients at
  * Qout and Kout.  Writes the query and key columns of dQKV [M x (q_cnt + 2 kv_cnt) head_dim] (the value columns stay as they are) and the gradients of the gammas,
  * fp32 [head_dim], 4-byte aligned, sums over the tokens and the heads that share them (either may be NULL: not wanted; a gradient of a gamma that is NULL is refused); accumulate != 0 adds into them.  dQ and dK may be the query and key
- * columns of dQKV itself (ntp_attn_core_shard_bwd's dQKV, with its leading dimension); no other aliasing (of dQKV with QKV, dQ or dK: refused).  Deterministic: the order of the sums is fixed by the shape, the handle and
+ * columns of dQKV itself (ntp_attn_core_shard_bwd's dQKV, with its leading dimension); no other aliasing (of dQKV with QKV, dQ or dK, and of the two gradients of gammas
+ * with each other: refused; one gamma for queries and keys has both, which the caller adds).  Deterministic: the order of the sums is fixed by the shape, the handle and
  * whether its workspace has room for their partial sums (ntp_workspace_bytes, NTP_CALL_QK_NORM; without it one workgroup forms them in a pass of its own: slow). */
 int ntp_qk_norm_shard_bwd(ntp_handle_t* h, const ntp_kv_append_shape_t* shape, const ntp_qk_norm_t* norm, const void* QKV, int64_t ldqkv, const void* dQ, int64_t lddq,
                           const void* dK, int64_t lddk, const int32_t* positions, const double* inv_freq, void* dQKV, int64_t lddqkv, float* d_q_gamma,

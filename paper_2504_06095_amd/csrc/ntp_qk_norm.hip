@@ -14,6 +14,7 @@
 #include <algorithm>
 #include <cmath>
 #include <cstdint>
+#include <functional>
 
 #include "ntp_internal.h"
 #include "ntp_kv_cache.h"
@@ -504,6 +505,7 @@ extern "C" int ntp_qk_norm_shard_bwd(ntp_handle_t* h, const ntp_kv_append_shape_
   if ((d_q_gamma && (!norm || !norm->q_gamma)) || (d_k_gamma && (!norm || !norm->k_gamma))) return NTP_ERR_INVALID_ARG;
   const int64_t d = s->head_dim, wq = s->q_cnt * d, wk = s->kv_cnt * d, w = wq + 2 * wk;
   if (off(d_q_gamma, 4) || off(d_k_gamma, 4)) return NTP_ERR_ALIGNMENT;
+  if (d_q_gamma && d_k_gamma && std::less<>{}(d_q_gamma, d_k_gamma + d) && std::less<>{}(d_k_gamma, d_q_gamma + d)) return NTP_ERR_INVALID_ARG;  // (they are written side by side)
   const bool rows = s->M > 0 && wq + wk > 0;
   if (rows) {
     if (!QKV || !dQKV || (wq > 0 && !dQ) || (wk > 0 && !dK) || (s->rotary_dim > 0 && (!positions || !inv_freq)) || ldqkv < w || lddqkv < w || (wq > 0 && lddq < wq) ||
