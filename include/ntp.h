@@ -670,7 +670,9 @@ int ntp_reshard_plan_destroy(ntp_reshard_plan_t* plan);
  * Measurement aid (not part of the method).  When enabled, every kernel the
  * library enqueues is bracketed by two HIP events on the caller's stream and
  * recorded with its algorithmic work: flops = 2 M N K on the logical GEMM
- * dimensions, bytes = bytes read + bytes written by a reshard launch.  This is
+ * dimensions, bytes = bytes read + bytes written by a reshard launch.  Attention over
+ * pages: of one new token flops of max_len tokens a sequence, a bound; of chunks neither,
+ * since only the device knows the lengths.  This is
  * the only part of the library that creates HIP objects (events); it is off by
  * default and per handle.  ntp_kernel_timing_read waits for the recorded
  * kernels, writes at most max_records entries (launch order), stores the number

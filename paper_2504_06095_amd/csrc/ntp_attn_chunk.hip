@@ -191,7 +191,7 @@ extern "C" int ntp_attn_chunk_shard(ntp_handle_t* h, const ntp_attn_chunk_shape_
   a.kv_first = c.kv_first, a.kv_used = c.kv_used, a.gmax = c.gmax, a.g_first = c.g_first, a.g_last = c.g_last, a.cap = c.cap, a.shares = c.shares, a.tile_wgs = int32_t(c.tile_wgs), a.slots = c.slots, a.parts = int32_t(h->opt[NTP_OPT_ATTN_PARTS]);
   a.scale_log2 = float(1.4426950408889634 / std::sqrt(double(s->head_dim)));
   hipStream_t hs = static_cast<hipStream_t>(stream);
-  if (ntp::timing_on(h)) ntp::timing_begin(h, stream, fp8 ? "attn_chunk8" : "attn_chunk", 4.0 * double(s->M) * double(s->max_len) * s->head_dim * s->q_cnt, 0.0);
+  if (ntp::timing_on(h)) ntp::timing_begin(h, stream, fp8 ? "attn_chunk8" : "attn_chunk", 0.0, 0.0);  // (lengths are on the device)
   const bool ok = s->head_dim == 128 ? (fp8 ? launch_chunk<128, true>(a, c, hs) : launch_chunk<128, false>(a, c, hs))
                                      : (fp8 ? launch_chunk<64, true>(a, c, hs) : launch_chunk<64, false>(a, c, hs));
   ntp::timing_end(h, stream);

@@ -55,3 +55,16 @@ def test_sequences_shorter_than_their_rows_do_not_count_against_the_work(others,
     C, LSE, written = _run(c)
     assert _pieces(c, written, whole) >= 8 * 30
     c.check(C, LSE)
+
+
+@pytest.mark.parametrize("fmt,name", [(16, "attn_chunk"), (8, "attn_chunk8")])
+def test_timing_records_name_no_work_that_only_the_device_knows(fmt, name):
+    """Bounds far above the lengths: no count of operations that follows from them is the call's."""
+    c = Case([3, 50], [30, 100], 4, 1, 64, 16, 0, 0, 4, fmt, max_len=100000, max_new=50)
+    N, h = c.N, c.N.ntp_create()
+    N.ntp_kernel_timing_enable(True, handle=h)
+    C = c.torch.empty(c.M, 256, dtype=c.torch.bfloat16, device="cuda")
+    N.ntp_attn_chunk_shard(c.shape, c.pages, c.Q, c.starts_dev, c.table, c.len_dev, C, handle=h)
+    records = N.ntp_kernel_timing_read(handle=h)
+    N.ntp_destroy(h)
+    assert [(r["name"], r["flops"], r["bytes"]) for r in records] == [(name, 0.0, 0.0)] and records[0]["ms"] > 0
