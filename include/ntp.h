@@ -508,7 +508,8 @@ int ntp_qk_norm_shard_bwd(ntp_handle_t* h, const ntp_kv_append_shape_t* shape, c
                           float* d_k_gamma, int32_t accumulate, void* stream);
 
 /* Attention of the new tokens of a batch of sequences over their pages, the new tokens' own keys and values, appended before, included: one token a
- * sequence, a few (proposed tokens checked at once), the chunk of a long prompt, whole packed prompts, or all of them in one call.  Sequence s has the rows
+ * sequence, a few (proposed tokens checked at once), the chunk of a long prompt, whole packed prompts, or all of them in one call.  (One token of every sequence over bf16 pages, up to 16 query heads a
+ * KV head: ntp_attn_decode_shard computes the same and takes up to a tenth less of small calls; with more heads this call, which reads a KV head's tokens once for up to 128 of them, is the faster one.)  Sequence s has the rows
  * row_starts[s] .. row_starts[s + 1] - 1 of Q and C; its n rows are the last n of its lengths[s] tokens, so that its row i sees the first lengths[s] - n + i + 1 of them:
  *   C[row, j] = softmax(q_j K_g^T / sqrt(head_dim)) V_g     over those tokens, KV head g of query head j as in ntp_attn_core_shard_fwd.
  *   Q           [M x q_cnt head_dim] bf16, rotated: Qout of the append

@@ -1,5 +1,5 @@
 // Chunk attention, sequences of few rows (tokens x query heads of a KV head: up to 16 or 32): every key and value is read once for all of them, HBM bounds it (one new token of 64
-// sequences of up to 8192, 14 heads, 8 bits: 162 us and 5 in the join, 6.1 TB/s; four tokens of 32 sequences of up to 4100, 8 heads on one: 13.5 and 4, latency).
+// sequences of up to 8192, 14 heads, 8 bits: 163 us and 5 in the join, 6.1 TB/s; four tokens of 32 sequences of up to 4100, 8 heads on one: 14 and 4, latency).
 //
 // A unit is a sequence and KV head; its rows (token i, head h: number i G + h) are the columns of the matrix instruction, as in ntp_attn_decode.hip: both products run on the
 // 16x16x32 bf16 instruction with the row on the lane axis (S^T = K Q^T, O^T += V^T P^T), one or two blocks of 16 rows a wavefront.  The units' steps form a line, which is cut into equal shares, two workgroups per
@@ -337,7 +337,7 @@ __device__ __forceinline__ void chunk_rows(const ChunkArgs& a, const int wg, uns
         }
     }
     // weights as operand B of the second product, per 32 tokens: bf16, and what that leaves, rounded to bf16 too, in a product of its own (as ntp_attn_decode.hip): 2^-16 of a weight
-    // is lost, whatever else is in the batch.  The matrix pipe has room for it: HBM and latency bound these walks
+    // is lost, whatever else is in the batch.  The matrix pipe has room for it: HBM and latency bound these walks (four tokens of 32 sequences, 8 heads on one: 17.8 -> 18.1 us with the rest)
     bf16x8 pf[QB][NB / 2], pr[QB][NB / 2];
 #pragma unroll
     for (int qb = 0; qb < QB; ++qb) {

@@ -1,6 +1,6 @@
 // Chunk attention, sequences of many rows: 4 d operations a (row, token) on the matrix pipe, about five vector instructions beside them for the softmax, which bound it together (512
-// tokens behind 130560, 16 heads on one KV head: bf16 471 us, 1.16 PFLOP/s, 8 bits 522, the pipe busy for 44 % and the vector unit for 53 % of it; one prompt of 8192 tokens, 14 heads:
-// 231 us, 1.04 PFLOP/s; d = 64: 164 us).
+// tokens behind 130560, 16 heads on one KV head: bf16 472 us, 1.16 PFLOP/s, 8 bits 513, the pipe busy for 44 % and the vector unit for 53 % of it; one prompt of 8192 tokens, 14 heads:
+// 234 us, 1.03 PFLOP/s; d = 64: 162 us).
 //
 // A workgroup takes 128 rows (token i, head h of a KV head's G: number i G + h) of a sequence and KV head, a wavefront 32 of them in two blocks of 16, and walks over the
 // tokens that they see in tiles of 64, which all wavefronts share: two buffers a matrix, one barrier a tile, two workgroups a compute unit.  Grouped heads stand in one tile,
@@ -9,7 +9,8 @@
 // are read it would be four times the work, on the vector unit that the softmax needs.
 //
 // Where a batch has fewer tiles than the GPU has room for, walks are cut into pieces, by the lengths on the device, whose partial results a second kernel joins
-// (512 tokens behind 130560: 64 tiles in 512 pieces; their join 9 us).
+// (512 tokens behind 130560: 64 tiles in 512 pieces; their join 9 us).  Up to 64 sequences, one a lane, are looked at together: whole walks go longest first, and the best of several cuts is
+// taken.  Of more, whole walks go as they stand in the batch (64 prompts of up to 512 tokens, 14 heads: 97 us, 65: 108) and one cut is tried.
 #ifndef NTP_ATTN_CHUNK_TILES_H_
 #define NTP_ATTN_CHUNK_TILES_H_
 
@@ -158,7 +159,7 @@ struct TilePlan {
     return PerHead{from(tiles.first, a.g_first), from(tiles.middle, a.gmax), from(tiles.last, a.g_last)};
   }
   static constexpr int kLevel = 8;  // key tiles
-  // x < total: its sequence, KV head, row tile, and piece.  Where there are more whole walks than places, the longest come first, whosever they are, by levels of their lengths: tiles of a
+  // x < total: its sequence, KV head, row tile, and piece.  Whole walks of up to 64 sequences come longest first, whosever they are, by levels of their lengths: tiles of a
   // level are numbered sequence by sequence, head by head.
   int seq, head, tile, piece, n_pieces, seq_start, seq_n, seq_len;
   __device__ __forceinline__ void find(const ChunkArgs& a, int x) {
@@ -535,7 +536,8 @@ __device__ __forceinline__ void chunk_tiles(const ChunkArgs& a, const int wg, un
           ls += pr[kb][r];
         }
       l_run[qb] += ls;
-      // weights as bf16: half a step of 2^-8 each, of a mean of values that is rounded to the same
+      // weights as bf16: half a step of 2^-8 each, of a mean of values that is rounded to the same (errors against 64 bits 0.0019 to 0.0022, of fp32 weights 0.0017); what that leaves in a
+      // product of its own, as for few rows, would be half as many matrix instructions again on the pipe that bounds this
 #pragma unroll
       for (int s2 = 0; s2 < 2; ++s2)
 #pragma unroll

@@ -7,7 +7,7 @@
 // Backward: with u = R^T dy, xh = x rstd and w = u .* gamma:  dx = rstd (w - xh (w . xh) / d),  dgamma = sum over tokens and heads of u .* xh.  rstd is formed again
 // from x, which the gradient reads anyway: nothing is kept by the forward call.
 //
-// HBM bounds both: 8192 tokens, 14 heads of 128 of each kind, into 8-bit pages 33 us (5.3 TB/s; the vector unit issues for 87 % of it), the gradient at 405B shape 26 us (5.1 TB/s) and 5
+// HBM bounds both: 8192 tokens, 14 heads of 128 of each kind, into 8-bit pages 32-35 us (5.0-5.5 TB/s; the vector unit issues for 86 % of it), into bf16 ones 32 (6.4), the gradient at 405B shape 26 us (5.1 TB/s) and 5
 // in the second launch; small calls cost their launch (4 us).
 #include <hip/hip_runtime.h>
 
